@@ -283,6 +283,80 @@ typedef struct {
 CONDENSA_API int condensa_lstep_update(condensa_ctx *ctx, const condensa_opt_tensor *tensors, int T,
                                        float mu, const condensa_opt *opt, void *stream);
 
+/* ---- AdamW over a tensor list, and the norm that clips its gradient.
+ *
+ * The L step of a language model, and of the low-rank adapters below: decoupled weight decay,
+ * gradients in 32 or 16 bits, moments in 32 or 8 bits, an optional 16-bit copy of the new weights
+ * for the next forward pass, one launch for the list (one per 360 tensors). No call here copies
+ * anything from the host or allocates, except that condensa_grad_norm() grows a small workspace
+ * (partial sums) the first time; both can be captured into a CUDA graph after one plain call.
+ *
+ * Per element, in this order of single fp32 operations (`grad` widened to fp32 first):
+ *     g = grad_scale * grad;    [theta given:  d = w - theta;  p = mu*d;  q = p - lambda;  g = g + q]
+ *     [clip given:  g = coef * g]
+ *     m' = beta1*m + (1-beta1)*g;  v' = beta2*v + (1-beta2)*(g*g);  r' = sqrt(v')
+ *     w' = w*(1 - lr*weight_decay)  -  step_size * ( m' / ( r'*root_corr + eps ) )
+ * with step_size = lr/(1-beta1^step), root_corr = 1/sqrt(1-beta2^step) and 1 - lr*weight_decay
+ * formed in double from the fp32 parameters and rounded once (1-beta in fp32).
+ *
+ * States in 8 bits (state_dtype CONDENSA_DTYPE_FP8_E4M3): m and r = sqrt(v) are held as E4M3 codes in
+ * blocks of CONDENSA_STATE_BLOCK elements (counted from the tensor's start; the last may be shorter)
+ * under one fp32 power of two each: scale = 2^(e-7), e the exponent of the block's largest finite
+ * magnitude, at least 2^-126; code = E4M3(x / scale), round to nearest even. A positive r never
+ * becomes 0 (its code is at least 1, i.e. scale * 2^-9), so that a small second moment cannot turn into a
+ * division by eps; a value that is not finite becomes NaN. w' is formed from m' and r' before they
+ * are rounded. Zero states are zero bytes with any finite scale. */
+#define CONDENSA_STATE_BLOCK 256
+enum { CONDENSA_DTYPE_FP32 = 0 };
+
+typedef struct {
+    float *w;               /* i/o: weights, fp32                                                  */
+    const float *theta;     /* in : compressed weights, NULL: no penalty gradient                  */
+    const float *lambda;    /* in : multipliers, NULL: 0 (read only with theta)                    */
+    const void *grad;       /* in : loss gradient, grad_dtype                                      */
+    void *m;                /* i/o: first moment, fp32 or E4M3 codes                               */
+    void *v;                /* i/o: second moment, fp32, or E4M3 codes of its root                 */
+    float *m_scale;         /* i/o: 8-bit states: one per block of 256 elements                    */
+    float *v_scale;         /* i/o: the same for the root of the second moment                     */
+    uint16_t *w_h;          /* out: w' rounded to w_h_dtype. NULL: not written                     */
+    int64_t numel;
+} condensa_adamw_tensor;
+
+typedef struct {
+    float lr, beta1, beta2, eps, weight_decay;
+    float grad_scale;       /* factor on the loss gradient, e.g. one over a loss scale             */
+    int64_t step;           /* 1-based                                                             */
+    int32_t grad_dtype;     /* CONDENSA_DTYPE_FP32, _FP16 or _BF16                                 */
+    int32_t state_dtype;    /* CONDENSA_DTYPE_FP32 or _FP8_E4M3                                    */
+    int32_t w_h_dtype;      /* CONDENSA_DTYPE_FP16 or _BF16; read where a w_h is given             */
+    int32_t reserved;       /* 0                                                                   */
+} condensa_adamw;
+
+/* What condensa_grad_norm() leaves on the device. */
+typedef struct {
+    float norm;             /* L2 norm of the whole list's gradient                                */
+    float coef;             /* min(1, max_norm / (norm + 1e-6)); 1 when max_norm <= 0              */
+    float finite;           /* 1, or 0 when the norm is not finite                                 */
+    float reserved;         /* 0                                                                   */
+} condensa_clip;
+
+/* `clip` (DEVICE, may be NULL): the step uses clip->coef, and where clip->finite is 0 it leaves
+ * every buffer as it was (a step skipped on an overflow), decided on the device. */
+CONDENSA_API int condensa_lstep_adamw(condensa_ctx *ctx, const condensa_adamw_tensor *tensors, int T,
+                                      float mu, const condensa_adamw *opt, const condensa_clip *clip,
+                                      void *stream);
+
+/* Norm of the gradient g (before clipping) that condensa_lstep_adamw() would form from the same
+ * arguments: reads grad and, where theta is given, w, theta and lambda; the other fields are
+ * not looked at. Squares are summed in fp64 in an order that depends on the list and the device
+ * only, so equal inputs give equal bits. `clip` (DEVICE) receives the record, `norms` (DEVICE, T
+ * floats, may be NULL) the norm of each tensor (0 for an empty one). A norm beyond fp32 reads as
+ * infinite. max_norm <= 0: the norm is only measured. A captured call must not run while another
+ * call of the context runs. */
+CONDENSA_API int condensa_grad_norm(condensa_ctx *ctx, const condensa_adamw_tensor *tensors, int T,
+                                    float mu, int grad_dtype, float grad_scale, float max_norm,
+                                    condensa_clip *clip, float *norms, void *stream);
+
 /* Operation selector for condensa_cstep_host(). */
 enum { CONDENSA_OP_PRUNE = 0, CONDENSA_OP_FILTER = 1, CONDENSA_OP_BLOCK = 2,
        CONDENSA_OP_QUANTIZE = 3, CONDENSA_OP_LAGRANGE = 4 };

@@ -9,35 +9,59 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcondensa_cstep.so")
-SOURCES = ["api.cu"]
-HEADERS = ["common.cuh", "elementwise.cuh", "select.cuh", "structured.cuh", "fused.cuh", "fused_fast.cuh", "fused_blockg.cuh",
-           "sample.cuh", "lstep.cuh", "thin.cuh", "small_select.cuh", "small_prune.cuh",
-           os.path.join("..", "..", "include", "condensa_cstep.h")]
+OBJ = os.path.join(HERE, "build")
+API_H = os.path.join("..", "..", "include", "condensa_cstep.h")
+# each source with the headers it includes (they are compiled side by side)
+SOURCES = {
+    "api.cu": ["common.cuh", "ctx.cuh", "elementwise.cuh", "select.cuh", "structured.cuh", "fused.cuh", "fused_fast.cuh",
+               "fused_blockg.cuh", "sample.cuh", "lstep.cuh", "thin.cuh", "small_select.cuh", "small_prune.cuh", API_H],
+    "adamw.cu": ["common.cuh", "ctx.cuh", "adamw.cuh", API_H],
+}
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-              "--shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
+              "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
               "--ftz=false", "--prec-div=true", "--prec-sqrt=true"]
 
 
+def _deps(src):
+    return [os.path.join(CSRC, f) for f in [src] + SOURCES[src]] + [os.path.abspath(__file__)]
+
+
+def _older(path, deps) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps)
+
+
 def stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS] + [os.path.abspath(__file__)]
-    return any(os.path.getmtime(d) > t for d in deps)
+    return any(_older(LIB, _deps(s)) for s in SOURCES)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + \
-        ["-o", LIB + ".tmp"] + [os.path.join(CSRC, s) for s in SOURCES]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or r.returncode:
-        sys.stderr.write(r.stdout + r.stderr)
+    os.makedirs(OBJ, exist_ok=True)
+    jobs, objects = [], []
+    for src in SOURCES:
+        obj = os.path.join(OBJ, src + ".o")
+        objects.append(obj)
+        if force or _older(obj, _deps(src)):
+            cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", obj + ".tmp", os.path.join(CSRC, src)]
+            jobs.append((src, obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    failed = []
+    for src, obj, p in jobs:
+        out = p.communicate()[0]
+        if verbose or p.returncode:
+            sys.stderr.write(out)
+        if p.returncode:
+            failed.append(src)
+        else:
+            os.replace(obj + ".tmp", obj)
+    if failed:
+        raise RuntimeError("nvcc failed on %s" % ", ".join(failed))
+    r = subprocess.run([nvcc] + NVCC_FLAGS + ["--shared", "-o", LIB + ".tmp"] + objects, capture_output=True, text=True)
     if r.returncode:
-        raise RuntimeError("nvcc failed building %s" % LIB)
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("nvcc failed linking %s" % LIB)
     os.replace(LIB + ".tmp", LIB)
     return LIB
 

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "ctx.cuh"
 #include "elementwise.cuh"
 #include "select.cuh"
 #include "structured.cuh"
@@ -32,83 +33,6 @@ using namespace cs;
 static_assert(sizeof(condensa_result) == sizeof(cs::Result), "result layouts must agree");
 
 namespace {
-
-std::string g_create_error;
-
-struct KernelInfo {
-    int occ = 0;     // CTAs per SM
-};
-
-struct DeviceMirror {   // device copies used by condensa_cstep_host
-    char *buf = nullptr;
-    size_t bytes = 0;
-};
-
-}  // namespace
-
-struct condensa_ctx {
-    int device = 0;
-    int num_sms = 0;
-    bool coop = false;
-    std::string err;
-    char *ws = nullptr;
-    size_t ws_bytes = 0;
-    char *h_stage = nullptr;        // pinned staging of the descriptor upload
-    size_t h_stage_bytes = 0;
-    cudaEvent_t stage_ev = nullptr;
-    cudaEvent_t tail_ev = nullptr;  // recorded behind the last kernel of every call
-    bool tail_recorded = false;
-    uint64_t seed = 0;              // sample positions of the single-pass path
-    std::vector<char> last_upload;  // what the device descriptor area holds now
-    char *last_upload_dst = nullptr;
-    int64_t launches = 0;
-    cudaStream_t last_stream = nullptr;
-    bool has_result = false;
-    Ctl *ctl = nullptr;
-    int occ_select[4] = {0, 0, 0, 0};
-    int occ_stream = 0;
-    int occ_filter = 0;
-    int occ_prune_small = 0;        // resident CTAs per SM of the register-resident small-list kernel
-    bool small_smem_set = false;    // dynamic shared memory limit of k_select_small raised on this device
-    bool block_smem_set = false;    // the same for the tiled block kernel
-    size_t blockg_smem_set = 0;     // ... and for the tiled bh x bw kernel (bytes it has been allowed so far)
-    DeviceMirror mirror;
-    // optional per-kernel timing (event pair around every launch)
-    bool prof_on = false;
-    std::vector<cudaEvent_t> prof_ev;       // start/stop pairs
-    std::vector<int> prof_name;             // index into prof_names per pair
-    std::vector<std::string> prof_names;
-    size_t prof_used = 0;                   // pairs recorded since the last read
-    std::vector<double> prof_ms;            // accumulated per name
-    std::vector<int64_t> prof_cnt;
-};
-
-namespace {
-
-int fail(condensa_ctx *c, int code, const char *fmt, ...)
-{
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof(buf), fmt, ap);
-    va_end(ap);
-    if (c) c->err = buf; else g_create_error = buf;
-    return code;
-}
-
-#define CU_TRY(ctx, call)                                                                   \
-    do {                                                                                    \
-        cudaError_t e_ = (call);                                                            \
-        if (e_ != cudaSuccess)                                                              \
-            return fail(ctx, CONDENSA_ERR_CUDA, "%s: %s", #call, cudaGetErrorString(e_));   \
-    } while (0)
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-struct Interval {
-    uintptr_t lo, hi;
-    bool out;
-};
 
 // Layout of one call's workspace.
 struct Layout {
@@ -413,87 +337,6 @@ int occupancy(K kernel)
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, kernel, THREADS, 0) != cudaSuccess) occ = 1;
     return occ < 1 ? 1 : occ;
 }
-
-int stream_grid(condensa_ctx *ctx, long long n_items, int occ)
-{
-    long long g = (long long)ctx->num_sms * occ;
-    if (g > n_items) g = n_items;
-    if (g < 1) g = 1;
-    return (int)g;
-}
-
-int prof_begin(condensa_ctx *ctx, const char *name, cudaStream_t stream)
-{
-    if (!ctx->prof_on) return 0;
-    if (ctx->prof_used * 2 + 2 > ctx->prof_ev.size()) {
-        for (int i = 0; i < 2; ++i) {
-            cudaEvent_t e;
-            if (cudaEventCreate(&e) != cudaSuccess) return 0;
-            ctx->prof_ev.push_back(e);
-        }
-    }
-    int id = -1;
-    for (size_t i = 0; i < ctx->prof_names.size(); ++i)
-        if (ctx->prof_names[i] == name) id = (int)i;
-    if (id < 0) {
-        id = (int)ctx->prof_names.size();
-        ctx->prof_names.push_back(name);
-        ctx->prof_ms.push_back(0.0);
-        ctx->prof_cnt.push_back(0);
-    }
-    if (ctx->prof_name.size() <= ctx->prof_used) ctx->prof_name.resize(ctx->prof_used + 1);
-    ctx->prof_name[ctx->prof_used] = id;
-    cudaEventRecord(ctx->prof_ev[ctx->prof_used * 2], stream);
-    return 1;
-}
-
-void prof_end(condensa_ctx *ctx, int active, cudaStream_t stream)
-{
-    if (!active) return;
-    cudaEventRecord(ctx->prof_ev[ctx->prof_used * 2 + 1], stream);
-    ctx->prof_used += 1;
-}
-
-// Folds the recorded event pairs into the per-kernel totals (synchronises).
-void prof_collect(condensa_ctx *ctx)
-{
-    for (size_t i = 0; i < ctx->prof_used; ++i) {
-        float ms = 0.0f;
-        cudaEventSynchronize(ctx->prof_ev[2 * i + 1]);
-        if (cudaEventElapsedTime(&ms, ctx->prof_ev[2 * i], ctx->prof_ev[2 * i + 1]) == cudaSuccess) {
-            ctx->prof_ms[ctx->prof_name[i]] += ms;
-            ctx->prof_cnt[ctx->prof_name[i]] += 1;
-        }
-    }
-    ctx->prof_used = 0;
-}
-
-// Launch configuration with the programmatic-dependent-launch attribute (dropped while every
-// kernel is bracketed by an event pair: nothing can overlap then).
-struct PdlLaunch {
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr;
-    PdlLaunch(const condensa_ctx *ctx, int grid, int block, size_t smem, cudaStream_t stream)
-    {
-        memset(&cfg, 0, sizeof(cfg));
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr.val.programmaticStreamSerializationAllowed = 1;
-        cfg.gridDim = dim3((unsigned)grid);
-        cfg.blockDim = dim3((unsigned)block);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = stream;
-        cfg.attrs = &attr;
-        cfg.numAttrs = ctx->prof_on ? 0 : 1;
-    }
-};
-
-#define LAUNCH_CHECK(ctx)                                                                    \
-    do {                                                                                     \
-        cudaError_t e_ = cudaGetLastError();                                                 \
-        if (e_ != cudaSuccess)                                                               \
-            return fail(ctx, CONDENSA_ERR_CUDA, "kernel launch: %s", cudaGetErrorString(e_)); \
-        ctx->launches += 1;                                                                  \
-    } while (0)
 
 template <int SRC>
 int launch_select(condensa_ctx *ctx, Params &P, int first_listed, int pre_scan, cudaStream_t stream,
@@ -997,6 +840,8 @@ int condensa_destroy(condensa_ctx *ctx)
     cudaDeviceSynchronize();
     if (ctx->ws) cudaFree(ctx->ws);
     if (ctx->mirror.buf) cudaFree(ctx->mirror.buf);
+    if (ctx->op_ws) cudaFree(ctx->op_ws);
+    if (ctx->op_ev) cudaEventDestroy(ctx->op_ev);
     if (ctx->h_stage) cudaFreeHost(ctx->h_stage);
     if (ctx->stage_ev) cudaEventDestroy(ctx->stage_ev);
     if (ctx->tail_ev) cudaEventDestroy(ctx->tail_ev);

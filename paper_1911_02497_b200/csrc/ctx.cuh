@@ -1,0 +1,236 @@
+// What every source file of the host side shares: the context, error texts, per-kernel timing,
+// launch helpers, the workspace of the list operators and the adapters.
+#pragma once
+#include "../../include/condensa_cstep.h"
+
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <cstring>
+#include <string>
+#include <vector>
+
+#include "common.cuh"
+
+using cs::Ctl;
+
+inline std::string g_create_error;   // text of a failure without a context
+
+struct KernelInfo {
+    int occ = 0;     // CTAs per SM
+};
+
+struct DeviceMirror {   // device copies used by condensa_cstep_host
+    char *buf = nullptr;
+    size_t bytes = 0;
+};
+
+struct condensa_ctx {
+    int device = 0;
+    int num_sms = 0;
+    bool coop = false;
+    std::string err;
+    char *ws = nullptr;
+    size_t ws_bytes = 0;
+    char *h_stage = nullptr;        // pinned staging of the descriptor upload
+    size_t h_stage_bytes = 0;
+    cudaEvent_t stage_ev = nullptr;
+    cudaEvent_t tail_ev = nullptr;  // recorded behind the last kernel of every call
+    bool tail_recorded = false;
+    uint64_t seed = 0;              // sample positions of the single-pass path
+    std::vector<char> last_upload;  // what the device descriptor area holds now
+    char *last_upload_dst = nullptr;
+    int64_t launches = 0;
+    cudaStream_t last_stream = nullptr;
+    bool has_result = false;
+    Ctl *ctl = nullptr;
+    int occ_select[4] = {0, 0, 0, 0};
+    int occ_stream = 0;
+    int occ_filter = 0;
+    int occ_prune_small = 0;        // resident CTAs per SM of the register-resident small-list kernel
+    bool small_smem_set = false;    // dynamic shared memory limit of k_select_small raised on this device
+    bool block_smem_set = false;    // the same for the tiled block kernel
+    size_t blockg_smem_set = 0;     // ... and for the tiled bh x bw kernel (bytes it has been allowed so far)
+    DeviceMirror mirror;
+    // optional per-kernel timing (event pair around every launch)
+    bool prof_on = false;
+    std::vector<cudaEvent_t> prof_ev;       // start/stop pairs
+    std::vector<int> prof_name;             // index into prof_names per pair
+    std::vector<std::string> prof_names;
+    size_t prof_used = 0;                   // pairs recorded since the last read
+    std::vector<double> prof_ms;            // accumulated per name
+    std::vector<int64_t> prof_cnt;
+    // workspace of the list operators and the adapters (partial sums); apart from the C-step's
+    char *op_ws = nullptr;
+    size_t op_ws_bytes = 0;
+    cudaEvent_t op_ev = nullptr;            // recorded behind the last call that used it
+    cudaStream_t op_stream = nullptr;
+    bool op_recorded = false;
+    bool op_capturing = false;              // the call under way is being captured
+};
+
+inline int fail(condensa_ctx *c, int code, const char *fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof(buf), fmt, ap);
+    va_end(ap);
+    if (c) c->err = buf; else g_create_error = buf;
+    return code;
+}
+
+#define CU_TRY(ctx, call)                                                                   \
+    do {                                                                                    \
+        cudaError_t e_ = (call);                                                            \
+        if (e_ != cudaSuccess)                                                              \
+            return fail(ctx, CONDENSA_ERR_CUDA, "%s: %s", #call, cudaGetErrorString(e_));   \
+    } while (0)
+
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+struct Interval {
+    uintptr_t lo, hi;
+    bool out;
+};
+
+inline int stream_grid(condensa_ctx *ctx, long long n_items, int occ)
+{
+    long long g = (long long)ctx->num_sms * occ;
+    if (g > n_items) g = n_items;
+    if (g < 1) g = 1;
+    return (int)g;
+}
+
+inline int prof_begin(condensa_ctx *ctx, const char *name, cudaStream_t stream)
+{
+    if (!ctx->prof_on) return 0;
+    if (ctx->prof_used * 2 + 2 > ctx->prof_ev.size()) {
+        for (int i = 0; i < 2; ++i) {
+            cudaEvent_t e;
+            if (cudaEventCreate(&e) != cudaSuccess) return 0;
+            ctx->prof_ev.push_back(e);
+        }
+    }
+    int id = -1;
+    for (size_t i = 0; i < ctx->prof_names.size(); ++i)
+        if (ctx->prof_names[i] == name) id = (int)i;
+    if (id < 0) {
+        id = (int)ctx->prof_names.size();
+        ctx->prof_names.push_back(name);
+        ctx->prof_ms.push_back(0.0);
+        ctx->prof_cnt.push_back(0);
+    }
+    if (ctx->prof_name.size() <= ctx->prof_used) ctx->prof_name.resize(ctx->prof_used + 1);
+    ctx->prof_name[ctx->prof_used] = id;
+    cudaEventRecord(ctx->prof_ev[ctx->prof_used * 2], stream);
+    return 1;
+}
+
+inline void prof_end(condensa_ctx *ctx, int active, cudaStream_t stream)
+{
+    if (!active) return;
+    cudaEventRecord(ctx->prof_ev[ctx->prof_used * 2 + 1], stream);
+    ctx->prof_used += 1;
+}
+
+// Folds the recorded event pairs into the per-kernel totals (synchronises).
+inline void prof_collect(condensa_ctx *ctx)
+{
+    for (size_t i = 0; i < ctx->prof_used; ++i) {
+        float ms = 0.0f;
+        cudaEventSynchronize(ctx->prof_ev[2 * i + 1]);
+        if (cudaEventElapsedTime(&ms, ctx->prof_ev[2 * i], ctx->prof_ev[2 * i + 1]) == cudaSuccess) {
+            ctx->prof_ms[ctx->prof_name[i]] += ms;
+            ctx->prof_cnt[ctx->prof_name[i]] += 1;
+        }
+    }
+    ctx->prof_used = 0;
+}
+
+// Launch configuration with the programmatic-dependent-launch attribute (dropped while every
+// kernel is bracketed by an event pair: nothing can overlap then).
+struct PdlLaunch {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr;
+    PdlLaunch(const condensa_ctx *ctx, int grid, int block, size_t smem, cudaStream_t stream)
+    {
+        memset(&cfg, 0, sizeof(cfg));
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3((unsigned)grid);
+        cfg.blockDim = dim3((unsigned)block);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = stream;
+        cfg.attrs = &attr;
+        cfg.numAttrs = ctx->prof_on ? 0 : 1;
+    }
+};
+
+#define LAUNCH_CHECK(ctx)                                                                    \
+    do {                                                                                     \
+        cudaError_t e_ = cudaGetLastError();                                                 \
+        if (e_ != cudaSuccess)                                                               \
+            return fail(ctx, CONDENSA_ERR_CUDA, "kernel launch: %s", cudaGetErrorString(e_)); \
+        ctx->launches += 1;                                                                  \
+    } while (0)
+
+// An output range may overlap nothing else of the call. Sorts `iv`.
+inline bool ranges_clash(std::vector<Interval> &iv)
+{
+    auto before = [](const Interval &a, const Interval &b) { return a.lo < b.lo; };
+    if (!std::is_sorted(iv.begin(), iv.end(), before)) std::sort(iv.begin(), iv.end(), before);
+    uintptr_t reach = 0, reach_out = 0;
+    for (const Interval &i : iv) {
+        if (i.lo < reach_out || (i.out && i.lo < reach)) return true;
+        reach = std::max(reach, i.hi);
+        if (i.out) reach_out = std::max(reach_out, i.hi);
+    }
+    return false;
+}
+
+// Room for `bytes` in the operators' workspace, ordered behind its last user on another stream.
+// The first 256 bytes hold counters that are zero between calls. Growing waits for the device once,
+// so it cannot happen inside a stream capture; a captured call is not ordered behind other streams
+// (the event would belong to work outside the graph): its replays must not overlap other calls.
+inline int op_workspace(condensa_ctx *ctx, size_t bytes, cudaStream_t stream)
+{
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    CU_TRY(ctx, cudaStreamIsCapturing(stream, &st));
+    ctx->op_capturing = st != cudaStreamCaptureStatusNone;
+    if (ctx->op_capturing) {
+        if (bytes > ctx->op_ws_bytes)
+            return fail(ctx, CONDENSA_ERR_WORKSPACE, "the workspace must grow, which a stream capture does not allow: make the call once before");
+        return CONDENSA_OK;
+    }
+    if (!ctx->op_ev) CU_TRY(ctx, cudaEventCreateWithFlags(&ctx->op_ev, cudaEventDisableTiming));
+    if (bytes > ctx->op_ws_bytes) {
+        CU_TRY(ctx, cudaDeviceSynchronize());
+        if (ctx->op_ws) cudaFree(ctx->op_ws);
+        ctx->op_ws = nullptr;
+        ctx->op_ws_bytes = 0;
+        ctx->op_recorded = false;
+        const size_t want = align_up(bytes + bytes / 4, 1 << 20);
+        const cudaError_t e = cudaMalloc((void **)&ctx->op_ws, want);
+        if (e != cudaSuccess) {
+            cudaGetLastError();
+            ctx->op_ws = nullptr;
+            return fail(ctx, CONDENSA_ERR_WORKSPACE, "cannot allocate %zu bytes of workspace: %s", want, cudaGetErrorString(e));
+        }
+        ctx->op_ws_bytes = want;
+        CU_TRY(ctx, cudaMemsetAsync(ctx->op_ws, 0, 256, stream));
+    } else if (ctx->op_recorded && ctx->op_stream != stream) {
+        CU_TRY(ctx, cudaStreamWaitEvent(stream, ctx->op_ev, 0));
+    }
+    ctx->op_stream = stream;
+    return CONDENSA_OK;
+}
+
+// Behind the last launch of a call that used the operators' workspace.
+inline int op_workspace_done(condensa_ctx *ctx, cudaStream_t stream)
+{
+    if (ctx->op_capturing) return CONDENSA_OK;
+    CU_TRY(ctx, cudaEventRecord(ctx->op_ev, stream));
+    ctx->op_recorded = true;
+    return CONDENSA_OK;
+}

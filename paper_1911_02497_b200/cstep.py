@@ -30,7 +30,8 @@ EXPORTS = ["condensa_create", "condensa_destroy", "condensa_cstep_prune", "conde
            "condensa_cstep_prune_noalloc", "condensa_lstep_update",
            "condensa_cstep_structure", "condensa_thin_flags", "condensa_thin_compact",
            "condensa_count_nonzero", "condensa_set_seed", "condensa_noalloc_status",
-           "condensa_cstep_structured", "condensa_workspace_bytes", "condensa_thin_list"]
+           "condensa_cstep_structured", "condensa_workspace_bytes", "condensa_thin_list",
+           "condensa_lstep_adamw", "condensa_grad_norm"]
 
 
 class CondensaError(RuntimeError):
@@ -91,6 +92,24 @@ class Opt(C.Structure):
 OPT_SGD, OPT_ADAM = 0, 1
 
 
+DTYPE_FP32 = 0
+STATE_BLOCK = 256               # elements that share a scale of the 8-bit states
+
+
+class AdamwTensor(C.Structure):
+    """Mirror of ``condensa_adamw_tensor``."""
+    _fields_ = [("w", C.c_void_p), ("theta", C.c_void_p), ("lam", C.c_void_p), ("grad", C.c_void_p),
+                ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("w_h", C.c_void_p), ("numel", C.c_int64)]
+
+
+class Adamw(C.Structure):
+    """Mirror of ``condensa_adamw``."""
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+                ("weight_decay", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int64),
+                ("grad_dtype", C.c_int32), ("state_dtype", C.c_int32), ("w_h_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
 class KernelTime(C.Structure):
     """Mirror of ``condensa_kernel_time``."""
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int64), ("total_ms", C.c_double)]
@@ -131,6 +150,8 @@ def load():
     L.condensa_thin_compact.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp, vp, vp]
     L.condensa_count_nonzero.argtypes = [vp, C.POINTER(vp), C.POINTER(i64), i32, vp, vp]
     L.condensa_thin_list.argtypes = [vp, C.POINTER(ThinLayer), i32, vp]
+    L.condensa_lstep_adamw.argtypes = [vp, vp, i32, f32, C.POINTER(Adamw), vp, vp]
+    L.condensa_grad_norm.argtypes = [vp, vp, i32, f32, i32, f32, f32, vp, vp, vp]
     L.condensa_launch_count.argtypes = [vp]
     L.condensa_launch_count.restype = C.c_int64
     L.condensa_last_error.argtypes = [vp]
@@ -200,6 +221,66 @@ def opt_table(w, theta, lam, grad, buf1=None, buf2=None):
         e.buf1 = _addr(buf1[t]) if buf1 is not None else None
         e.buf2 = _addr(buf2[t]) if buf2 is not None else None
         e.numel = int(w[t].numel()) if hasattr(w[t], "numel") else int(w[t].size)
+    return tab
+
+
+_DTYPES = {"float32": DTYPE_FP32, "float16": DTYPE_FP16, "bfloat16": DTYPE_BF16, "float8_e4m3fn": DTYPE_FP8_E4M3,
+           "uint8": DTYPE_FP8_E4M3}
+
+
+def _dtype_code(x, allowed, what: str) -> int:
+    code = _DTYPES.get(str(x.dtype).replace("torch.", ""))
+    if code not in allowed:
+        raise TypeError("%s: type %s is not supported" % (what, x.dtype))
+    return code
+
+
+def _contiguous(x) -> bool:
+    return x.is_contiguous() if hasattr(x, "is_contiguous") else bool(x.flags["C_CONTIGUOUS"])
+
+
+def _numel(x) -> int:
+    return int(x.numel()) if hasattr(x, "numel") else int(x.size)
+
+
+class AdamwTable:
+    """A ``condensa_adamw_tensor[T]`` array with the types of its gradients, states and copies."""
+
+    def __init__(self, T: int):
+        self.T, self.entries = T, (AdamwTensor * max(T, 1))()
+        self.grad_dtype, self.state_dtype, self.w_h_dtype = DTYPE_FP32, DTYPE_FP32, DTYPE_FP16
+
+
+def adamw_table(w, grad, m=None, v=None, m_scale=None, v_scale=None, theta=None, lam=None, w_h=None) -> AdamwTable:
+    """Table for :meth:`Context.lstep_adamw` and :meth:`Context.grad_norm` from per-tensor device buffers; a list or an
+    entry of it may be None where the header allows NULL. ``grad`` float32, float16 or bfloat16; ``m`` and ``v`` float32, or
+    float8_e4m3fn (uint8) with a float32 scale per ``STATE_BLOCK`` elements; ``w_h`` float16 or bfloat16. The caller keeps the
+    buffers alive."""
+    tab = AdamwTable(len(grad))
+    kinds = {"grad": set(), "state": set(), "w_h": set()}
+    groups = [("w", w, (DTYPE_FP32,), None), ("theta", theta, (DTYPE_FP32,), None), ("lam", lam, (DTYPE_FP32,), None),
+              ("grad", grad, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "grad"), ("m", m, (DTYPE_FP32, DTYPE_FP8_E4M3), "state"),
+              ("v", v, (DTYPE_FP32, DTYPE_FP8_E4M3), "state"), ("m_scale", m_scale, (DTYPE_FP32,), None),
+              ("v_scale", v_scale, (DTYPE_FP32,), None), ("w_h", w_h, (DTYPE_FP16, DTYPE_BF16), "w_h")]
+    for t in range(tab.T):
+        e = tab.entries[t]
+        e.numel = n = _numel(grad[t])
+        for name, group, allowed, kind in groups:
+            x = group[t] if group is not None else None
+            if x is None:
+                continue
+            code = _dtype_code(x, allowed, "tensor %d: %s" % (t, name))
+            want = -(-n // STATE_BLOCK) if name.endswith("_scale") else n
+            if _numel(x) != want or not _contiguous(x):
+                raise ValueError("tensor %d: %s must be contiguous and hold %d elements" % (t, name, want))
+            setattr(e, name, _addr(x))
+            if kind:
+                kinds[kind].add(code)
+    for kind, codes in kinds.items():
+        if len(codes) > 1:
+            raise TypeError("all tensors of a list share one type of %s" % kind)
+        for code in codes:
+            setattr(tab, kind + "_dtype", code)
     return tab
 
 
@@ -322,6 +403,19 @@ class Context:
         o = Opt({"sgd": OPT_SGD, "adam": OPT_ADAM}[kind], lr, momentum, weight_decay, beta1, beta2, eps, step)
         self._check(self._lib.condensa_lstep_update(self._h, tab, T, float(mu), C.byref(o),
                                                     _stream_handle(stream)))
+
+    def lstep_adamw(self, tab: AdamwTable, mu=0.0, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1,
+                    grad_scale=1.0, clip=None, stream=None):
+        """One AdamW step over the list. ``clip``: the device record of :meth:`grad_norm` (4 float32), or None."""
+        o = Adamw(lr, beta1, beta2, eps, weight_decay, grad_scale, step, tab.grad_dtype, tab.state_dtype, tab.w_h_dtype, 0)
+        self._check(self._lib.condensa_lstep_adamw(self._h, tab.entries, tab.T, mu, C.byref(o), _addr(clip),
+                                                   _stream_handle(stream)))
+
+    def grad_norm(self, tab: AdamwTable, mu, max_norm, clip, norms=None, grad_scale=1.0, stream=None):
+        """Gradient norm of the list: ``clip`` (4 float32 on the device) receives norm, coefficient, finite flag, 0;
+        ``norms`` (T float32, may be None) the norm of each tensor."""
+        self._check(self._lib.condensa_grad_norm(self._h, tab.entries, tab.T, mu, tab.grad_dtype, grad_scale, max_norm,
+                                                 _addr(clip), _addr(norms), _stream_handle(stream)))
 
     def thin_flags(self, theta, d0, d1, inner, axis, keep, stream=None):
         self._check(self._lib.condensa_thin_flags(self._h, _addr(theta), int(d0), int(d1), int(inner), int(axis),
