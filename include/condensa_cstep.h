@@ -357,6 +357,63 @@ CONDENSA_API int condensa_grad_norm(condensa_ctx *ctx, const condensa_adamw_tens
                                     float mu, int grad_dtype, float grad_scale, float max_norm,
                                     condensa_clip *clip, float *norms, void *stream);
 
+/* ---- Low-rank adapters of many requests beside one shared projection.
+ *
+ * A projection that a C-step has compressed stays as it is; what is trained beside it, per task or per
+ * user, is a pair A [rank][k], B [n][rank]. The rows of a batch belong to requests, each a run of
+ * consecutive rows with an adapter of its own or none (-1), in any order and mixture: one token each
+ * when decoding, whole prompts, training sequences. Row i of a request with adapter a:
+ *   forward   h_i = A_a x_i                      y_i  <- y_i + scale_a * (B_a h_i)
+ *   backward  u_i = scale_a * (B_a^T dy_i)       dx_i <- dx_i + A_a^T u_i
+ *             dA_a = sum_i u_i x_i^T             dB_a = scale_a * sum_i dy_i h_i^T
+ * y and dx hold what the shared projection (and its gradient) put there; the adapters' part is added in
+ * fp32 and rounded once. Rows without an adapter are neither read nor written.
+ *
+ * x, y, dy, dx, A and B share one type (CONDENSA_DTYPE_FP32, _FP16, _BF16); h, dA and dB are fp32.
+ * Rows may lie `ld` elements apart; A, B, dA and dB are contiguous. Products of 16-bit types
+ * are exact and summed in fp32; h and u enter the second product as sums of two (gradients of
+ * bfloat16: three) 16-bit parts, fp32 operands as two TF32 parts, so nothing is rounded to 16 bits but
+ * the results. Sums run in an order that depends on the shapes, the requests and the device only.
+ *
+ * The request lists and the adapter table are HOST arrays and are used up when the call returns.
+ * Nothing is copied to the device ahead of the kernels (the lists travel as kernel parameters), so
+ * calls may be captured into a CUDA graph; a captured backward call must not run while another
+ * backward call of the context runs (they share a workspace of partial sums). */
+#define CONDENSA_ADAPTER_MAX_RANK 128
+
+typedef struct {
+    const void *a;          /* [rank][k]                                                          */
+    const void *b;          /* [n][rank]                                                          */
+    float *grad_a;          /* backward: dA, [rank][k] fp32, contiguous. NULL: not formed         */
+    float *grad_b;          /* backward: dB, [n][rank] fp32, contiguous. NULL: not formed         */
+    float scale;
+    int32_t rank;           /* 1 .. CONDENSA_ADAPTER_MAX_RANK, adapters of a call may differ      */
+} condensa_adapter;
+
+typedef struct {
+    const condensa_adapter *adapters;   /* HOST                                                   */
+    int32_t n_adapters;
+    int32_t n_requests;
+    const int64_t *request_rows;        /* HOST: rows of each request, >= 0; they follow one another */
+    const int32_t *request_adapter;     /* HOST: index into adapters, or -1                       */
+    int64_t k, n;                       /* widths of x and y                                      */
+    int32_t dtype;
+    int32_t reserved;                   /* 0                                                      */
+} condensa_adapter_batch;
+
+/* h (NULL: not kept): columns 0..rank-1 of the rows with an adapter are written; what backward needs. */
+CONDENSA_API int condensa_adapter_forward(condensa_ctx *ctx, const condensa_adapter_batch *batch,
+                                          const void *x, int64_t ldx, void *y, int64_t ldy,
+                                          float *h, int64_t ldh, void *stream);
+
+/* dx may be NULL (not formed). With `accumulate` 0 every grad_a and grad_b of the table is overwritten, by
+ * zeros for an adapter without rows; otherwise the sums are added to what is there. x and h are read
+ * where a grad_a resp. grad_b is given, and may be NULL where none is. */
+CONDENSA_API int condensa_adapter_backward(condensa_ctx *ctx, const condensa_adapter_batch *batch,
+                                           const void *x, int64_t ldx, const void *dy, int64_t lddy,
+                                           const float *h, int64_t ldh, void *dx, int64_t lddx,
+                                           int accumulate, void *stream);
+
 /* Operation selector for condensa_cstep_host(). */
 enum { CONDENSA_OP_PRUNE = 0, CONDENSA_OP_FILTER = 1, CONDENSA_OP_BLOCK = 2,
        CONDENSA_OP_QUANTIZE = 3, CONDENSA_OP_LAGRANGE = 4 };

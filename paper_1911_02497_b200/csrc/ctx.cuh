@@ -60,6 +60,7 @@ struct condensa_ctx {
     size_t prof_used = 0;                   // pairs recorded since the last read
     std::vector<double> prof_ms;            // accumulated per name
     std::vector<int64_t> prof_cnt;
+    uint64_t op_smem_set = 0;               // adapter kernels whose shared memory limit has been raised on this device
     // workspace of the list operators and the adapters (partial sums); apart from the C-step's
     char *op_ws = nullptr;
     size_t op_ws_bytes = 0;

@@ -11,6 +11,8 @@ import ctypes as C
 import os
 from typing import Optional, Sequence
 
+import numpy as np
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcondensa_cstep.so")
 
@@ -31,7 +33,7 @@ EXPORTS = ["condensa_create", "condensa_destroy", "condensa_cstep_prune", "conde
            "condensa_cstep_structure", "condensa_thin_flags", "condensa_thin_compact",
            "condensa_count_nonzero", "condensa_set_seed", "condensa_noalloc_status",
            "condensa_cstep_structured", "condensa_workspace_bytes", "condensa_thin_list",
-           "condensa_lstep_adamw", "condensa_grad_norm"]
+           "condensa_lstep_adamw", "condensa_grad_norm", "condensa_adapter_forward", "condensa_adapter_backward"]
 
 
 class CondensaError(RuntimeError):
@@ -110,6 +112,21 @@ class Adamw(C.Structure):
                 ("grad_dtype", C.c_int32), ("state_dtype", C.c_int32), ("w_h_dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
+ADAPTER_MAX_RANK = 128
+
+
+class Adapter(C.Structure):
+    """Mirror of ``condensa_adapter``."""
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("grad_a", C.c_void_p), ("grad_b", C.c_void_p),
+                ("scale", C.c_float), ("rank", C.c_int32)]
+
+
+class AdapterBatch(C.Structure):
+    """Mirror of ``condensa_adapter_batch``."""
+    _fields_ = [("adapters", C.c_void_p), ("n_adapters", C.c_int32), ("n_requests", C.c_int32), ("request_rows", C.c_void_p),
+                ("request_adapter", C.c_void_p), ("k", C.c_int64), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
 class KernelTime(C.Structure):
     """Mirror of ``condensa_kernel_time``."""
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int64), ("total_ms", C.c_double)]
@@ -152,6 +169,8 @@ def load():
     L.condensa_thin_list.argtypes = [vp, C.POINTER(ThinLayer), i32, vp]
     L.condensa_lstep_adamw.argtypes = [vp, vp, i32, f32, C.POINTER(Adamw), vp, vp]
     L.condensa_grad_norm.argtypes = [vp, vp, i32, f32, i32, f32, f32, vp, vp, vp]
+    L.condensa_adapter_forward.argtypes = [vp, C.POINTER(AdapterBatch), vp, i64, vp, i64, vp, i64, vp]
+    L.condensa_adapter_backward.argtypes = [vp, C.POINTER(AdapterBatch), vp, i64, vp, i64, vp, i64, vp, i64, i32, vp]
     L.condensa_launch_count.argtypes = [vp]
     L.condensa_launch_count.restype = C.c_int64
     L.condensa_last_error.argtypes = [vp]
@@ -282,6 +301,59 @@ def adamw_table(w, grad, m=None, v=None, m_scale=None, v_scale=None, theta=None,
         for code in codes:
             setattr(tab, kind + "_dtype", code)
     return tab
+
+
+class AdapterTable:
+    """A ``condensa_adapter`` array: the adapters that are loaded beside one projection of ``k`` to ``n``."""
+
+    def __init__(self, entries, count: int, k: int, n: int, dtype):
+        self.entries, self.count, self.k, self.n, self.dtype = entries, count, k, n, dtype
+        self.code = _DTYPES[str(dtype).replace("torch.", "")]
+        self.address = C.addressof(entries)
+
+
+def adapter_table(a, b, scale, grad_a=None, grad_b=None) -> AdapterTable:
+    """Table for :meth:`Context.adapter_forward` and :meth:`Context.adapter_backward`: ``a[i]`` [rank_i, k] and ``b[i]`` [n, rank_i] of
+    one type (float32, float16, bfloat16) on the device, ``scale[i]`` a number; ``grad_a[i]`` and ``grad_b[i]`` float32 of the same
+    shapes, or None. The caller keeps the buffers alive."""
+    if not len(a) or len(a) != len(b) or len(a) != len(scale):
+        raise ValueError("a, b and scale need one entry per adapter, and at least one")
+    k, n, dtype = int(a[0].shape[1]), int(b[0].shape[0]), a[0].dtype
+    _dtype_code(a[0], (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "adapters")
+    entries = (Adapter * len(a))()
+    for i, e in enumerate(entries):
+        rank = int(a[i].shape[0])
+        wanted = [("a", a[i], (rank, k), dtype), ("b", b[i], (n, rank), dtype)]
+        for name, group, shape in (("grad_a", grad_a, (rank, k)), ("grad_b", grad_b, (n, rank))):
+            if group is not None and group[i] is not None:
+                wanted.append((name, group[i], shape, None))
+        for name, x, shape, kind in wanted:
+            if kind is None:
+                _dtype_code(x, (DTYPE_FP32,), "adapter %d: %s" % (i, name))
+            elif x.dtype != kind:
+                raise TypeError("adapter %d: %s has type %s, the table's is %s" % (i, name, x.dtype, kind))
+            if tuple(x.shape) != shape or not _contiguous(x):
+                raise ValueError("adapter %d: %s must be contiguous, of shape %s" % (i, name, shape))
+            setattr(e, name, _addr(x))
+        e.scale, e.rank = float(scale[i]), rank
+    return AdapterTable(entries, len(a), k, n, dtype)
+
+
+def _rows_of(x, rows: int, width: int, dtype, name: str):
+    """Address and row stride of a [rows, width] matrix whose rows are contiguous."""
+    if x is None:
+        return None, 0
+    if x.dtype != dtype or x.dim() != 2 or x.shape[0] != rows or x.shape[1] < width or (width > 1 and x.stride(1) != 1):
+        raise ValueError("%s must be a [%d, %d] matrix of %s with contiguous rows" % (name, rows, width, dtype))
+    return x.data_ptr(), (x.stride(0) if rows > 1 else max(width, x.stride(0)))
+
+
+def _kept_rows(h, rows: int):
+    if h is None:
+        return None, 0
+    if _DTYPES.get(str(h.dtype).replace("torch.", "")) != DTYPE_FP32 or h.dim() != 2 or h.shape[0] != rows or (h.shape[1] > 1 and h.stride(1) != 1):
+        raise ValueError("h must be a float32 matrix of %d contiguous rows" % rows)
+    return h.data_ptr(), (h.stride(0) if rows > 1 else max(h.shape[1], h.stride(0)))
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -416,6 +488,36 @@ class Context:
         ``norms`` (T float32, may be None) the norm of each tensor."""
         self._check(self._lib.condensa_grad_norm(self._h, tab.entries, tab.T, mu, tab.grad_dtype, grad_scale, max_norm,
                                                  _addr(clip), _addr(norms), _stream_handle(stream)))
+
+    def _adapter_batch(self, tab: AdapterTable, request_rows, request_adapter):
+        """The batch, its number of rows, and the arrays that must live through the call."""
+        rows = np.ascontiguousarray(request_rows, dtype=np.int64)
+        which = np.ascontiguousarray(request_adapter, dtype=np.int32)
+        if rows.shape != which.shape or rows.ndim != 1:
+            raise ValueError("request_rows and request_adapter need one entry per request")
+        return AdapterBatch(tab.address, tab.count, rows.size, rows.ctypes.data, which.ctypes.data, tab.k, tab.n, tab.code, 0), \
+            int(rows.sum()), (rows, which)
+
+    def adapter_forward(self, tab: AdapterTable, request_rows, request_adapter, x, y, h=None, stream=None):
+        """``y += scale (x A^T) B^T`` row by row, each request with its adapter (-1: none). ``request_rows`` and ``request_adapter``:
+        host arrays; ``x`` [rows, k] and ``y`` [rows, n] of the table's type; ``h`` [rows, max rank] float32 receives x A^T for
+        :meth:`adapter_backward`, or None."""
+        batch, m, keep = self._adapter_batch(tab, request_rows, request_adapter)
+        px, ldx = _rows_of(x, m, tab.k, tab.dtype, "x")
+        py, ldy = _rows_of(y, m, tab.n, tab.dtype, "y")
+        ph, ldh = _kept_rows(h, m)
+        self._check(self._lib.condensa_adapter_forward(self._h, C.byref(batch), px, ldx, py, ldy, ph, ldh, _stream_handle(stream)))
+
+    def adapter_backward(self, tab: AdapterTable, request_rows, request_adapter, x, dy, h=None, dx=None, accumulate=False, stream=None):
+        """Gradients of :meth:`adapter_forward`: ``dx`` (may be None) is added to, the table's ``grad_a`` and ``grad_b`` are
+        overwritten, or added to with ``accumulate``."""
+        batch, m, keep = self._adapter_batch(tab, request_rows, request_adapter)
+        px, ldx = _rows_of(x, m, tab.k, tab.dtype, "x")
+        pdy, lddy = _rows_of(dy, m, tab.n, tab.dtype, "dy")
+        pdx, lddx = _rows_of(dx, m, tab.k, tab.dtype, "dx")
+        ph, ldh = _kept_rows(h, m)
+        self._check(self._lib.condensa_adapter_backward(self._h, C.byref(batch), px, ldx, pdy, lddy, ph, ldh, pdx, lddx,
+                                                        1 if accumulate else 0, _stream_handle(stream)))
 
     def thin_flags(self, theta, d0, d1, inner, axis, keep, stream=None):
         self._check(self._lib.condensa_thin_flags(self._h, _addr(theta), int(d0), int(d1), int(inner), int(axis),
