@@ -15,7 +15,10 @@ API_H = os.path.join("..", "..", "include", "condensa_cstep.h")
 SOURCES = {
     "api.cu": ["common.cuh", "ctx.cuh", "elementwise.cuh", "select.cuh", "structured.cuh", "fused.cuh", "fused_fast.cuh",
                "fused_blockg.cuh", "sample.cuh", "lstep.cuh", "thin.cuh", "small_select.cuh", "small_prune.cuh", API_H],
-    "adapter.cu": ["common.cuh", "ctx.cuh", "adapter.cuh", API_H],
+    "adapter.cu": ["common.cuh", "ctx.cuh", "adapter.cuh", "adapter_launch.cuh", API_H],
+    "adapter_bf16.cu": ["common.cuh", "ctx.cuh", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
+    "adapter_f16.cu": ["common.cuh", "ctx.cuh", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
+    "adapter_f32.cu": ["common.cuh", "ctx.cuh", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
     "adamw.cu": ["common.cuh", "ctx.cuh", "adamw.cuh", API_H],
 }
 

@@ -1,10 +1,9 @@
-// Host side of the low-rank adapters: argument checks, tiles and splits, launches.
+// Host side of the low-rank adapters: argument checks, rows by adapter, launches.
 #include <cmath>
 #include <cstddef>
 #include <new>
 
-#include "adapter.cuh"
-#include "ctx.cuh"
+#include "adapter_launch.cuh"
 
 using namespace cs;
 
@@ -13,21 +12,18 @@ static_assert(CONDENSA_ADAPTER_MAX_RANK == AD_MAX_RANK, "largest rank");
 namespace {
 
 struct Run {
-    int first, count;               // rows
+    int first, count;               // rows that follow one another
 };
 
 // The rows of a batch by adapter.
 struct Rows {
     long long total = 0, live = 0;              // rows of the batch; rows with an adapter
     std::vector<int> used;                      // adapters with rows, ascending
-    std::vector<std::vector<Run>> runs;         // of used[i]
+    std::vector<int> begin;                     // used[i]'s runs: [begin[i], end[i])
+    std::vector<int> end;
+    std::vector<int> count;                     // rows of used[i]
+    std::vector<Run> runs;
     int max_rank = 0;
-};
-
-struct Tiles {
-    std::vector<AdapterTile> tile;              // `list` into `rows`
-    std::vector<int> owner;                     // place in Rows::used
-    std::vector<int> rows;
 };
 
 int type_bytes(int dtype) { return dtype == CONDENSA_DTYPE_FP32 ? 4 : 2; }
@@ -49,8 +45,9 @@ int read_batch(condensa_ctx *ctx, const condensa_adapter_batch *b, Rows &rows)
     if (b->n_requests < 0 || (b->n_requests > 0 && (!b->request_rows || !b->request_adapter)))
         return fail(ctx, CONDENSA_ERR_INVALID_ARG, "request lists are NULL");
     if (b->k < 1 || b->n < 1) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "k and n must be positive");
-    if (b->k > 0x7FFFFFFFll || b->n > 0x7FFFFFFFll) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "k and n must be below 2^31");
-    std::vector<int> place((size_t)b->n_adapters, -1);
+    if (b->k > AD_MAX_WIDTH || b->n > AD_MAX_WIDTH) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "k and n must not exceed %d", AD_MAX_WIDTH);
+    std::vector<int> place((size_t)b->n_adapters, 0);          // requests with rows, then the place in `used`
+    int live_requests = 0;
     for (int q = 0; q < b->n_requests; ++q) {
         const long long n = b->request_rows[q];
         const int a = b->request_adapter[q];
@@ -59,185 +56,250 @@ int read_batch(condensa_ctx *ctx, const condensa_adapter_batch *b, Rows &rows)
         if (n > 0x7FFFFFFFll - rows.total) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "a batch has fewer than 2^31 rows");
         if (n > 0 && a >= 0) {
             rows.live += n;
-            place[a] = 0;
+            place[a] += 1;
+            ++live_requests;
         }
         rows.total += n;
     }
-    for (int a = 0; a < b->n_adapters; ++a) {
-        if (place[a] < 0) continue;
-        const condensa_adapter &x = b->adapters[a];
-        if (!x.a || !x.b) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "adapter %d: a or b is NULL", a);
-        place[a] = (int)rows.used.size();
-        rows.used.push_back(a);
-    }
+    if (rows.total != b->rows) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "the requests have %lld rows, the batch %lld", rows.total, (long long)b->rows);
     const int e = type_bytes(b->dtype);
+    int at = 0;
     for (int a = 0; a < b->n_adapters; ++a) {
         const condensa_adapter &x = b->adapters[a];
-        const bool grads = x.grad_a || x.grad_b;
-        if (place[a] < 0 && !grads) continue;
+        const bool live = place[a] > 0;
+        if (!live && !x.grad_a && !x.grad_b) continue;
+        if (live && (!x.a || !x.b)) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "adapter %d: a or b is NULL", a);
         if (x.rank < 1) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "adapter %d: rank must be positive", a);
         if (x.rank > AD_MAX_RANK) return fail(ctx, CONDENSA_ERR_UNSUPPORTED, "adapter %d: ranks above %d are not built", a, AD_MAX_RANK);
         if (!std::isfinite(x.scale)) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "adapter %d: scale must be finite", a);
         if ((uintptr_t)x.a % e || (uintptr_t)x.b % e || (uintptr_t)x.grad_a % 4 || (uintptr_t)x.grad_b % 4)
             return fail(ctx, CONDENSA_ERR_INVALID_ARG, "adapter %d: a pointer is not aligned to its type", a);
-        if (place[a] >= 0) rows.max_rank = std::max(rows.max_rank, (int)x.rank);
+        if (!live) continue;
+        rows.max_rank = std::max(rows.max_rank, (int)x.rank);
+        rows.begin.push_back(at);
+        at += place[a];
+        place[a] = (int)rows.used.size();
+        rows.used.push_back(a);
     }
-    rows.runs.resize(rows.used.size());
-    int at = 0;
+    rows.end = rows.begin;
+    rows.count.assign(rows.used.size(), 0);
+    rows.runs.resize((size_t)live_requests);
+    int first = 0;
     for (int q = 0; q < b->n_requests; ++q) {
         const int n = (int)b->request_rows[q], a = b->request_adapter[q];
         if (n > 0 && a >= 0) {
-            std::vector<Run> &r = rows.runs[(size_t)place[a]];
-            if (!r.empty() && r.back().first + r.back().count == at) r.back().count += n;
-            else r.push_back({at, n});
+            const int i = place[a];
+            Run *last = rows.end[i] > rows.begin[i] ? &rows.runs[rows.end[i] - 1] : nullptr;
+            if (last && last->first + last->count == first) last->count += n;
+            else rows.runs[rows.end[i]++] = {first, n};
+            rows.count[i] += n;
         }
-        at += n;
+        first += n;
     }
     return CONDENSA_OK;
 }
 
-// Cuts every adapter's rows into tiles of up to `tm`.
-void make_tiles(const Rows &rows, int tm, Tiles &t)
-{
-    std::vector<Run> part;
-    for (size_t a = 0; a < rows.used.size(); ++a) {
-        int filled = 0;
-        part.clear();
-        auto flush = [&]() {
-            if (!filled) return;
-            AdapterTile x;
-            x.first = part[0].first;
-            x.count = (u16)filled;
-            x.adapter = (u16)0;
-            x.list = -1;
-            if (part.size() > 1) {
-                x.list = (int)t.rows.size();
-                for (const Run &r : part)
-                    for (int i = 0; i < r.count; ++i) t.rows.push_back(r.first + i);
-            }
-            t.tile.push_back(x);
-            t.owner.push_back((int)a);
-            filled = 0;
-            part.clear();
-        };
-        for (const Run &r : rows.runs[a]) {
-            for (int done = 0; done < r.count;) {
-                const int n = std::min(r.count - done, tm - filled);
-                part.push_back({r.first + done, n});
-                filled += n;
-                done += n;
-                if (filled == tm) flush();
-            }
-        }
-        flush();
-    }
-}
-
-// The tiles of one launch, as they go into its parameters.
-struct TileList {
-    std::vector<AdapterTile> tiles;
-    std::vector<int> rows;
-    size_t bytes() const { return tiles.size() * sizeof(AdapterTile) + rows.size() * sizeof(int); }
-    size_t bytes_with(const AdapterTile &x) const { return bytes() + sizeof(AdapterTile) + (x.list >= 0 ? x.count * sizeof(int) : 0); }
-    void add(const Tiles &t, size_t i, int entry)
+// Entries of the adapters and their runs, as they go into the parameters of a launch.
+template <class Entry>
+struct Blob {
+    std::vector<Entry> entries;
+    std::vector<AdapterRun> runs;
+    int room() const { return (int)((AD_BLOB - (entries.size() + 1) * sizeof(Entry)) / sizeof(AdapterRun)) - (int)runs.size(); }
+    // Adds runs [from, to) of the batch for `e`.
+    void add(Entry e, const Rows &rows, int from, int to)
     {
-        AdapterTile x = t.tile[i];
-        if (x.list >= 0) {
-            const int from = x.list;
-            x.list = (int)rows.size();
-            rows.insert(rows.end(), t.rows.begin() + from, t.rows.begin() + from + x.count);
+        e.run0 = (u16)runs.size();
+        e.n_runs = (u16)(to - from);
+        e.n_rows = 0;
+        for (int r = from; r < to; ++r) {
+            runs.push_back({rows.runs[r].first, e.n_rows});
+            e.n_rows += rows.runs[r].count;
         }
-        x.adapter = (u16)entry;
-        tiles.push_back(x);
+        entries.push_back(e);
     }
-    void write(char *p) const
+    void write(u32 *blob) const
     {
-        if (!tiles.empty()) memcpy(p, tiles.data(), tiles.size() * sizeof(AdapterTile));
-        if (!rows.empty()) memcpy(p + tiles.size() * sizeof(AdapterTile), rows.data(), rows.size() * sizeof(int));
+        char *p = (char *)blob;
+        if (!entries.empty()) memcpy(p, entries.data(), entries.size() * sizeof(Entry));
+        if (!runs.empty()) memcpy(p + entries.size() * sizeof(Entry), runs.data(), runs.size() * sizeof(AdapterRun));
+    }
+    void clear()
+    {
+        entries.clear();
+        runs.clear();
     }
 };
 
-// ------------------------------------------------------------------ kernels by type, tile height, rank
-template <class T, bool TRANS, int TM, int RP>
-int launch_adapter_of(condensa_ctx *ctx, const AdapterParams &P, int cluster, int id, cudaStream_t stream)
+// ------------------------------------------------------------------ launches
+int allow_smem(condensa_ctx *ctx, const AdapterKernel &k)
 {
-    using G = AdGeom<T, TRANS, TM, RP>;
-    const void *kernel = (const void *)k_adapter<T, TRANS, TM, RP>;
-    if (!(ctx->op_smem_set >> id & 1)) {
-        CU_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
-        ctx->op_smem_set |= 1ull << id;
-    }
+    for (const void *f : ctx->op_smem_set)
+        if (f == k.f) return CONDENSA_OK;
+    CU_TRY(ctx, cudaFuncSetAttribute(k.f, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem));
+    ctx->op_smem_set.push_back(k.f);
+    return CONDENSA_OK;
+}
+
+// A launch in clusters; `pdl`: it may start while the kernel ahead of it ends.
+int launch_cluster(condensa_ctx *ctx, const AdapterKernel &k, dim3 grid, dim3 cluster, bool pdl, void *params, const char *name, cudaStream_t stream)
+{
+    const int rc = allow_smem(ctx, k);
+    if (rc) return rc;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)(P.n_tiles * cluster));
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = G::SMEM;
+    cfg.dynamicSmemBytes = (size_t)k.smem;
     cfg.stream = stream;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)cluster;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[0].val.clusterDim.x = cluster.x;
+    at[0].val.clusterDim.y = cluster.y;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
-    const int pa_ = prof_begin(ctx, TRANS ? "k_adapter_backward" : "k_adapter_forward", stream);
-    void *args[] = {(void *)&P};
-    CU_TRY(ctx, cudaLaunchKernelExC(&cfg, kernel, args));
+    cfg.numAttrs = pdl && !ctx->prof_on ? 2 : 1;
+    void *args[] = {params};
+    const int pa_ = prof_begin(ctx, name, stream);
+    CU_TRY(ctx, cudaLaunchKernelExC(&cfg, k.f, args));
     ctx->launches += 1;
     prof_end(ctx, pa_, stream);
     return CONDENSA_OK;
 }
 
-template <class T, bool TRANS, int TM>
-int launch_adapter_rank(condensa_ctx *ctx, const AdapterParams &P, int cluster, int rank, int id, cudaStream_t stream)
+// Clusters of `n` CTAs of a kernel that the device holds at once (clusters do not cross its groups of SMs).
+int resident_clusters(condensa_ctx *ctx, const AdapterKernel &k, int n, int &count)
 {
-    if (rank <= 16) return launch_adapter_of<T, TRANS, TM, 16>(ctx, P, cluster, id, stream);
-    if (rank <= 32) return launch_adapter_of<T, TRANS, TM, 32>(ctx, P, cluster, id + 1, stream);
-    if (rank <= 64) return launch_adapter_of<T, TRANS, TM, 64>(ctx, P, cluster, id + 2, stream);
-    return launch_adapter_of<T, TRANS, TM, 128>(ctx, P, cluster, id + 3, stream);
-}
-
-template <class T>
-int launch_adapter_type(condensa_ctx *ctx, const AdapterParams &P, bool trans, int tm, int cluster, int rank, int id, cudaStream_t stream)
-{
-    if (!trans) return tm == 16 ? launch_adapter_rank<T, false, 16>(ctx, P, cluster, rank, id, stream) : launch_adapter_rank<T, false, 64>(ctx, P, cluster, rank, id + 4, stream);
-    return tm == 16 ? launch_adapter_rank<T, true, 16>(ctx, P, cluster, rank, id + 8, stream) : launch_adapter_rank<T, true, 64>(ctx, P, cluster, rank, id + 12, stream);
-}
-
-int launch_adapter(condensa_ctx *ctx, const AdapterParams &P, int dtype, bool trans, int tm, int cluster, int rank, cudaStream_t stream)
-{
-    if (dtype == CONDENSA_DTYPE_BF16) return launch_adapter_type<__nv_bfloat16>(ctx, P, trans, tm, cluster, rank, 0, stream);
-    if (dtype == CONDENSA_DTYPE_FP16) return launch_adapter_type<__half>(ctx, P, trans, tm, cluster, rank, 16, stream);
-    return launch_adapter_type<float>(ctx, P, trans, tm, cluster, rank, 32, stream);
-}
-
-template <class T, int RP>
-int launch_wgrad_of(condensa_ctx *ctx, WgradParams &P, int id, cudaStream_t stream)
-{
-    using G = WgGeom<T, RP>;
-    const void *kernel = (const void *)k_adapter_wgrad<T, RP>;
-    if (!(ctx->op_smem_set >> id & 1)) {
-        CU_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM));
-        ctx->op_smem_set |= 1ull << id;
-    }
-    P.strips0 = (int)((P.side[0].width + G::WC - 1) / G::WC);
-    const int strips1 = (int)((P.side[1].width + G::WC - 1) / G::WC);
-    const int pa_ = prof_begin(ctx, "k_adapter_wgrad", stream);
-    k_adapter_wgrad<T, RP><<<dim3((unsigned)(P.strips0 + strips1), (unsigned)P.n_splits), THREADS, G::SMEM, stream>>>(P);
-    LAUNCH_CHECK(ctx);
-    prof_end(ctx, pa_, stream);
+    for (const condensa_ctx::ClusterFit &f : ctx->cluster_fit)
+        if (f.f == k.f && f.size == n) {
+            count = f.count;
+            return CONDENSA_OK;
+        }
+    const int rc = allow_smem(ctx, k);
+    if (rc) return rc;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)n);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)k.smem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)n;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    count = 0;
+    CU_TRY(ctx, cudaOccupancyMaxActiveClusters(&count, k.f, &cfg));
+    if (count < 1) return fail(ctx, CONDENSA_ERR_INTERNAL, "no cluster of %d CTAs fits the device", n);
+    ctx->cluster_fit.push_back({k.f, n, count});
     return CONDENSA_OK;
 }
 
-template <class T>
-int launch_wgrad_type(condensa_ctx *ctx, WgradParams &P, int rank, int id, cudaStream_t stream)
+// How many CTAs share a tile of the row kernel (a cluster: columns of both sides), and how many clusters share its
+// destination columns, each of them forming h again. Taken is what a simple account of the rounds makes least: a CTA's
+// time goes with its columns, those of the destination counting twice, plus some fixed work (about 600 columns' worth);
+// two CTAs on an SM take 1.2 times as long as one. Measured at 12 tiles of 1500 -> 33278 columns in fp32: cluster 8
+// alone 106 us, the choice (7, 3) 73 us; at 131 tiles of 4096 -> 4096 in bf16: cluster 4 50 us, the choice (2, 1) 45 us.
+int choose_shape(condensa_ctx *ctx, const AdapterKernel &k, long long tiles, long long ws, long long wd, int &cluster, int &splits)
 {
-    if (rank <= 16) return launch_wgrad_of<T, 16>(ctx, P, id, stream);
-    if (rank <= 32) return launch_wgrad_of<T, 32>(ctx, P, id + 1, stream);
-    if (rank <= 64) return launch_wgrad_of<T, 64>(ctx, P, id + 2, stream);
-    return launch_wgrad_of<T, 128>(ctx, P, id + 3, stream);
+    double best = 0.0;
+    for (int c = 1; c <= AD_MAX_CLUSTER; ++c) {
+        int fit = 0;
+        const int rc = resident_clusters(ctx, k, c, fit);
+        if (rc) return rc;
+        for (int s = 1; s <= (wd ? AD_MAX_CLUSTER : 1); ++s) {
+            const long long n = tiles * s, full = n / fit, rest = n % fit;
+            const double w = (double)ws / c + 2.0 * (double)wd / (c * s), crowded = 1.2 * w + 600.0;
+            double t = (double)full * crowded;
+            if (rest) t += rest * c > ctx->num_sms ? crowded : w + 600.0;
+            if ((c == 1 && s == 1) || t < 0.999 * best) {
+                best = t;
+                cluster = c;
+                splits = s;
+            }
+        }
+    }
+    return CONDENSA_OK;
 }
 
-int wgrad_strip(int dtype, int rank) { return dtype != CONDENSA_DTYPE_FP32 && rank <= 64 ? WgGeom<__half, 64>::WC : WgGeom<float, 64>::WC; }
+AdapterKernel row_kernel_of(int dtype, const RowShape &s)
+{
+    return dtype == CONDENSA_DTYPE_BF16 ? row_kernel<__nv_bfloat16>(s) : dtype == CONDENSA_DTYPE_FP16 ? row_kernel<__half>(s) : row_kernel<float>(s);
+}
+
+AdapterKernel wgrad_kernel_of(int dtype, int rank, int vec, int &strip)
+{
+    return dtype == CONDENSA_DTYPE_BF16 ? wgrad_kernel<__nv_bfloat16>(rank, vec, strip)
+         : dtype == CONDENSA_DTYPE_FP16 ? wgrad_kernel<__half>(rank, vec, strip) : wgrad_kernel<float>(rank, vec, strip);
+}
+
+// ------------------------------------------------------------------ adapters laid out anew
+constexpr size_t NONE = ~(size_t)0;
+struct Packed {
+    std::vector<size_t> a, b;           // byte offsets in the workspace, of used[i]; NONE: used as it is
+    size_t bytes = 0;
+    bool trans = false;
+};
+
+long long packed_ld(long long width, int e) { return (width * e + 15) / 16 * 16 / e; }
+
+// `vec`: access width of the row kernel. It reads rows of A by 16 bytes (8 where vec is 8), rows of B by 8.
+void plan_packing(const condensa_adapter_batch *b, const Rows &rows, bool trans, int vec, Packed &pk)
+{
+    const int e = type_bytes(b->dtype);
+    pk.trans = trans;
+    pk.a.assign(rows.used.size(), NONE);
+    pk.b.assign(rows.used.size(), NONE);
+    for (size_t i = 0; i < rows.used.size(); ++i) {
+        const condensa_adapter &x = b->adapters[rows.used[i]];
+        if (trans || widest(x.a, b->k * e) < (vec == 8 ? 8 : 16)) {
+            pk.a[i] = pk.bytes;
+            pk.bytes += align_up((size_t)((trans ? b->k * packed_ld(x.rank, e) : x.rank * packed_ld(b->k, e)) * e), 256);
+        }
+        if (trans || widest(x.b, (long long)x.rank * e) < 8) {
+            pk.b[i] = pk.bytes;
+            pk.bytes += align_up((size_t)((trans ? x.rank * packed_ld(b->n, e) : b->n * packed_ld(x.rank, e)) * e), 256);
+        }
+    }
+}
+
+int run_packing(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &rows, const Packed &pk, char *ws, cudaStream_t stream)
+{
+    const int e = type_bytes(b->dtype);
+    PackParams P;
+    P.n = 0;
+    long long blocks = 0;
+    auto flush = [&]() -> int {
+        if (!P.n) return CONDENSA_OK;
+        const int pa_ = prof_begin(ctx, "k_adapter_pack", stream);
+        if (e == 2) k_adapter_pack<u16><<<(unsigned)blocks, THREADS, 0, stream>>>(P);
+        else k_adapter_pack<u32><<<(unsigned)blocks, THREADS, 0, stream>>>(P);
+        LAUNCH_CHECK(ctx);
+        prof_end(ctx, pa_, stream);
+        P.n = 0;
+        blocks = 0;
+        return CONDENSA_OK;
+    };
+    for (size_t i = 0; i < rows.used.size(); ++i) {
+        const condensa_adapter &x = b->adapters[rows.used[i]];
+        for (int side = 0; side < 2; ++side) {
+            const size_t at = side ? pk.b[i] : pk.a[i];
+            if (at == NONE) continue;
+            const long long r = side ? b->n : x.rank, w = side ? x.rank : b->k;
+            // (a tile past the rows covers the padding of transposed rows)
+            const long long ld = packed_ld(pk.trans ? r : w, e), T = AD_PACK_TILE;
+            const long long tiles = ((pk.trans ? ld : r) + T - 1) / T * (((pk.trans ? w : ld) + T - 1) / T);
+            if (P.n == AD_PACK_MAX || (P.n && blocks + tiles > 0x7FFFFFFFll)) {
+                const int rc = flush();
+                if (rc) return rc;
+            }
+            P.item[P.n++] = {side ? x.b : x.a, ws + at, r, w, (int)ld, pk.trans ? 1 : 0, (int)blocks, 0};
+            blocks += tiles;
+        }
+    }
+    return flush();
+}
 
 // ------------------------------------------------------------------ both directions of the row kernel
 struct RowCall {
@@ -246,184 +308,157 @@ struct RowCall {
     float *h;
     long long ld_src, ld_dst, ld_h;
     bool trans;
+    int vec;                // accesses that the rows of src and dst allow: 16, 8, or 0 for less
 };
 
-int run_rows(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &rows, const RowCall &c, cudaStream_t stream)
+RowCall row_call(const void *src, void *dst, float *h, long long ld_src, long long ld_dst, long long ld_h, bool trans, int e)
+{
+    const int v = std::min(widest(src, ld_src * e), dst ? widest(dst, ld_dst * e) : 16);
+    return {src, dst, h, ld_src, ld_dst, ld_h, trans, v >= 8 ? v : 0};
+}
+
+int run_rows(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &rows, const Packed &pk, const char *pk_ws, const RowCall &c, cudaStream_t stream)
 {
     const int e = type_bytes(b->dtype);
-    const long long ws = c.trans ? b->n : b->k, wd = c.trans ? b->k : b->n;
     // tiles of 64 rows where the adapters have that many; for a few rows each, 16 waste less and spread further
     const int tm = rows.live >= 48ll * (long long)rows.used.size() ? 64 : 16;
-    Tiles t;
-    make_tiles(rows, tm, t);
-    // as many CTAs per tile as it takes to cover the SMs about twice
-    int cluster = 1;
-    while (cluster < AD_MAX_CLUSTER && (long long)t.tile.size() * cluster < 2ll * ctx->num_sms) cluster *= 2;
+    long long all = 0;
+    for (int n : rows.count) all += (n + tm - 1) / tm;
+    const AdapterKernel kernel = row_kernel_of(b->dtype, {tm, rows.max_rank, c.vec});
+    const long long ws = c.trans ? b->n : b->k, wd = c.dst ? (c.trans ? b->k : b->n) : 0;
+    int cluster = 1, splits = 1;
+    int rc = choose_shape(ctx, kernel, all, ws, wd, cluster, splits);
+    if (rc) return rc;
     AdapterParams P;
+    memset(&P, 0, offsetof(AdapterParams, blob));
     P.src = c.src; P.dst = c.dst; P.h = c.h;
     P.ld_src = c.ld_src; P.ld_dst = c.ld_dst; P.ld_h = c.ld_h;
-    P.width_src = ws; P.width_dst = wd;
+    P.width_src = ws;
+    P.width_dst = c.trans ? b->k : b->n;
     P.vec_src = widest(c.src, c.ld_src * e);
     P.vec_dst = c.dst ? widest(c.dst, c.ld_dst * e) : 16;
-    for (size_t i = 0; i < t.tile.size();) {        // as many tiles per launch as their lists fit the parameters
-        std::vector<AdapterEntry> entries;
-        TileList l;
-        for (int last = -1; i < t.tile.size(); ++i) {
-            const int a = t.owner[i];
-            if ((entries.size() + (a != last)) * sizeof(AdapterEntry) + l.bytes_with(t.tile[i]) > AD_BLOB) break;
-            if (a != last) {
-                const condensa_adapter &ad = b->adapters[rows.used[a]];
-                const uint8_t va = (uint8_t)widest(ad.a, b->k * e), vb = (uint8_t)widest(ad.b, (long long)ad.rank * e);
-                AdapterEntry en;
-                en.shrink = c.trans ? ad.b : ad.a;
-                en.expand = c.trans ? ad.a : ad.b;
-                en.scale = ad.scale;
-                en.rank = (u16)ad.rank;
-                en.vec_s = c.trans ? vb : va;
-                en.vec_e = c.trans ? va : vb;
-                entries.push_back(en);
-                last = a;
+    P.splits = splits;
+    P.scale_h = c.trans ? 1 : 0;
+    Blob<AdapterEntry> blob;
+    int tiles = 0;
+    auto flush = [&]() -> int {
+        P.n_entries = (int)blob.entries.size();
+        blob.write(P.blob);
+        rc = launch_cluster(ctx, kernel, dim3((unsigned)(tiles * cluster * P.splits)), dim3((unsigned)cluster), pk.bytes != 0, &P,
+                                      c.trans ? "k_adapter_backward" : "k_adapter_forward", stream);
+        blob.clear();
+        tiles = 0;
+        return rc;
+    };
+    for (size_t i = 0; i < rows.used.size(); ++i) {
+        const condensa_adapter &ad = b->adapters[rows.used[i]];
+        for (int run = rows.begin[i]; run < rows.end[i];) {
+            // (an adapter is cut only where its runs fill a launch's parameters by themselves)
+            if (!blob.entries.empty() && blob.room() < rows.end[i] - run && (rc = flush()) != 0) return rc;
+            const int to = std::min(rows.end[i], run + blob.room());
+            const bool pa = pk.a[i] != NONE, pb = pk.b[i] != NONE;
+            const void *am = pa ? pk_ws + pk.a[i] : (const char *)ad.a, *bm = pb ? pk_ws + pk.b[i] : (const char *)ad.b;
+            AdapterEntry en;
+            memset(&en, 0, sizeof(en));
+            if (c.trans) {
+                en.shrink = bm; en.ld_s = (int)packed_ld(b->n, e);
+                en.expand = am; en.ld_e = (int)packed_ld(ad.rank, e);
+            } else {
+                en.shrink = am; en.ld_s = (int)(pa ? packed_ld(b->k, e) : b->k);
+                en.expand = bm; en.ld_e = (int)(pb ? packed_ld(ad.rank, e) : ad.rank);
             }
-            l.add(t, i, (int)entries.size() - 1);
+            en.scale = ad.scale;
+            en.rank = (u16)ad.rank;
+            en.tile0 = tiles;
+            blob.add(en, rows, run, to);
+            tiles += (blob.entries.back().n_rows + tm - 1) / tm;
+            run = to;
         }
-        P.n_entries = (int)entries.size();
-        P.n_tiles = (int)l.tiles.size();
-        char *p = (char *)P.blob;
-        memcpy(p, entries.data(), entries.size() * sizeof(AdapterEntry));
-        l.write(p + entries.size() * sizeof(AdapterEntry));
-        const int rc = launch_adapter(ctx, P, b->dtype, c.trans, tm, cluster, rows.max_rank, stream);
-        if (rc) return rc;
     }
-    return CONDENSA_OK;
+    return blob.entries.empty() ? CONDENSA_OK : flush();
 }
 
 // ------------------------------------------------------------------ weight gradients
-struct Split {
-    int owner, tile0, n_tiles;
-};
-
 struct Wgrad {
     const void *x, *dy;
     const float *u, *h;
     long long ldx, lddy, ldu, ldh;
-    bool need_a, need_b;                // some adapter has a grad_a, a grad_b
-    int accumulate;
+    bool accumulate;
+    bool behind;                        // the row kernel goes ahead
 };
 
-// Splits of the adapters' rows, and the workspace that their sums take (floats).
-void make_splits(const condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &rows, const Tiles &t, std::vector<Split> &splits,
-                 std::vector<long long> &slot, long long &floats)
-{
-    const int wc = wgrad_strip(b->dtype, rows.max_rank);
-    const long long strips = (b->k + wc - 1) / wc + (b->n + wc - 1) / wc;
-    // CTAs for about four rounds of the SMs; a split's sums are written and read again, so none is shorter than four tiles
-    const long long want = std::max<long long>(1, 4ll * ctx->num_sms / strips);
-    const int per = (int)std::min<long long>(0x7FFF, std::max<long long>(4, ((long long)t.tile.size() + want - 1) / want));
-    std::vector<int> count(rows.used.size(), 0);
-    TileList l;
-    for (size_t i = 0; i < t.tile.size(); ++i) {
-        const bool fits = sizeof(WgEntry) + sizeof(WgSplit) + l.bytes_with(t.tile[i]) <= AD_BLOB;
-        if (splits.empty() || splits.back().owner != t.owner[i] || splits.back().n_tiles == per || !fits) {
-            splits.push_back({t.owner[i], (int)i, 0});
-            count[t.owner[i]] += 1;
-            l = TileList();
-        }
-        splits.back().n_tiles += 1;
-        l.add(t, i, 0);
-    }
-    floats = 0;
-    slot.assign(rows.used.size(), -1);
-    for (size_t a = 0; a < rows.used.size(); ++a) {
-        if (count[a] <= 1) continue;
-        slot[a] = floats;
-        floats += (long long)count[a] * b->adapters[rows.used[a]].rank * (b->k + b->n);
-    }
-}
-
-int run_wgrad(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &rows, const Tiles &t, const std::vector<Split> &splits,
-              const std::vector<long long> &slot, const Wgrad &w, float *part, cudaStream_t stream)
+int run_wgrad(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &rows, const Wgrad &w, cudaStream_t stream)
 {
     const int e = type_bytes(b->dtype);
     WgradParams P;
     memset(&P, 0, offsetof(WgradParams, blob));
     P.side[0] = {w.x, w.u, w.ldx, w.ldu, b->k, w.x ? widest(w.x, w.ldx * e) : 16, w.u ? widest(w.u, w.ldu * 4) : 16};
-    P.side[1] = {w.dy, w.h, w.lddy, w.ldh, b->n, widest(w.dy, w.lddy * e), w.h ? widest(w.h, w.ldh * 4) : 16};
-    P.part = part;
-    P.accumulate = w.accumulate;
-    std::vector<int> of_owner(rows.used.size(), 0);         // splits of an adapter so far
-    for (size_t i = 0; i < splits.size();) {
-        std::vector<WgEntry> entries;
-        std::vector<WgSplit> sp;
-        TileList l;
-        for (int last = -1; i < splits.size(); ++i) {
-            const Split &q = splits[i];
-            const condensa_adapter &ad = b->adapters[rows.used[q.owner]];
-            size_t bytes = (entries.size() + (q.owner != last)) * sizeof(WgEntry) + (sp.size() + 1) * sizeof(WgSplit);
-            TileList with = l;
-            for (int k = 0; k < q.n_tiles; ++k) with.add(t, (size_t)(q.tile0 + k), 0);
-            if (!sp.empty() && bytes + with.bytes() > AD_BLOB) break;
-            if (q.owner != last) {
-                entries.push_back({{ad.grad_a, ad.grad_b}, ad.scale, ad.rank});
-                last = q.owner;
+    P.side[1] = {w.dy, w.h, w.lddy, w.ldh, b->n, w.dy ? widest(w.dy, w.lddy * e) : 16, w.h ? widest(w.h, w.ldh * 4) : 16};
+    const int v = std::min(P.side[0].vec_act, P.side[1].vec_act), vec = v >= 8 ? v : 0;
+    Blob<WgEntry> blob;
+    int rank = 1, most_tiles = 1;
+    bool first = w.behind;
+    auto flush = [&](bool accumulate) -> int {
+        P.n_entries = (int)blob.entries.size();
+        P.accumulate = accumulate ? 1 : 0;
+        blob.write(P.blob);
+        int strip;
+        const AdapterKernel kernel = wgrad_kernel_of(b->dtype, rank, vec, strip);
+        P.strips0 = (int)((b->k + strip - 1) / strip);
+        const int strips = P.strips0 + (int)((b->n + strip - 1) / strip);
+        // CTAs that share an adapter's rows: the number whose rounds of the SMs take least, a CTA's time going with its
+        // tiles and some fixed work
+        int cluster = 1;
+        double best = 0.0;
+        for (int n = 1; n <= std::min(AD_MAX_CLUSTER, most_tiles); ++n) {
+            const long long slots = (long long)ctx->num_sms * kernel.per_sm / n;
+            const double t = (double)(((long long)strips * P.n_entries + slots - 1) / slots) * ((double)((most_tiles + n - 1) / n) + 2.0);
+            if (n == 1 || t < best) {
+                best = t;
+                cluster = n;
             }
-            WgSplit x;
-            x.slot = slot[q.owner] < 0 ? -1 : slot[q.owner] + (long long)of_owner[q.owner] * ad.rank * (b->k + b->n);
-            x.tile0 = (int)l.tiles.size();
-            x.n_tiles = (u16)q.n_tiles;
-            x.adapter = (u16)(entries.size() - 1);
-            of_owner[q.owner] += 1;
-            sp.push_back(x);
-            l = with;
         }
-        P.n_entries = (int)entries.size();
-        P.n_splits = (int)sp.size();
-        P.n_tiles = (int)l.tiles.size();
-        char *p = (char *)P.blob;
-        memcpy(p, entries.data(), entries.size() * sizeof(WgEntry)); p += entries.size() * sizeof(WgEntry);
-        memcpy(p, sp.data(), sp.size() * sizeof(WgSplit)); p += sp.size() * sizeof(WgSplit);
-        l.write(p);
-        int rc;
-        if (b->dtype == CONDENSA_DTYPE_BF16) rc = launch_wgrad_type<__nv_bfloat16>(ctx, P, rows.max_rank, 48, stream);
-        else if (b->dtype == CONDENSA_DTYPE_FP16) rc = launch_wgrad_type<__half>(ctx, P, rows.max_rank, 52, stream);
-        else rc = launch_wgrad_type<float>(ctx, P, rows.max_rank, 56, stream);
-        if (rc) return rc;
-    }
-    // gradients of several splits, and of adapters without rows (zeros, or nothing to add)
-    ReduceParams R;
-    memset(&R, 0, offsetof(ReduceParams, e));
-    R.part = part;
-    R.width[0] = b->k;
-    R.width[1] = b->n;
-    R.accumulate = w.accumulate;
-    int n = 0;
-    long long most = 0;
-    auto flush = [&]() -> int {
-        if (!n) return CONDENSA_OK;
-        const int blocks = (int)std::min<long long>((most + THREADS - 1) / THREADS, 4ll * ctx->num_sms);
-        const int pa_ = prof_begin(ctx, "k_adapter_reduce", stream);
-        k_adapter_reduce<<<dim3((unsigned)blocks, (unsigned)n), THREADS, 0, stream>>>(R);
-        LAUNCH_CHECK(ctx);
-        prof_end(ctx, pa_, stream);
-        n = 0;
-        most = 0;
-        return CONDENSA_OK;
+        const int rc = launch_cluster(ctx, kernel, dim3((unsigned)strips, (unsigned)(P.n_entries * cluster)), dim3(1, (unsigned)cluster), first, &P,
+                                      "k_adapter_wgrad", stream);
+        blob.clear();
+        rank = most_tiles = 1;
+        first = false;
+        return rc;
     };
     size_t u = 0;
     for (int a = 0; a < b->n_adapters; ++a) {
         const condensa_adapter &ad = b->adapters[a];
         const bool live = u < rows.used.size() && rows.used[u] == a;
-        const size_t owner = u;
+        const size_t i = u;
         if (live) ++u;
-        if (!ad.grad_a && !ad.grad_b) continue;
-        if (live ? slot[owner] < 0 : w.accumulate != 0) continue;
-        R.e[n++] = {{ad.grad_a, ad.grad_b}, live ? slot[owner] : 0, live ? of_owner[owner] : 0, ad.rank};
-        most = std::max(most, (long long)ad.rank * (b->k + b->n));
-        if (n == AD_RED_MAX) {
-            const int rc = flush();
-            if (rc) return rc;
-        }
+        if ((!ad.grad_a && !ad.grad_b) || (!live && w.accumulate)) continue;
+        int run = live ? rows.begin[i] : 0;
+        const int end = live ? rows.end[i] : 0;
+        bool more = false;
+        do {            // once, but where an adapter's runs fill a launch's parameters by themselves: the rest is added
+            if (!blob.entries.empty() && (more || blob.room() < end - run)) {
+                const int rc = flush(w.accumulate);
+                if (rc) return rc;
+            }
+            const int to = std::min(end, run + blob.room());
+            WgEntry en;
+            memset(&en, 0, sizeof(en));
+            en.out[0] = ad.grad_a;
+            en.out[1] = ad.grad_b;
+            en.scale = ad.scale;
+            en.rank = ad.rank;
+            blob.add(en, rows, run, to);
+            rank = std::max(rank, (int)ad.rank);
+            most_tiles = std::max(most_tiles, (blob.entries.back().n_rows + AD_WG_ROWS - 1) / AD_WG_ROWS);
+            run = to;
+            if (more || run < end) {
+                const int rc = flush(more || w.accumulate);
+                if (rc) return rc;
+                more = true;
+            }
+        } while (run < end);
     }
-    return flush();
+    return blob.entries.empty() ? CONDENSA_OK : flush(w.accumulate);
 }
 
 // ------------------------------------------------------------------ calls
@@ -466,7 +501,17 @@ int forward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, l
     if (ranges_clash(r.iv)) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "an output buffer overlaps another buffer of the call");
     if (rows.live == 0) return CONDENSA_OK;
     CU_TRY(ctx, cudaSetDevice(ctx->device));
-    return run_rows(ctx, b, rows, {x, y, h, ldx, ldy, ldh, false}, stream);
+    const RowCall call = row_call(x, y, h, ldx, ldy, ldh, false, e);
+    Packed pk;
+    plan_packing(b, rows, false, call.vec, pk);
+    char *ws = nullptr;
+    if (pk.bytes) {
+        if ((rc = op_workspace(ctx, 256 + pk.bytes, stream)) != 0) return rc;
+        ws = ctx->op_ws + 256;
+        if ((rc = run_packing(ctx, b, rows, pk, ws, stream)) != 0) return rc;
+    }
+    if ((rc = run_rows(ctx, b, rows, pk, ws, call, stream)) != 0) return rc;
+    return pk.bytes ? op_workspace_done(ctx, stream) : CONDENSA_OK;
 }
 
 int backward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, long long ldx, const void *dy, long long lddy, const float *h,
@@ -476,7 +521,7 @@ int backward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, 
     int rc = read_batch(ctx, b, rows);
     if (rc) return rc;
     const int e = type_bytes(b->dtype);
-    bool need_a = false, need_b = false, any = false;       // of adapters with rows; of any adapter
+    bool need_a = false, need_b = false;       // a grad_a, a grad_b of an adapter with rows
     for (int a : rows.used) {
         need_a = need_a || b->adapters[a].grad_a;
         need_b = need_b || b->adapters[a].grad_b;
@@ -494,30 +539,27 @@ int backward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, 
             r.add(ad.a, (long long)ad.rank * b->k * e, false);
             r.add(ad.b, (long long)ad.rank * b->n * e, false);
         }
-        any = any || ad.grad_a || ad.grad_b;
         r.add(ad.grad_a, (long long)ad.rank * b->k * 4, true);
         r.add(ad.grad_b, (long long)ad.rank * b->n * 4, true);
     }
     if (ranges_clash(r.iv)) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "an output buffer overlaps another buffer of the call");
     CU_TRY(ctx, cudaSetDevice(ctx->device));
-    if (!any) return rows.live && dx ? run_rows(ctx, b, rows, {dy, dx, nullptr, lddy, lddx, 0, true}, stream) : CONDENSA_OK;
-    Tiles t;
-    make_tiles(rows, AD_WG_ROWS, t);
-    std::vector<Split> splits;
-    std::vector<long long> slot;
-    long long floats = 0;
-    if (need_a || need_b) make_splits(ctx, b, rows, t, splits, slot, floats);
-    else slot.assign(rows.used.size(), -1);
+    const bool row_kernel = rows.live && (dx || need_a);
+    Packed pk;
+    if (row_kernel) plan_packing(b, rows, true, 16, pk);
     const long long ldu = (rows.max_rank + 3) / 4 * 4;
     const size_t u_bytes = need_a ? align_up(sizeof(float) * (size_t)(rows.total * ldu), 256) : 0;
-    rc = op_workspace(ctx, 256 + u_bytes + sizeof(float) * (size_t)floats, stream);
-    if (rc) return rc;
-    float *u_ws = need_a ? (float *)(ctx->op_ws + 256) : nullptr;
-    float *part = (float *)(ctx->op_ws + 256 + u_bytes);
-    if (rows.live && (dx || need_a) && (rc = run_rows(ctx, b, rows, {dy, dx, u_ws, lddy, lddx, ldu, true}, stream)) != 0) return rc;
-    rc = run_wgrad(ctx, b, rows, t, splits, slot, {x, dy, u_ws, h, ldx, lddy, ldu, ldh, need_a, need_b, accumulate != 0}, part, stream);
-    if (rc) return rc;
-    return op_workspace_done(ctx, stream);
+    float *u_ws = nullptr;
+    char *pk_ws = nullptr;
+    if (u_bytes + pk.bytes) {
+        if ((rc = op_workspace(ctx, 256 + u_bytes + pk.bytes, stream)) != 0) return rc;
+        u_ws = need_a ? (float *)(ctx->op_ws + 256) : nullptr;
+        pk_ws = ctx->op_ws + 256 + u_bytes;
+    }
+    if (pk.bytes && (rc = run_packing(ctx, b, rows, pk, pk_ws, stream)) != 0) return rc;
+    if (row_kernel && (rc = run_rows(ctx, b, rows, pk, pk_ws, row_call(dy, dx, u_ws, lddy, lddx, ldu, true, e), stream)) != 0) return rc;
+    if ((rc = run_wgrad(ctx, b, rows, {x, dy, u_ws, h, ldx, lddy, ldu, ldh, accumulate != 0, row_kernel}, stream)) != 0) return rc;
+    return u_bytes + pk.bytes ? op_workspace_done(ctx, stream) : CONDENSA_OK;
 }
 
 }  // namespace

@@ -8,13 +8,16 @@
 // k_adapter does both in one launch. A tile is up to TM rows of one adapter, from one request or from
 // several; a thread-block cluster works on it. Each CTA of the cluster contracts its part of the source
 // columns, the CTAs add their partial h over distributed shared memory, and each then expands its part
-// of the destination columns, whose old values were already on their way. src is read once, dst once
+// of the destination columns, whose first values are already on their way. src is read once, dst once
 // and written once, h never makes a trip through global memory in between.
 //
 // The arithmetic is small (2 * rank operations per source and destination element), so the
-// kernels are bound by memory up to ranks of 64 or so; the products run on the warp-level matrix instruction
-// (operands from shared memory into registers), whose rate is far above what the memory can feed.
-// tcgen05 would want 128-row accumulators in tensor memory for an 8- to 64-wide product.
+// kernels are bound by memory up to ranks of 64 or so; the row kernel's products run on the warp-level matrix
+// instruction, whose operands are loaded from global memory straight into the registers that it wants them in: the
+// order of the terms of a sum is free, so each lane takes 16 neighbouring bytes of a row for two steps of the
+// product, of src and of the matrix alike. No shared memory and no barrier stand in its two loops. (Staged through a
+// ring in shared memory, the same products were 1.3 to 2 times slower: two barriers' worth of latency per chunk, and
+// most instructions spent on copies.)
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -28,24 +31,25 @@ typedef unsigned short u16;
 constexpr int AD_BLOB = 3840;                // bytes of lists in the kernel parameters
 constexpr int AD_MAX_RANK = 128;
 constexpr int AD_MAX_CLUSTER = 8;
+constexpr int AD_MAX_WIDTH = 1 << 22;        // of x and y: places in A are 32-bit offsets (2^22 * 128 ranks * 4 bytes = 2^31)
 constexpr int AD_WG_ROWS = 64;               // rows of a tile of the weight gradients
+
+struct AdapterRun {                          // rows of an adapter that follow one another
+    int first;                               // the first of them
+    int before;                              // the adapter's rows ahead of it
+};
 
 struct AdapterEntry {                        // an adapter as k_adapter sees it
     const void *shrink;
     const void *expand;
     float scale;
-    u16 rank;
-    uint8_t vec_s, vec_e;                    // widest access both allow (bytes)
+    int n_rows;
+    int tile0;                               // its first tile
+    u16 run0, n_runs;                        // its rows
+    u16 rank, pad;
+    int ld_s, ld_e;                          // row strides: shrink [rank][source columns], expand [destination columns][rank]
 };
-static_assert(sizeof(AdapterEntry) == 24, "packed into the parameters");
-
-struct AdapterTile {
-    int first;                               // first row, where the rows follow one another
-    int list;                                // else: place of their numbers in the row list; -1
-    u16 count;
-    u16 adapter;                             // place in the parameters
-};
-static_assert(sizeof(AdapterTile) == 12, "packed into the parameters");
+static_assert(sizeof(AdapterEntry) == 48, "packed into the parameters");
 
 struct AdapterParams {
     const void *src;
@@ -54,18 +58,32 @@ struct AdapterParams {
     long long ld_src, ld_dst, ld_h;
     long long width_src, width_dst;
     int vec_src, vec_dst;
-    int n_entries, n_tiles;
-    u32 blob[AD_BLOB / 4];                   // entries, tiles, rows
+    int n_entries;
+    int splits;                              // clusters that share a tile's destination columns (each forms all of h)
+    int scale_h;                             // 1 (backward): h is scale * S src, and the expansion takes no factor
+    int pad;
+    u32 blob[AD_BLOB / 4];                   // entries, runs
 };
 static_assert(sizeof(AdapterParams) <= 4096, "kernel parameters");
 
+// Row i of an adapter with these runs.
+__device__ __forceinline__ int adapter_row(const AdapterRun *runs, int n, int i)
+{
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (runs[mid].before <= i) lo = mid; else hi = mid - 1;
+    }
+    return runs[lo].first + (i - runs[lo].before);
+}
+
 // ------------------------------------------------------------------ types
 template <class T> struct AdType {           // 16-bit types
-    static constexpr int E = 2, KSTEP = 16, NT = 4;      // bytes; depth of a product step; 8-column tiles of a warp
+    static constexpr int E = 2, KSTEP = 16;              // bytes; depth of a product step
     static constexpr int PARTS = 2;                      // 16-bit parts of an fp32 operand of the expansion
 };
 template <> struct AdType<float> {
-    static constexpr int E = 4, KSTEP = 8, NT = 2;
+    static constexpr int E = 4, KSTEP = 8;
     static constexpr int PARTS = 1;
 };
 
@@ -90,32 +108,30 @@ __device__ __forceinline__ void st_shared16(u32 dst, uint4 v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(dst), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ void st_shared2(u32 dst, u16 v) { asm volatile("st.shared.u16 [%0], %1;" :: "r"(dst), "h"(v) : "memory"); }
 
-// 16 bytes of a row into shared memory, the first `left` of them exist (the rest become zero). `vec`: the
-// accesses that the row's alignment allows. `any` is some address that may be formed when nothing exists.
-__device__ __forceinline__ void copy_unit(u32 dst, const char *src, const char *any, int left, int vec)
+// 16 bytes of a row into shared memory, the first `n` (0 to 16) of them exist (the rest become zero). V: the
+// accesses that every row allows, 16 or 8 bytes; 0: `vec` says it. `any`: an address that may be formed where
+// nothing exists.
+template <int V>
+__device__ __forceinline__ void copy_unit(u32 dst, const char *src, const char *any, int n, int vec)
 {
-    left = min(max(left, 0), 16);
-    if (vec >= 16) {
-        cp16(dst, left ? src : any, left);
-    } else if (vec == 8) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int n = min(max(left - 8 * i, 0), 8);
-            cp8(dst + 8 * i, n ? src + 8 * i : any, n);
-        }
+    if (V == 16) {
+        cp16(dst, n ? src : any, n);
+    } else if (V == 8 || vec >= 8) {
+        const int m = max(n - 8, 0);
+        cp8(dst, n ? src : any, min(n, 8));
+        cp8(dst + 8, m ? src + 8 : any, m);
     } else if (vec == 4) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int n = min(max(left - 4 * i, 0), 4);
-            cp4(dst + 4 * i, n ? src + 4 * i : any, n);
+            const int m = min(max(n - 4 * i, 0), 4);
+            cp4(dst + 4 * i, m ? src + 4 * i : any, m);
         }
     } else {
         u32 w[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (left > 2 * i) w[i >> 1] |= (u32) * reinterpret_cast<const u16 *>(src + 2 * i) << (16 * (i & 1));
+            if (n > 2 * i) w[i >> 1] |= (u32) * reinterpret_cast<const u16 *>(src + 2 * i) << (16 * (i & 1));
         st_shared16(dst, make_uint4(w[0], w[1], w[2], w[3]));
     }
 }
@@ -134,25 +150,17 @@ __device__ __forceinline__ float lds_f32(u32 addr)
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
-__device__ __forceinline__ u32 to_tf32(float x)
-{
-    u32 r;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-    return r;
-}
-
 // Operand fragments of one product step (16 x KSTEP times KSTEP x 8).
 template <class T> struct FragA { u32 r[4]; };
 template <class T> struct FragB { u32 r[2]; };
 template <> struct FragA<float> { u32 hi[4], lo[4]; };       // two TF32 parts: 22 bits of the operand
 template <> struct FragB<float> { u32 hi[2], lo[2]; };
 
+// (the instruction reads the upper 19 bits of an operand: the second part needs no rounding of its own)
 __device__ __forceinline__ void split_tf32(float x, u32 &hi, u32 &lo)
 {
-    hi = to_tf32(x);
-    const float rest = x - __uint_as_float(hi);
-    // an operand that is not finite has no rest
-    lo = (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u ? 0u : to_tf32(rest);
+    hi = __float_as_uint(x) & 0xFFFFE000u;
+    lo = __float_as_uint(x - __uint_as_float(hi));
 }
 
 __device__ __forceinline__ void mma_step(float (&c)[4], const FragA<__nv_bfloat16> &a, const FragB<__nv_bfloat16> &b)
@@ -165,6 +173,17 @@ __device__ __forceinline__ void mma_step(float (&c)[4], const FragA<__half> &a, 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]));
 }
+// The same on a sum that starts at zero.
+__device__ __forceinline__ void mma_first(float (&c)[4], const FragA<__nv_bfloat16> &a, const FragB<__nv_bfloat16> &b)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]), "f"(0.0f));
+}
+__device__ __forceinline__ void mma_first(float (&c)[4], const FragA<__half> &a, const FragB<__half> &b)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]), "f"(0.0f));
+}
 __device__ __forceinline__ void mma_tf32(float (&c)[4], const u32 (&a)[4], const u32 (&b)[2])
 {
     asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -176,21 +195,12 @@ __device__ __forceinline__ void mma_step(float (&c)[4], const FragA<float> &a, c
     mma_tf32(c, a.hi, b.lo);
     mma_tf32(c, a.hi, b.hi);
 }
+__device__ __forceinline__ void mma_first(float (&c)[4], const FragA<float> &a, const FragB<float> &b)
+{
+    c[0] = c[1] = c[2] = c[3] = 0.0f;
+    mma_step(c, a, b);
+}
 
-// A operand from [m][k] at `base` (rows of `stride` bytes).
-template <class T>
-__device__ __forceinline__ void load_a(FragA<T> &f, u32 base, int stride, int lane)
-{
-    ldsm4(f.r, base + (lane & 15) * stride + (lane >> 4) * 16);
-}
-__device__ __forceinline__ void load_a(FragA<float> &f, u32 base, int stride, int lane)
-{
-    const u32 p = base + (lane >> 2) * stride + (lane & 3) * 4;
-    split_tf32(lds_f32(p), f.hi[0], f.lo[0]);
-    split_tf32(lds_f32(p + 8 * stride), f.hi[1], f.lo[1]);
-    split_tf32(lds_f32(p + 16), f.hi[2], f.lo[2]);
-    split_tf32(lds_f32(p + 8 * stride + 16), f.hi[3], f.lo[3]);
-}
 // A operand from [k][m] (its transpose lies in memory).
 template <class T>
 __device__ __forceinline__ void load_a_t(FragA<T> &f, u32 base, int stride, int lane)
@@ -206,25 +216,7 @@ __device__ __forceinline__ void load_a_t(FragA<float> &f, u32 base, int stride, 
     split_tf32(lds_f32(p + 4 * stride), f.hi[2], f.lo[2]);
     split_tf32(lds_f32(p + 4 * stride + 32), f.hi[3], f.lo[3]);
 }
-// B operands of two neighbouring 8-column tiles from [n][k].
-template <class T>
-__device__ __forceinline__ void load_b2(FragB<T> (&f)[2], u32 base, int stride, int lane)
-{
-    u32 r[4];
-    const int q = lane >> 3;
-    ldsm4(r, base + ((q >> 1) * 8 + (lane & 7)) * stride + (q & 1) * 16);
-    f[0].r[0] = r[0]; f[0].r[1] = r[1]; f[1].r[0] = r[2]; f[1].r[1] = r[3];
-}
-__device__ __forceinline__ void load_b2(FragB<float> (&f)[2], u32 base, int stride, int lane)
-{
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const u32 p = base + (i * 8 + (lane >> 2)) * stride + (lane & 3) * 4;
-        split_tf32(lds_f32(p), f[i].hi[0], f[i].lo[0]);
-        split_tf32(lds_f32(p + 16), f[i].hi[1], f[i].lo[1]);
-    }
-}
-// ... and from [k][n].
+// B operands of two neighbouring 8-column tiles from [k][n].
 template <class T>
 __device__ __forceinline__ void load_b2_t(FragB<T> (&f)[2], u32 base, int stride, int lane)
 {
@@ -279,198 +271,385 @@ __device__ __forceinline__ float4 ld_cluster(u32 addr, u32 rank)
     return v;
 }
 
-// ------------------------------------------------------------------ geometry
-// TM rows of a tile: TM / 16 groups of rows, 8 / (TM / 16) warps side by side in each.
-template <class T, bool TRANS, int TM, int RP>
-struct AdGeom {
-    static constexpr int E = AdType<T>::E, NT = AdType<T>::NT;
-    static constexpr int RG = TM / 16, KW = WARPS / RG;
-    static constexpr int KC = 256 / E;                               // source columns of a chunk
-    static constexpr int NWC = 8 * NT;                               // destination columns of a warp
-    static constexpr int NC = NWC * KW;                              // ... of a chunk
-    static constexpr int X_STRIDE = 256 + 16;                        // row strides in shared memory: eight rows at a
-    static constexpr int S_STRIDE = TRANS ? RP * E + 16 : 256 + 16;  // 16-byte step meet all banks
-    static constexpr int S_ROWS = TRANS ? KC : RP;
-    static constexpr int Y_STRIDE = NC * E + 64;                     // two rows of four 16-byte accesses meet all banks
-    static constexpr int E_STRIDE = TRANS ? NC * E + 16 : RP * E + 16;
-    static constexpr int E_ROWS = TRANS ? RP : NC;
-    static constexpr int STAGE1 = TM * X_STRIDE + S_ROWS * S_STRIDE;
-    static constexpr int STAGE2 = TM * Y_STRIDE + E_ROWS * E_STRIDE;
-    static constexpr int STAGE = STAGE1 > STAGE2 ? STAGE1 : STAGE2;
-    static constexpr int HP_STRIDE = RP + 4;                         // floats
-    static constexpr int HP = (KW > 1 ? KW / 2 : 1) * TM * HP_STRIDE * 4;    // partial sums
-    static constexpr int HO_STRIDE = E == 2 ? RP * 2 + 16 : RP * 4 + 16;     // operand of the expansion, bytes
-    static constexpr int HO = TM * HO_STRIDE * AdType<T>::PARTS;
-    static constexpr int FIXED = HP + HO + TM * 8;
-    static constexpr int HALF_SM = 113 * 1024, WHOLE_SM = 227 * 1024;
-    static constexpr int stages()
-    {
-        for (int s = 4; s >= 2; --s)
-            if (FIXED + s * STAGE <= HALF_SM) return s;
-        return FIXED + 3 * STAGE <= WHOLE_SM ? 3 : 2;
-    }
-    static constexpr int STAGES = stages();
-    static constexpr int SMEM = FIXED + STAGES * STAGE;
-    static_assert(SMEM <= WHOLE_SM, "shared memory");
-    static_assert(STAGE % 16 == 0 && HP % 16 == 0 && HO % 16 == 0, "alignment");
-};
-
-// Where column c of a warp's NWC destination columns is put, so that a thread's accumulators
-// (columns 2t, 2t+1 of every 8-column tile) are 2 * NT neighbouring columns of the destination.
-template <int NT>
-__device__ __forceinline__ int place_of(int c)
+// ------------------------------------------------------------------ fragments straight from rows
+// Step s (0 or 1) of a block of 4 * (16 / E) columns: lane t of a quad holds 16 bytes of each row, words 2s and 2s + 1 of
+// them are its share of the step's depth. In both operands alike, so the permutation of the depth drops out.
+template <class T>
+__device__ __forceinline__ void frag_a(FragA<T> &f, const uint4 &up, const uint4 &low, int s)
 {
-    const int l = c % (8 * NT), t = l / (2 * NT), j = (l % (2 * NT)) >> 1;
-    return c - l + j * 8 + 2 * t + (c & 1);
+    f.r[0] = s ? up.z : up.x; f.r[1] = s ? low.z : low.x;
+    f.r[2] = s ? up.w : up.y; f.r[3] = s ? low.w : low.y;
+}
+__device__ __forceinline__ void frag_a(FragA<float> &f, const uint4 &up, const uint4 &low, int s)
+{
+    split_tf32(__uint_as_float(s ? up.z : up.x), f.hi[0], f.lo[0]);
+    split_tf32(__uint_as_float(s ? low.z : low.x), f.hi[1], f.lo[1]);
+    split_tf32(__uint_as_float(s ? up.w : up.y), f.hi[2], f.lo[2]);
+    split_tf32(__uint_as_float(s ? low.w : low.y), f.hi[3], f.lo[3]);
+}
+template <class T>
+__device__ __forceinline__ void frag_b(FragB<T> &f, u32 w0, u32 w1)
+{
+    f.r[0] = w0; f.r[1] = w1;
+}
+__device__ __forceinline__ void frag_b(FragB<float> &f, u32 w0, u32 w1)
+{
+    split_tf32(__uint_as_float(w0), f.hi[0], f.lo[0]);
+    split_tf32(__uint_as_float(w1), f.hi[1], f.lo[1]);
+}
+template <class T>
+__device__ __forceinline__ void frag_h(FragA<T> &f, uint2 up, uint2 low)
+{
+    f.r[0] = up.x; f.r[1] = low.x; f.r[2] = up.y; f.r[3] = low.y;
+}
+__device__ __forceinline__ void frag_h(FragA<float> &f, uint2 up, uint2 low)
+{
+    split_tf32(__uint_as_float(up.x), f.hi[0], f.lo[0]);
+    split_tf32(__uint_as_float(low.x), f.hi[1], f.lo[1]);
+    split_tf32(__uint_as_float(up.y), f.hi[2], f.lo[2]);
+    split_tf32(__uint_as_float(low.y), f.hi[3], f.lo[3]);
 }
 
-template <class T, bool TRANS, int TM, int RP>
-__global__ void __launch_bounds__(THREADS) k_adapter(const __grid_constant__ AdapterParams P)
+// 16 bytes of a row. V: the access that every row allows, 16 or 8 bytes; 0: value by value. STREAM: read once,
+// not worth a place in the L1 cache, where A and B are shared by the warps.
+template <int V, int E, bool STREAM>
+__device__ __forceinline__ uint4 load_unit(const char *p)
 {
-    using G = AdGeom<T, TRANS, TM, RP>;
-    constexpr int E = G::E, NT = G::NT, KSTEP = AdType<T>::KSTEP, PARTS = AdType<T>::PARTS;
+    uint4 r;
+    if (V == 16) {
+        if (STREAM) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+        else r = *reinterpret_cast<const uint4 *>(p);
+    } else if (V == 8) {
+        const uint2 a = reinterpret_cast<const uint2 *>(p)[0], b = reinterpret_cast<const uint2 *>(p)[1];
+        r = make_uint4(a.x, a.y, b.x, b.y);
+    } else if (E == 4) {
+        const u32 *q = reinterpret_cast<const u32 *>(p);
+        r = make_uint4(q[0], q[1], q[2], q[3]);
+    } else {
+        const u16 *q = reinterpret_cast<const u16 *>(p);
+        r = make_uint4(q[0] | (u32)q[1] << 16, q[2] | (u32)q[3] << 16, q[4] | (u32)q[5] << 16, q[6] | (u32)q[7] << 16);
+    }
+    return r;
+}
+// The first n values of it; the others are zero.
+template <int E>
+__device__ __noinline__ uint4 load_some(const char *p, int n)
+{
+    u32 w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16 / E; ++i)
+        if (i < n) {
+            if (E == 4) w[i] = reinterpret_cast<const u32 *>(p)[i];
+            else w[i >> 1] |= (u32)reinterpret_cast<const u16 *>(p)[i] << (16 * (i & 1));
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Sixteen bytes of destination values plus factor times a lane's accumulators, rounded once.
+__device__ __forceinline__ void unpack2(u32 w, float &lo, float &hi, __nv_bfloat16)
+{
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xFFFF0000u);
+}
+__device__ __forceinline__ void unpack2(u32 w, float &lo, float &hi, __half)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    lo = f.x;
+    hi = f.y;
+}
+__device__ __forceinline__ u32 pack2(float lo, float hi, __nv_bfloat16)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const u32 *>(&v);
+}
+__device__ __forceinline__ u32 pack2(float lo, float hi, __half)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const u32 *>(&v);
+}
+template <class T, int NT>
+__device__ __forceinline__ uint4 add_unit(const uint4 &old, const float (&d)[NT][4], int half, float factor)
+{
+    const u32 o[4] = {old.x, old.y, old.z, old.w};
+    u32 w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 2) {
+            float lo, hi;
+            unpack2(o[j], lo, hi, T());
+            w[j] = pack2(fmaf(factor, d[j][2 * half], lo), fmaf(factor, d[j][2 * half + 1], hi), T());
+        } else {
+            w[j] = __float_as_uint(fmaf(factor, d[j >> 1][2 * half + (j & 1)], __uint_as_float(o[j])));
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int V, int E>
+__device__ __forceinline__ void store_unit(char *p, const uint4 &v, int n)
+{
+    if (V == 16 && n == 16 / E) *reinterpret_cast<uint4 *>(p) = v;
+    else if (V == 8 && n == 16 / E) {
+        reinterpret_cast<uint2 *>(p)[0] = make_uint2(v.x, v.y);
+        reinterpret_cast<uint2 *>(p)[1] = make_uint2(v.z, v.w);
+    } else {
+        const u32 w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 16 / E; ++e)
+            if (e < n) {
+                if (E == 4) reinterpret_cast<u32 *>(p)[e] = w[e];
+                else reinterpret_cast<u16 *>(p)[e] = (u16)(w[e >> 1] >> (16 * (e & 1)));
+            }
+    }
+}
+
+// ------------------------------------------------------------------ geometry
+// A warp takes 16 rows; the RG warps above one another cover the tile, the KW side by side share its columns.
+template <class T, int TM, int RP>
+struct AdGeom {
+    static constexpr int E = AdType<T>::E, U = 16 / E;               // bytes of a value; values of a lane's unit
+    static constexpr int RG = TM / 16, KW = WARPS / RG;
+    static constexpr int KB = 4 * U, NT = U / 2;                     // columns of a block; 8-column product tiles of one
+    static constexpr int NB = RP <= 16 ? 2 : 1;                      // source blocks of a step of the first loop
+    static constexpr bool AHEAD = RP <= 32;                          // A and B, too, are loaded a step ahead; else half a step
+    static constexpr int HP_STRIDE = RP + 4;                         // floats
+    static constexpr int HP = (KW > 1 ? KW / 2 : 1) * TM * HP_STRIDE * 4;    // partial sums
+    static constexpr int HO_STRIDE = RP * E + (RP * E == 32 ? 0 : 32);       // operand of the expansion: four rows meet all banks
+    static constexpr int HO = TM * HO_STRIDE * AdType<T>::PARTS;
+    static constexpr int SMEM = HP + HO + TM * 8;
+    static constexpr int CTAS = RP <= 64 ? 2 : 1;                    // resident on an SM, at least
+    static_assert(HP % 16 == 0 && HO % 16 == 0 && SMEM <= 227 * 1024, "shared memory");
+};
+
+template <class T, int TM, int RP, int V>
+__global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(const __grid_constant__ AdapterParams P)
+{
+    using G = AdGeom<T, TM, RP>;
+    constexpr int E = G::E, U = G::U, NT = G::NT, NB = G::NB, KB = G::KB, KW = G::KW, KSTEP = AdType<T>::KSTEP, PARTS = AdType<T>::PARTS;
+    constexpr int WV = V == 8 ? 8 : 16;                              // access to A (laid out anew where it allows less)
+    constexpr int JT = RP / 8, ST = RP / KSTEP;                      // tiles and steps of the rank
+    constexpr int BLOCK = KB * E;                                    // bytes of a block: 64
     extern __shared__ __align__(128) char sm[];
     float *hp = reinterpret_cast<float *>(sm);
     char *ho = sm + G::HP;
     int *srow = reinterpret_cast<int *>(ho + G::HO);
     float *sfac = reinterpret_cast<float *>(srow + TM);
-    const u32 ring = smem_u32(sm + G::FIXED);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rg = warp / G::KW, kw = warp % G::KW;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+    const int rg = warp / KW, kw = warp % KW;
     const int C = (int)cluster_size(), c_rank = (int)cluster_rank();
 
     const AdapterEntry *entries = reinterpret_cast<const AdapterEntry *>(P.blob);
-    const AdapterTile *tiles = reinterpret_cast<const AdapterTile *>(P.blob + P.n_entries * (sizeof(AdapterEntry) / 4));
-    const int *row_list = reinterpret_cast<const int *>(tiles + P.n_tiles);
-    const AdapterTile tile = tiles[blockIdx.x / C];
-    const AdapterEntry ent = entries[tile.adapter];
-    const int count = tile.count, rank = ent.rank, r16 = (rank + 15) & ~15;
-    if (tid < TM) srow[tid] = tid < count ? (tile.list < 0 ? tile.first + tid : row_list[tile.list + tid]) : 0;
+    const AdapterRun *runs = reinterpret_cast<const AdapterRun *>(entries + P.n_entries);
+    const int tile = (int)blockIdx.x / (C * P.splits), split = (int)blockIdx.x / C % P.splits;
+    int which = 0;
+    for (int hi = P.n_entries - 1; which < hi;) {
+        const int mid = (which + hi + 1) >> 1;
+        if (entries[mid].tile0 <= tile) which = mid; else hi = mid - 1;
+    }
+    const AdapterEntry &ent = entries[which];
+    const int row0 = (tile - ent.tile0) * TM, count = min(TM, ent.n_rows - row0), rank = ent.rank, r16 = (rank + 15) & ~15;
+    // (places without a row take the tile's first: what they yield is dropped)
+    if (tid < TM) srow[tid] = adapter_row(runs + ent.run0, ent.n_runs, row0 + (tid < count ? tid : 0));
     __syncthreads();
 
-    const int KT = (int)((P.width_src + G::KC - 1) / G::KC), NTt = P.dst ? (int)((P.width_dst + G::NC - 1) / G::NC) : 0;
-    const int kc0 = (int)((long long)c_rank * KT / C), nk = (int)((long long)(c_rank + 1) * KT / C) - kc0;
-    const int nc0 = (int)((long long)c_rank * NTt / C), nn = (int)((long long)(c_rank + 1) * NTt / C) - nc0;
-    const char *src = (const char *)P.src, *shrink = (const char *)ent.shrink, *expand = (const char *)ent.expand;
-
-    // chunk i of this CTA's work (source columns first, then destination columns) into a stage of the ring
-    auto issue = [&](int i) {
-        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE;
-        if (i < nk) {
-            const long long col = (long long)(kc0 + i) * G::KC;
-            const int left = (int)min((long long)256, (P.width_src - col) * E);       // bytes of the chunk that exist
-            for (int u = tid; u < count * 16; u += THREADS) {
-                const int r = u >> 4, q = (u & 15) * 16;
-                copy_unit(st + r * G::X_STRIDE + q, src + ((long long)srow[r] * P.ld_src + col) * E + q, src, left - q, P.vec_src);
-            }
-            const u32 ss = st + TM * G::X_STRIDE;
-            if (!TRANS) {
-                for (int u = tid; u < rank * 16; u += THREADS) {
-                    const int r = u >> 4, q = (u & 15) * 16;
-                    copy_unit(ss + r * G::S_STRIDE + q, shrink + ((long long)r * P.width_src + col) * E + q, shrink, left - q, ent.vec_s);
-                }
-            } else {
-                const int upr = r16 * E / 16;
-                for (int u = tid; u < G::KC * upr; u += THREADS) {
-                    const int r = u / upr, q = (u % upr) * 16;
-                    const bool there = col + r < P.width_src;
-                    copy_unit(ss + r * G::S_STRIDE + q, shrink + (col + r) * rank * E + q, shrink, there ? rank * E - q : 0, ent.vec_s);
-                }
-            }
-        } else if (i < nk + nn) {
-            const long long col = (long long)(nc0 + i - nk) * G::NC;
-            const int wide = (int)min((long long)G::NC, P.width_dst - col);            // columns of the chunk that exist
-            constexpr int YU = G::NC * E / 16;
-            const char *dst = (const char *)P.dst;
-            for (int u = tid; u < count * YU; u += THREADS) {
-                const int r = u / YU, q = (u % YU) * 16;
-                copy_unit(st + r * G::Y_STRIDE + q, dst + ((long long)srow[r] * P.ld_dst + col) * E + q, dst, wide * E - q, P.vec_dst);
-            }
-            const u32 se = st + TM * G::Y_STRIDE;
-            if (!TRANS) {
-                const int upr = r16 * E / 16;
-                for (int u = tid; u < wide * upr; u += THREADS) {
-                    const int c = u / upr, q = (u % upr) * 16;
-                    copy_unit(se + place_of<NT>(c) * G::E_STRIDE + q, expand + (col + c) * rank * E + q, expand, rank * E - q, ent.vec_e);
-                }
-            } else {
-                // a 16-byte unit is one thread's columns: its pairs go to NT tiles
-                for (int u = tid; u < r16 * YU; u += THREADS) {
-                    const int r = u / YU, c = (u % YU) * (16 / E);
-                    const char *s = expand + ((long long)r * P.width_dst + col + c) * E;
-                    const u32 d = se + r * G::E_STRIDE + place_of<NT>(c) * E;
-                    const int left = r < rank ? (wide - c) * E : 0;
+    const int ws = (int)P.width_src, wd = (int)P.width_dst;          // (below 2^31)
+    const int KBT = (ws + KB - 1) / KB, NBT = P.dst ? (wd + KB - 1) / KB : 0;
+    // this warp's source blocks, and its destination blocks (kw, kw + KW, ... of the CTA's)
+    const int kparts = C * KW, kpart = c_rank * KW + kw;
+    const int kb0 = (int)((long long)kpart * KBT / kparts), kb1 = (int)((long long)(kpart + 1) * KBT / kparts);
+    const int part = split * C + c_rank, parts = C * P.splits;
+    const int nb0 = (int)((long long)part * NBT / parts) + kw, nb1 = (int)((long long)(part + 1) * NBT / parts);
+    const char *px[2];
+    char *py[2];
+    bool live[2];
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        const int n = min(max(left - 2 * E * j, 0), 2 * E);
-                        if (E == 2) {
-                            if (ent.vec_e >= 4) cp4(d + j * 16, n ? s + 4 * j : expand, n);
-                            else
-                                for (int e = 0; e < 2; ++e) st_shared2(d + j * 16 + 2 * e, n > 2 * e ? *reinterpret_cast<const u16 *>(s + 4 * j + 2 * e) : (u16)0);
-                        } else {
-                            if (ent.vec_e >= 8) cp8(d + j * 32, n ? s + 8 * j : expand, n);
-                            else
-                                for (int e = 0; e < 2; ++e) cp4(d + j * 32 + 4 * e, n > 4 * e ? s + 8 * j + 4 * e : expand, n > 4 * e ? 4 : 0);
-                        }
-                    }
+    for (int h = 0; h < 2; ++h) {
+        const long long row = srow[rg * 16 + g + 8 * h];
+        px[h] = (const char *)P.src + (row * P.ld_src + t4 * U) * E + (long long)kb0 * BLOCK;
+        py[h] = (char *)P.dst + (row * P.ld_dst + t4 * U) * E + (long long)nb0 * BLOCK;
+        live[h] = rg * 16 + g + 8 * h < count;
+    }
+
+    // ---- shrink: this warp's share of h. The blocks that exist as a whole go through two sets of registers in turn
+    float acc[JT][4];
+#pragma unroll
+    for (int j = 0; j < JT; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[j][q] = 0.0f;
+    struct SrcX { uint4 x[NB][2]; };
+    constexpr int JH = G::AHEAD ? JT : JT / 2;              // tiles of the rank that are loaded at a time
+    struct SrcW { uint4 w[NB][JH]; };
+    // rows of S past the rank are read as its last one: what they yield is dropped
+    const char *pw = (const char *)ent.shrink + (long long)kb0 * BLOCK + t4 * 16;
+    u32 w_off[JT];
+#pragma unroll
+    for (int j = 0; j < JT; ++j) w_off[j] = (u32)min(8 * j + g, rank - 1) * (u32)(ent.ld_s * E);
+    auto load_x = [&](SrcX &s) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s.x[b][h] = load_unit<V, E, true>(px[h] + b * BLOCK);
+            px[h] += NB * BLOCK;
+        }
+    };
+    auto load_w = [&](SrcW &s, int j0) {
+#pragma unroll
+        for (int j = 0; j < JH; ++j) {
+            if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s.w[b][j] = load_unit<WV, E, false>(pw + w_off[j0 + j] + b * BLOCK);
+        }
+        if (j0 + JH == JT) pw += NB * BLOCK;
+    };
+    auto multiply = [&](const SrcX &x, const SrcW &w, int blocks, int j0) {
+        // the matrix instruction truncates its sums: at low ranks (whose registers suffice) a few steps' are kept
+        // apart and added with rounding
+        constexpr bool APART = RP <= 32;
+        float d[APART ? JT : 1][4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            if (b >= blocks) break;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                FragA<T> a;
+                frag_a(a, x.x[b][0], x.x[b][1], t);
+#pragma unroll
+                for (int j = 0; j < JH; ++j) {
+                    if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
+                    FragB<T> f;
+                    frag_b(f, t ? w.w[b][j].z : w.w[b][j].x, t ? w.w[b][j].w : w.w[b][j].y);
+                    if constexpr (!APART) mma_step(acc[j0 + j], a, f);
+                    else if (b == 0 && t == 0) mma_first(d[j], a, f);
+                    else mma_step(d[j], a, f);
                 }
+            }
+        }
+        if constexpr (APART) {
+#pragma unroll
+            for (int j = 0; j < JT; ++j) {
+                if (j >= 2 && j * 8 >= r16) break;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[j][q] += d[j][q];
             }
         }
     };
-
-    const int total = nk + nn;
-#pragma unroll
-    for (int i = 0; i < G::STAGES - 1; ++i) {
-        issue(i);
-        cp_commit();
-    }
-    // ---- shrink: this CTA's partial h
-    float acc[RP / 8][4];
-#pragma unroll
-    for (int j = 0; j < RP / 8; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) acc[j][q] = 0.0f;
-    int i = 0;
-    for (; i < nk; ++i) {
-        cp_wait<G::STAGES - 2>();
-        __syncthreads();
-        issue(i + G::STAGES - 1);
-        cp_commit();
-        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE, ss = st + TM * G::X_STRIDE;
-        constexpr int KPW = G::KC / G::KW;                   // source columns of a warp
-#pragma unroll
-        for (int k = 0; k < KPW; k += KSTEP) {
-            const int kk = kw * KPW + k;
-            FragA<T> a;
-            load_a(a, st + rg * 16 * G::X_STRIDE + kk * E, G::X_STRIDE, lane);
-#pragma unroll
-            for (int j = 0; j < RP / 8; j += 2) {
-                if (j * 8 >= r16) break;
-                FragB<T> b[2];
-                if (!TRANS) load_b2(b, ss + j * 8 * G::S_STRIDE + kk * E, G::S_STRIDE, lane);
-                else load_b2_t(b, ss + kk * G::S_STRIDE + j * 8 * E, G::S_STRIDE, lane);
-                mma_step(acc[j], a, b[0]);
-                mma_step(acc[j + 1], a, b[1]);
+    {
+        const int steps = max(0, min(kb1, ws / KB) - kb0) / NB;
+        SrcX x0, x1;
+        SrcW w0, w1;
+        if (steps > 0) load_x(x0);
+        pdl_wait();             // A and B may have been laid out by the kernel ahead
+        pdl_launch_dependents();
+        if (steps > 0) load_w(w0, 0);
+        if constexpr (G::AHEAD) {
+#pragma unroll 1
+            for (int i = 0; i < steps; i += 2) {
+                if (i + 1 < steps) {
+                    load_x(x1);
+                    load_w(w1, 0);
+                }
+                multiply(x0, w0, NB, 0);
+                if (i + 2 < steps) {
+                    load_x(x0);
+                    load_w(w0, 0);
+                }
+                if (i + 1 < steps) multiply(x1, w1, NB, 0);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < steps; i += 2) {
+                load_w(w1, JH);
+                if (i + 1 < steps) load_x(x1);
+                multiply(x0, w0, NB, 0);
+                if (i + 1 < steps) load_w(w0, 0);
+                multiply(x0, w1, NB, JH);
+                if (i + 1 < steps) {
+                    load_w(w1, JH);
+                    if (i + 2 < steps) load_x(x0);
+                    multiply(x1, w0, NB, 0);
+                    if (i + 2 < steps) load_w(w0, 0);
+                    multiply(x1, w1, NB, JH);
+                }
             }
         }
+        // what is left: at most NB blocks, the last of them perhaps in part
+#pragma unroll 1
+        for (int kb = kb0 + steps * NB; kb < kb1; ++kb) {
+            const int n = min(max(ws - kb * KB - t4 * U, 0), U);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                x0.x[0][h] = load_some<E>(px[h], n);
+                px[h] += BLOCK;
+            }
+#pragma unroll
+            for (int j0 = 0; j0 < JT; j0 += JH) {
+#pragma unroll
+                for (int j = 0; j < JH; ++j) {
+                    if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
+                    w0.w[0][j] = load_some<E>(pw + w_off[j0 + j], n);
+                }
+                multiply(x0, w0, 1, j0);
+            }
+            pw += BLOCK;
+        }
+    }
+    // ---- the first destination block sets out. The accumulator columns of tile j are columns 2j, 2j + 1 of every lane's U:
+    // that is the column of B which this lane's 8-column index g stands for
+    struct DstY { uint4 y[2]; };
+    constexpr int SH = G::AHEAD ? ST : ST / 2;              // steps of the rank that are loaded at a time
+    struct DstB { uint2 b[SH][NT]; };
+    const int bcol = (g >> 1) * U + (g & 1);
+    const char *pb = (const char *)ent.expand + (((long long)nb0 * KB + bcol) * ent.ld_e + t4 * (KSTEP / 4)) * E;
+    const long long b_next = (long long)KW * KB * ent.ld_e * E;
+    const u32 b_pair = 2u * (u32)ent.ld_e * E;
+    // a lane holds a quad of ranks per step; those past the end of a row are read as zeros (ranks are whole quads here)
+    u32 b_there = 0;
+#pragma unroll
+    for (int s = 0; s < ST; ++s)
+        if (s * KSTEP + t4 * (KSTEP / 4) < rank) b_there |= 1u << s;
+    // (of a block that exists in part, columns past the end are read as the last one)
+    auto load_b = [&](DstB &d, int s0, int last) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const char *p = pb + (last < KB ? (long long)(min(bcol + 2 * j, last) - bcol) * ent.ld_e * E : (long long)(j * b_pair));
+#pragma unroll
+            for (int s = 0; s < SH; ++s) {
+                if (s0 + s && (s0 + s) * KSTEP >= r16) break;
+                d.b[s][j] = (b_there >> (s0 + s) & 1) ? *reinterpret_cast<const uint2 *>(p + (s0 + s) * KSTEP * E) : make_uint2(0, 0);
+            }
+        }
+        if (s0 + SH == ST) pb += b_next;
+    };
+    auto load_y = [&](DstY &d) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            d.y[h] = load_unit<V, E, true>(py[h]);
+            py[h] += KW * BLOCK;
+        }
+    };
+    const int blocks = max(0, min(nb1, wd / KB) - nb0 + KW - 1) / KW;          // that exist as a whole
+    DstY y0, y1;
+    DstB b0;
+    if (blocks > 0) {
+        load_y(y0);
+        load_b(b0, 0, KB);
     }
     // ---- the warps of a row group add up, the upper half handing its sums to the lower
-    const int g = lane >> 2, t4 = lane & 3;
     auto spot = [&](int slot, int j, int half) { return hp + ((slot * TM + rg * 16 + g + 8 * half) * G::HP_STRIDE + j * 8 + 2 * t4); };
+    auto put = [&](int slot) {
 #pragma unroll
-    for (int w = G::KW / 2; w >= 1; w >>= 1) {
-        if (kw >= w && kw < 2 * w) {
-#pragma unroll
-            for (int j = 0; j < RP / 8; ++j) {
-                if (j * 8 >= r16) break;
-                *reinterpret_cast<float2 *>(spot(kw - w, j, 0)) = make_float2(acc[j][0], acc[j][1]);
-                *reinterpret_cast<float2 *>(spot(kw - w, j, 1)) = make_float2(acc[j][2], acc[j][3]);
-            }
+        for (int j = 0; j < JT; ++j) {
+            if (j * 8 >= r16) break;
+            *reinterpret_cast<float2 *>(spot(slot, j, 0)) = make_float2(acc[j][0], acc[j][1]);
+            *reinterpret_cast<float2 *>(spot(slot, j, 1)) = make_float2(acc[j][2], acc[j][3]);
         }
+    };
+#pragma unroll 1
+    for (int w = KW / 2; w >= 1; w >>= 1) {
+        if (kw >= w && kw < 2 * w) put(kw - w);
         __syncthreads();
         if (kw < w) {
 #pragma unroll
-            for (int j = 0; j < RP / 8; ++j) {
+            for (int j = 0; j < JT; ++j) {
                 if (j * 8 >= r16) break;
                 const float2 p = *reinterpret_cast<const float2 *>(spot(kw, j, 0)), q = *reinterpret_cast<const float2 *>(spot(kw, j, 1));
                 acc[j][0] += p.x; acc[j][1] += p.y; acc[j][2] += q.x; acc[j][3] += q.y;
@@ -478,21 +657,16 @@ __global__ void __launch_bounds__(THREADS) k_adapter(const __grid_constant__ Ada
         }
         __syncthreads();
     }
-    if (kw == 0) {
-#pragma unroll
-        for (int j = 0; j < RP / 8; ++j) {
-            if (j * 8 >= r16) break;
-            *reinterpret_cast<float2 *>(spot(0, j, 0)) = make_float2(acc[j][0], acc[j][1]);
-            *reinterpret_cast<float2 *>(spot(0, j, 1)) = make_float2(acc[j][2], acc[j][3]);
-        }
-    }
+    if (kw == 0) put(0);
     // ---- the CTAs of the cluster add up, in order of their rank; every one of them needs all of h
     cluster_arrive();
     cluster_wait();
+    const float factor = P.scale_h ? 1.0f : ent.scale;
     {
         constexpr int TPR = THREADS / TM;                    // threads of a row
         constexpr int QT = (RP / 4 + TPR - 1) / TPR;         // quads of a thread
         const int r = tid / TPR, sub = tid % TPR;
+        const float f = P.scale_h ? ent.scale : 1.0f;
         float4 v[QT];
         float most = 0.0f;
 #pragma unroll
@@ -508,13 +682,11 @@ __global__ void __launch_bounds__(THREADS) k_adapter(const __grid_constant__ Ada
 #pragma unroll
                 for (int p = 0; p < AD_MAX_CLUSTER; ++p)
                     if (p < C) { v[q].x += x[p].x; v[q].y += x[p].y; v[q].z += x[p].z; v[q].w += x[p].w; }
-                const float f = TRANS ? ent.scale : 1.0f;
-                // rows and columns that do not exist hold what shared memory held before
-                v[q].x = r < count && c < rank ? f * v[q].x : 0.0f;
-                v[q].y = r < count && c + 1 < rank ? f * v[q].y : 0.0f;
-                v[q].z = r < count && c + 2 < rank ? f * v[q].z : 0.0f;
-                v[q].w = r < count && c + 3 < rank ? f * v[q].w : 0.0f;
-                if (P.h && r < count && r % C == c_rank) {
+                v[q].x = c < rank ? f * v[q].x : 0.0f;
+                v[q].y = c + 1 < rank ? f * v[q].y : 0.0f;
+                v[q].z = c + 2 < rank ? f * v[q].z : 0.0f;
+                v[q].w = c + 3 < rank ? f * v[q].w : 0.0f;
+                if (P.h && split == 0 && r < count && r % C == c_rank) {
                     float *o = P.h + (long long)srow[r] * P.ld_h + c;
                     const float w[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
 #pragma unroll
@@ -528,16 +700,16 @@ __global__ void __launch_bounds__(THREADS) k_adapter(const __grid_constant__ Ada
         if (std::is_same<T, __half>::value) {       // binary16 has not fp32's range: a power of two per row
 #pragma unroll
             for (int o = TPR / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-            const float f = pow2_above(most);
-            inv = pow2_inverse(f);
-            if (sub == 0) sfac[r] = f;
+            const float p2 = pow2_above(most);
+            inv = pow2_inverse(p2);
+            if (sub == 0) sfac[r] = p2;
         }
 #pragma unroll
         for (int q = 0; q < QT; ++q) {
             const int c = 4 * (q * TPR + sub);
             if (c < r16) {
                 const float x[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
-                if constexpr (sizeof(T) == 2) {
+                if constexpr (E == 2) {
                     u16 p[4][PARTS];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) split16<T, PARTS>(x[e] * inv, p[e]);
@@ -553,91 +725,107 @@ __global__ void __launch_bounds__(THREADS) k_adapter(const __grid_constant__ Ada
     }
     cluster_arrive();           // this CTA has read its peers' sums
     __syncthreads();
-    // ---- expand
-    const u32 hob = smem_u32(ho);
-    const float factor = TRANS ? 1.0f : ent.scale;
-    float row_f[2] = {factor, factor};
-    if (std::is_same<T, __half>::value) {
-        row_f[0] *= sfac[rg * 16 + g];
-        row_f[1] *= sfac[rg * 16 + g + 8];
+    // ---- expand: a lane has U neighbouring columns of each of its two rows
+    float row_f[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) row_f[h] = std::is_same<T, __half>::value ? factor * sfac[rg * 16 + g + 8 * h] : factor;
+    auto load_h = [&](FragA<T> &a, int s, int p) {
+        const char *at = ho + (p * TM + rg * 16 + g) * G::HO_STRIDE + (s * KSTEP + t4 * (KSTEP / 4)) * E;
+        frag_h(a, *reinterpret_cast<const uint2 *>(at), *reinterpret_cast<const uint2 *>(at + 8 * G::HO_STRIDE));
+    };
+    constexpr bool HOLD = RP <= 32 && E == 2;                // h stays in registers
+    FragA<T> hold[HOLD ? ST : 1][PARTS];
+    if constexpr (HOLD) {
+#pragma unroll
+        for (int s = 0; s < ST; ++s)
+            if (s * KSTEP < r16)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) load_h(hold[s][p], s, p);
     }
-    for (; i < total; ++i) {
-        cp_wait<G::STAGES - 2>();
-        __syncthreads();
-        issue(i + G::STAGES - 1);
-        cp_commit();
-        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE, se = st + TM * G::Y_STRIDE;
-        float d[NT][4];
+    float d[NT][4];
+    auto expand = [&](const DstB &x, int s0) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int s = 0; s < SH; ++s) {
+            if (s0 + s && (s0 + s) * KSTEP >= r16) break;
+            FragB<T> b[NT];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) d[j][q] = 0.0f;
+            for (int j = 0; j < NT; ++j) frag_b(b[j], x.b[s][j].x, x.b[s][j].y);
 #pragma unroll
-        for (int k = 0; k < RP; k += KSTEP) {
-            if (k >= r16) break;
-            FragA<T> a[PARTS];
+            for (int p = PARTS - 1; p >= 0; --p) {
+                FragA<T> a;
+                if constexpr (HOLD) a = hold[s][p];
+                else load_h(a, s0 + s, p);
 #pragma unroll
-            for (int s = 0; s < PARTS; ++s) load_a(a[s], hob + (s * TM + rg * 16) * G::HO_STRIDE + k * E, G::HO_STRIDE, lane);
-#pragma unroll
-            for (int j = 0; j < NT; j += 2) {
-                FragB<T> b[2];
-                if (!TRANS) load_b2(b, se + (kw * G::NWC + j * 8) * G::E_STRIDE + k * E, G::E_STRIDE, lane);
-                else load_b2_t(b, se + k * G::E_STRIDE + (kw * G::NWC + j * 8) * E, G::E_STRIDE, lane);
-#pragma unroll
-                for (int s = PARTS - 1; s >= 0; --s) {
-                    mma_step(d[j], a[s], b[0]);
-                    mma_step(d[j + 1], a[s], b[1]);
+                for (int j = 0; j < NT; ++j) {
+                    if (s0 + s == 0 && p == PARTS - 1) mma_first(d[j], a, b[j]);
+                    else mma_step(d[j], a, b[j]);
                 }
             }
         }
-        // this thread's 2 * NT neighbouring columns of two rows
-        const int cl = kw * G::NWC + t4 * 2 * NT;
-        const long long col = (long long)(nc0 + i - nk) * G::NC + cl;
-        const int wide = (int)min((long long)(2 * NT), P.width_dst - col);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int r = rg * 16 + g + 8 * half;
-            if (r >= count || wide <= 0) continue;
-            const uint4 old = *reinterpret_cast<const uint4 *>(sm + G::FIXED + (i % G::STAGES) * G::STAGE + r * G::Y_STRIDE + cl * E);
-            const u32 o[4] = {old.x, old.y, old.z, old.w};
-            u32 w[4];
-            if constexpr (E == 2) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    T lo, hi;
-                    *reinterpret_cast<u16 *>(&lo) = (u16)(o[j] & 0xFFFF);
-                    *reinterpret_cast<u16 *>(&hi) = (u16)(o[j] >> 16);
-                    const T x = (T)((float)lo + row_f[half] * d[j][2 * half]), y = (T)((float)hi + row_f[half] * d[j][2 * half + 1]);
-                    w[j] = (u32) * reinterpret_cast<const u16 *>(&x) | ((u32) * reinterpret_cast<const u16 *>(&y) << 16);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    w[j] = __float_as_uint(__uint_as_float(o[j]) + row_f[half] * d[j >> 1][2 * half + (j & 1)]);
+    };
+    auto finish = [&](const DstY &y, char *o0, char *o1, int n) {
+        if (live[0]) store_unit<V, E>(o0, add_unit<T, NT>(y.y[0], d, 0, row_f[0]), n);
+        if (live[1]) store_unit<V, E>(o1, add_unit<T, NT>(y.y[1], d, 1, row_f[1]), n);
+    };
+    const long long ahead = blocks > 0 ? KW * BLOCK : 0;             // (the loads run ahead of the stores)
+    char *o0 = py[0] - ahead, *o1 = py[1] - ahead;
+    auto next = [&]() {
+        o0 += KW * BLOCK;
+        o1 += KW * BLOCK;
+    };
+    DstB b1;
+    if constexpr (G::AHEAD) {
+#pragma unroll 1
+        for (int i = 0; i < blocks; i += 2) {
+            if (i + 1 < blocks) {
+                load_y(y1);
+                load_b(b1, 0, KB);
             }
-            char *out = (char *)P.dst + ((long long)srow[r] * P.ld_dst + col) * E;
-            if (wide == 2 * NT && P.vec_dst >= 16) *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-            else if (wide == 2 * NT && P.vec_dst == 8) {
-                reinterpret_cast<uint2 *>(out)[0] = make_uint2(w[0], w[1]);
-                reinterpret_cast<uint2 *>(out)[1] = make_uint2(w[2], w[3]);
-            } else if (E == 4) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < wide) reinterpret_cast<u32 *>(out)[j] = w[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (P.vec_dst == 4 && 2 * j + 1 < wide) reinterpret_cast<u32 *>(out)[j] = w[j];
-                    else {
-                        if (2 * j < wide) reinterpret_cast<u16 *>(out)[2 * j] = (u16)w[j];
-                        if (2 * j + 1 < wide) reinterpret_cast<u16 *>(out)[2 * j + 1] = (u16)(w[j] >> 16);
-                    }
-                }
+            expand(b0, 0);
+            finish(y0, o0, o1, U);
+            next();
+            if (i + 2 < blocks) {
+                load_y(y0);
+                load_b(b0, 0, KB);
+            }
+            if (i + 1 < blocks) {
+                expand(b1, 0);
+                finish(y1, o0, o1, U);
+                next();
             }
         }
-        __syncwarp();
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < blocks; i += 2) {
+            load_b(b1, SH, KB);
+            if (i + 1 < blocks) load_y(y1);
+            expand(b0, 0);
+            if (i + 1 < blocks) load_b(b0, 0, KB);
+            expand(b1, SH);
+            finish(y0, o0, o1, U);
+            next();
+            if (i + 1 < blocks) {
+                load_b(b1, SH, KB);
+                if (i + 2 < blocks) load_y(y0);
+                expand(b0, 0);
+                if (i + 2 < blocks) load_b(b0, 0, KB);
+                expand(b1, SH);
+                finish(y1, o0, o1, U);
+                next();
+            }
+        }
     }
-    cp_wait<0>();
+    if (nb0 + blocks * KW < nb1) {              // the last block, in part
+        const int left = wd - (nb0 + blocks * KW) * KB, n = min(max(left - t4 * U, 0), U);
+        y0.y[0] = load_some<E>(o0, n);
+        y0.y[1] = load_some<E>(o1, n);
+#pragma unroll
+        for (int s0 = 0; s0 < ST; s0 += SH) {
+            load_b(b0, s0, left - 1);
+            expand(b0, s0);
+        }
+        finish(y0, o0, o1, n);
+    }
     __syncwarp();
     cluster_wait();             // peers may still read this CTA's sums until here
 }
@@ -645,22 +833,18 @@ __global__ void __launch_bounds__(THREADS) k_adapter(const __grid_constant__ Ada
 // ------------------------------------------------------------------ weight gradients
 // dA = u^T x and dB = scale * dy^T h: for each adapter, a sum over its rows of a column (u or h, `rank` numbers) times
 // a row of activations (x or dy). A CTA takes a strip of activation columns and a share of the adapter's
-// rows (a split), tile by tile; its sums go to the gradient itself where there is one split, else to the
-// workspace, and k_adapter_reduce adds the splits in order. The coefficients are fp32 and the results too,
-// so they enter the products with their whole precision: three 16-bit parts in bfloat16, two in binary16 under a
-// power of two that follows the largest seen so far.
+// rows, 64 at a time; the CTAs that share an adapter's rows are a cluster and add their sums over distributed
+// shared memory, in order, so there are neither atomics nor a second launch. The coefficients are fp32 and the
+// results too, so they enter the products with their whole precision: three 16-bit parts in bfloat16, two in
+// binary16 under a power of two that follows the largest seen so far.
 struct WgEntry {
     float *out[2];           // dA, dB; NULL: not formed
     float scale;
     int rank;
+    int n_rows;
+    u16 run0, n_runs;
 };
-struct WgSplit {
-    long long slot;          // place of its sums in the workspace (floats); -1: straight into the gradient
-    int tile0;
-    u16 n_tiles;
-    u16 adapter;
-};
-static_assert(sizeof(WgEntry) == 24 && sizeof(WgSplit) == 16, "packed into the parameters");
+static_assert(sizeof(WgEntry) == 32, "packed into the parameters");
 
 struct WgSide {
     const void *act;         // x | dy
@@ -671,71 +855,89 @@ struct WgSide {
 
 struct WgradParams {
     WgSide side[2];
-    float *part;
     int strips0;             // strips of side 0; the others are side 1's
     int accumulate;
-    int n_entries, n_splits, n_tiles;
+    int n_entries;
     int pad;
-    u32 blob[AD_BLOB / 4];   // entries, splits, tiles, rows
+    u32 blob[AD_BLOB / 4];   // entries, runs
 };
 static_assert(sizeof(WgradParams) <= 4096, "kernel parameters");
 
 template <class T, int RP>
 struct WgGeom {
-    static constexpr int E = AdType<T>::E;
+    static constexpr int E = AdType<T>::E, R = AD_WG_ROWS;
     static constexpr int WC = (E == 2 && RP <= 64) ? 256 : 128;        // columns of a strip
     static constexpr int NTW = WC / 64;                                // 8-column tiles of a warp
     static constexpr int X_STRIDE = WC * E + 16, F_STRIDE = RP * 4 + 16, C_STRIDE = RP * 2 + 16;
     static constexpr int PARTS = std::is_same<T, __nv_bfloat16>::value ? 3 : std::is_same<T, __half>::value ? 2 : 0;
-    static constexpr int STAGE = AD_WG_ROWS * (X_STRIDE + F_STRIDE);
-    static constexpr int CONV = PARTS * AD_WG_ROWS * C_STRIDE;
-    static constexpr int FIXED = CONV + 64;
+    static constexpr int STAGE = R * (X_STRIDE + F_STRIDE);
+    static constexpr int CONV = PARTS * R * C_STRIDE;
+    static constexpr int O_STRIDE = WC + 4;                            // floats: this CTA's sums, [rank][column]
+    static constexpr int ROWS = 4 * R * 4;                             // row numbers of four tiles
+    static constexpr int FIXED = CONV + ROWS + 64;
     static constexpr int STAGES = FIXED + 3 * STAGE <= 113 * 1024 ? 3 : FIXED + 2 * STAGE <= 113 * 1024 ? 2 : FIXED + 3 * STAGE <= 227 * 1024 ? 3 : 2;
     static constexpr int SMEM = FIXED + STAGES * STAGE;
     static_assert(SMEM <= 227 * 1024 && STAGE % 16 == 0 && CONV % 16 == 0, "shared memory");
+    static_assert(RP * O_STRIDE * 4 <= STAGES * STAGE, "the sums lie where the stages were");
 };
 
-template <class T, int RP>
+template <class T, int RP, int V>
 __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant__ WgradParams P)
 {
     using G = WgGeom<T, RP>;
-    constexpr int E = G::E, KSTEP = AdType<T>::KSTEP, NTW = G::NTW, R = AD_WG_ROWS;
+    constexpr int E = G::E, KSTEP = AdType<T>::KSTEP, NTW = G::NTW, R = G::R;
     constexpr bool HALF = std::is_same<T, __half>::value;
     extern __shared__ __align__(128) char sm[];
-    float *smax = reinterpret_cast<float *>(sm + G::CONV);
+    int *srow = reinterpret_cast<int *>(sm + G::CONV);                 // [4][R]
+    float *smax = reinterpret_cast<float *>(sm + G::CONV + G::ROWS);
     const u32 ring = smem_u32(sm + G::FIXED), conv = smem_u32(sm);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = (int)cluster_size(), c_rank = (int)cluster_rank();
     const int sd = (int)blockIdx.x >= P.strips0 ? 1 : 0;
     const WgSide &S = P.side[sd];
     const WgEntry *entries = reinterpret_cast<const WgEntry *>(P.blob);
-    const WgSplit *splits = reinterpret_cast<const WgSplit *>(entries + P.n_entries);
-    const AdapterTile *tiles = reinterpret_cast<const AdapterTile *>(splits + P.n_splits);
-    const int *row_list = reinterpret_cast<const int *>(tiles + P.n_tiles);
-    const WgSplit sp = splits[blockIdx.y];
-    const WgEntry ent = entries[sp.adapter];
+    const WgEntry &ent = entries[blockIdx.y / C];
+    const AdapterRun *runs = reinterpret_cast<const AdapterRun *>(entries + P.n_entries) + ent.run0;
     float *out = ent.out[sd];
-    if (!out) return;
-    const int rank = ent.rank, r16 = (rank + 15) & ~15;
+    if (!out) {                                                        // (all CTAs of the cluster leave)
+        pdl_wait();
+        return;
+    }
+    const int rank = ent.rank, r16 = (rank + 15) & ~15, n_rows = ent.n_rows, n_runs = ent.n_runs;
     const long long col0 = (long long)((int)blockIdx.x - (sd ? P.strips0 : 0)) * G::WC;
     const int wide = (int)min((long long)G::WC, S.width - col0);
+    const int tiles = (n_rows + R - 1) / R;
+    const int t0 = (int)((long long)c_rank * tiles / C), nt = (int)((long long)(c_rank + 1) * tiles / C) - t0;
+
+    auto number_rows = [&](int i) {                                    // rows of this CTA's tile i, -1 past the end
+        if (tid < R && i < nt) {
+            const int r = (t0 + i) * R + tid;
+            srow[(i & 3) * R + tid] = r < n_rows ? adapter_row(runs, n_runs, r) : -1;
+        }
+    };
+    constexpr int XU = G::WC * E / 16, XN = R * XU / THREADS, FU = RP / 4, FN = R * FU / THREADS;
+    const int xq = (tid % XU) * 16, xr = tid / XU, fq = (tid % FU) * 16, fr = tid / FU;
+    const int xn = min(max(wide * E - xq, 0), 16), fn = min(max(rank * 4 - fq, 0), 16);
+    const char *act = (const char *)S.act, *coef = (const char *)S.coef;
+    const char *xbase = act + col0 * E + xq;
+    const long long ldx = S.ld_act * E, ldf = S.ld_coef * 4;
+    const int vec_act = S.vec_act, vec_coef = S.vec_coef;             // (the latter at most 8: copied 8 bytes at a time)
 
     auto issue = [&](int i) {
-        if (i >= sp.n_tiles) return;
-        const AdapterTile tile = tiles[sp.tile0 + i];
-        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE;
-        auto row_of = [&](int r) { return (long long)(r < tile.count ? (tile.list < 0 ? tile.first + r : row_list[tile.list + r]) : 0); };
-        constexpr int XU = G::WC * E / 16;
-        for (int u = tid; u < R * XU; u += THREADS) {        // (rows that do not exist become zero: they are summed over)
-            const int r = u / XU, q = (u % XU) * 16;
-            copy_unit(st + r * G::X_STRIDE + q, (const char *)S.act + (row_of(r) * S.ld_act + col0) * E + q, (const char *)S.act,
-                      r < tile.count ? wide * E - q : 0, S.vec_act);
+        if (i >= nt) return;
+        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE, sf = st + R * G::X_STRIDE;
+        const int *rows = srow + (i & 3) * R;
+#pragma unroll
+        for (int j = 0; j < XN; ++j) {           // (rows that do not exist become zero: they are summed over)
+            const int r = xr + THREADS / XU * j, row = rows[r];
+            copy_unit<V>(st + r * G::X_STRIDE + xq, xbase + row * ldx, act, row >= 0 ? xn : 0, vec_act);
         }
-        const u32 sf = st + R * G::X_STRIDE;
-        const int upr = r16 / 4;
-        for (int u = tid; u < R * upr; u += THREADS) {
-            const int r = u / upr, q = (u % upr) * 16;
-            copy_unit(sf + r * G::F_STRIDE + q, (const char *)(S.coef + row_of(r) * S.ld_coef) + q, (const char *)S.coef,
-                      r < tile.count ? rank * 4 - q : 0, S.vec_coef);
+        if (fq < r16 * 4) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int r = fr + THREADS / FU * j, row = rows[r];
+                copy_unit<0>(sf + r * G::F_STRIDE + fq, coef + row * ldf + fq, coef, row >= 0 ? fn : 0, vec_coef);
+            }
         }
     };
 
@@ -748,26 +950,30 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant
             for (int q = 0; q < 4; ++q) acc[m][n][q] = 0.0f;
     float top = 0.0f, unit = 1.1754943508222875e-38f;        // binary16: largest coefficient so far, the power of two that goes with it
 #pragma unroll
-    for (int i = 0; i < G::STAGES - 1; ++i) {
-        issue(i);
-        cp_commit();
-    }
-    for (int i = 0; i < sp.n_tiles; ++i) {
-        cp_wait<G::STAGES - 2>();
-        __syncthreads();
+    for (int i = 0; i < G::STAGES; ++i) number_rows(i);
+    __syncthreads();
+    if (sd == 0) pdl_wait();                                           // u is the kernel before's; x, dy and h are not
+#pragma unroll 1
+    for (int i = 1 - G::STAGES; i < nt; ++i) {
+        if (i >= 0) {
+            cp_wait<G::STAGES - 2>();
+            __syncthreads();
+        }
         issue(i + G::STAGES - 1);
         cp_commit();
+        if (i < 0) continue;
+        number_rows(i + G::STAGES);
         const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE;
         const char *sf = sm + G::FIXED + (i % G::STAGES) * G::STAGE + R * G::X_STRIDE;
         if constexpr (E == 2) {
-            const int upr = r16 / 4;
-            float inv = 1.0f;
+            float4 v[FN];
+            float inv = 1.0f, most = 0.0f;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                v[j] = fq < r16 * 4 ? *reinterpret_cast<const float4 *>(sf + (fr + THREADS / FU * j) * G::F_STRIDE + fq) : make_float4(0.f, 0.f, 0.f, 0.f);
+                if (HALF) most = fmaxf(most, fmaxf(fmaxf(fabsf(v[j].x), fabsf(v[j].y)), fmaxf(fabsf(v[j].z), fabsf(v[j].w))));
+            }
             if constexpr (HALF) {
-                float most = 0.0f;
-                for (int u = tid; u < R * upr; u += THREADS) {
-                    const float4 v = *reinterpret_cast<const float4 *>(sf + (u / upr) * G::F_STRIDE + (u % upr) * 16);
-                    most = fmaxf(most, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
-                }
 #pragma unroll
                 for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
                 if (lane == 0) smax[warp] = most;
@@ -776,106 +982,174 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant
                 for (int w = 0; w < WARPS; ++w) most = fmaxf(most, smax[w]);
                 if (most > top) {
                     top = most;
-                    const float next = pow2_above(top), shrink = unit * pow2_inverse(next);      // at most 1
+                    const float next = pow2_above(top), less = unit * pow2_inverse(next);        // at most 1
                     unit = next;
 #pragma unroll
                     for (int m = 0; m < RP / 16; ++m)
 #pragma unroll
                         for (int n = 0; n < NTW; ++n)
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) acc[m][n][q] *= shrink;
+                            for (int q = 0; q < 4; ++q) acc[m][n][q] *= less;
                 }
                 inv = pow2_inverse(unit);
             }
-            for (int u = tid; u < R * upr; u += THREADS) {
-                const int r = u / upr, c = (u % upr) * 4;
-                const float4 v = *reinterpret_cast<const float4 *>(sf + r * G::F_STRIDE + c * 4);
-                const float x[4] = {v.x, v.y, v.z, v.w};
-                u16 p[4][G::PARTS];
+            if (fq < r16 * 4) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) split16<T, G::PARTS>(HALF ? x[e] * inv : x[e], p[e]);
+                for (int j = 0; j < FN; ++j) {
+                    const float x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+                    u16 p[4][G::PARTS];
 #pragma unroll
-                for (int s = 0; s < G::PARTS; ++s)
-                    *reinterpret_cast<uint2 *>(sm + (s * R + r) * G::C_STRIDE + 2 * c) =
-                        make_uint2((u32)p[0][s] | ((u32)p[1][s] << 16), (u32)p[2][s] | ((u32)p[3][s] << 16));
+                    for (int e = 0; e < 4; ++e) split16<T, G::PARTS>(HALF ? x[e] * inv : x[e], p[e]);
+#pragma unroll
+                    for (int s = 0; s < G::PARTS; ++s)
+                        *reinterpret_cast<uint2 *>(sm + (s * R + fr + THREADS / FU * j) * G::C_STRIDE + fq / 2) =
+                            make_uint2((u32)p[0][s] | ((u32)p[1][s] << 16), (u32)p[2][s] | ((u32)p[3][s] << 16));
+                }
             }
             __syncthreads();
         }
+        // 32 rows at a time, their sums apart from the others: the matrix instruction truncates
+        constexpr int HK = 32 / KSTEP;
 #pragma unroll 1
-        for (int k = 0; k < R; k += KSTEP) {
-            FragB<T> b[NTW / 2][2];
+        for (int k0 = 0; k0 < R; k0 += 32) {
+            FragB<T> b[HK][NTW / 2][2];
 #pragma unroll
-            for (int n = 0; n < NTW / 2; ++n) load_b2_t(b[n], st + k * G::X_STRIDE + (warp * NTW * 8 + n * 16) * E, G::X_STRIDE, lane);
+            for (int k = 0; k < HK; ++k)
+#pragma unroll
+                for (int n = 0; n < NTW / 2; ++n)
+                    load_b2_t(b[k][n], st + (k0 + k * KSTEP) * G::X_STRIDE + (warp * NTW * 8 + n * 16) * E, G::X_STRIDE, lane);
 #pragma unroll
             for (int m = 0; m < RP / 16; ++m) {
                 if (m * 16 >= r16) break;
-                if constexpr (E == 2) {
+                float d[NTW][4];
 #pragma unroll
-                    for (int s = G::PARTS - 1; s >= 0; --s) {
+                for (int n = 0; n < NTW; ++n)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) d[n][q] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < HK; ++k) {
+                    const int row = k0 + k * KSTEP;
+                    if constexpr (E == 2) {
+#pragma unroll
+                        for (int s = G::PARTS - 1; s >= 0; --s) {
+                            FragA<T> a;
+                            load_a_t(a, conv + (s * R + row) * G::C_STRIDE + m * 32, G::C_STRIDE, lane);
+#pragma unroll
+                            for (int n = 0; n < NTW; ++n) mma_step(d[n], a, b[k][n >> 1][n & 1]);
+                        }
+                    } else {
                         FragA<T> a;
-                        load_a_t(a, conv + (s * R + k) * G::C_STRIDE + m * 32, G::C_STRIDE, lane);
+                        load_a_t(a, smem_u32(sf) + row * G::F_STRIDE + m * 64, G::F_STRIDE, lane);
 #pragma unroll
-                        for (int n = 0; n < NTW; ++n) mma_step(acc[m][n], a, b[n >> 1][n & 1]);
+                        for (int n = 0; n < NTW; ++n) mma_step(d[n], a, b[k][n >> 1][n & 1]);
                     }
-                } else {
-                    FragA<T> a;
-                    load_a_t(a, smem_u32(sf) + k * G::F_STRIDE + m * 64, G::F_STRIDE, lane);
-#pragma unroll
-                    for (int n = 0; n < NTW; ++n) mma_step(acc[m][n], a, b[n >> 1][n & 1]);
                 }
+#pragma unroll
+                for (int n = 0; n < NTW; ++n)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[m][n][q] += d[n][q];
             }
         }
     }
+    // ---- this CTA's sums into shared memory, then the cluster's, each CTA adding its share of the columns
     cp_wait<0>();
+    __syncthreads();
+    float *so = reinterpret_cast<float *>(sm + G::FIXED);
     const float factor = (sd ? ent.scale : 1.0f) * (HALF ? unit : 1.0f);
-    const bool direct = sp.slot < 0, add = direct && P.accumulate;
-    float *o = direct ? out : P.part + sp.slot + (sd ? (long long)rank * P.side[0].width : 0);
     const int g = lane >> 2, t4 = lane & 3;
 #pragma unroll
-    for (int m = 0; m < RP / 16; ++m)
+    for (int m = 0; m < RP / 16; ++m) {
+        if (m * 16 >= r16) break;
 #pragma unroll
         for (int n = 0; n < NTW; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int row = m * 16 + g + (q >> 1) * 8, c = warp * NTW * 8 + n * 8 + 2 * t4 + (q & 1);
-                if (row < rank && c < wide) {
-                    float *to = o + (sd ? (col0 + c) * rank + row : (long long)row * S.width + col0 + c);
-                    const float v = factor * acc[m][n][q];
-                    *to = add ? *to + v : v;
-                }
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<float2 *>(so + (m * 16 + g + 8 * h) * G::O_STRIDE + warp * NTW * 8 + n * 8 + 2 * t4) =
+                    make_float2(factor * acc[m][n][2 * h], factor * acc[m][n][2 * h + 1]);
+    }
+    cluster_arrive();
+    cluster_wait();
+    const u32 so_u = smem_u32(so);
+    const int quads = rank * (G::WC / 4);
+    for (int u = c_rank * THREADS + tid; u < quads; u += C * THREADS) {
+        // dA is written along its rows, dB (whose rows are `rank` numbers) along the ranks
+        const int m = sd ? u % rank : u / (G::WC / 4), c = (sd ? u / rank : u % (G::WC / 4)) * 4;
+        if (c >= wide) continue;
+        const u32 at = so_u + (m * G::O_STRIDE + c) * 4;
+        float4 x[AD_MAX_CLUSTER], v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int p = 0; p < AD_MAX_CLUSTER; ++p)
+            if (p < C) x[p] = ld_cluster(at, (u32)p);
+#pragma unroll
+        for (int p = 0; p < AD_MAX_CLUSTER; ++p)
+            if (p < C) { v.x += x[p].x; v.y += x[p].y; v.z += x[p].z; v.w += x[p].w; }
+        const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < wide) {
+                float *to = out + (sd ? (col0 + c + e) * rank + m : (long long)m * S.width + col0 + c + e);
+                *to = P.accumulate ? *to + w[e] : w[e];
             }
+    }
+    if (sd) pdl_wait();         // no CTA leaves ahead of the kernel before
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();             // peers may still read this CTA's sums until here
 }
 
-// Adds the splits of each gradient, in order; an adapter without rows gets zeros.
-struct RedEntry {
-    float *out[2];
-    long long slot;          // first split's sums
-    int splits;
-    int rank;
+// A and B laid out anew ahead of the row kernel, rows padded with zeros to 16 bytes: for the backward pass transposed (it
+// wants B by its columns and A by its columns), for the forward pass where their rows do not allow the accesses that
+// it makes (odd ranks, odd widths). They are a small part of what the row kernel moves.
+struct PackItem {
+    const void *src;         // [rows][cols]
+    void *dst;               // [rows][ld], or transposed [cols][ld]
+    long long rows, cols;
+    int ld, trans;
+    int block0, pad;         // first CTA of the item
 };
-constexpr int AD_RED_MAX = 120;
-struct ReduceParams {
-    const float *part;
-    long long width[2];
-    int accumulate;
-    int pad;
-    RedEntry e[AD_RED_MAX];
+constexpr int AD_PACK_MAX = 80, AD_PACK_TILE = 64;
+struct PackParams {
+    int n, pad;
+    PackItem item[AD_PACK_MAX];
 };
-static_assert(sizeof(ReduceParams) <= 4096, "kernel parameters");
+static_assert(sizeof(PackItem) == 48 && sizeof(PackParams) <= 4096, "kernel parameters");
 
-__global__ void __launch_bounds__(THREADS) k_adapter_reduce(const __grid_constant__ ReduceParams P)
+// A CTA takes a tile of 64 x 64 values through shared memory.
+template <class U>
+__global__ void __launch_bounds__(THREADS) k_adapter_pack(const __grid_constant__ PackParams P)
 {
-    const RedEntry &r = P.e[blockIdx.y];
-    const long long n0 = (long long)r.rank * P.width[0], n = n0 + (long long)r.rank * P.width[1];
-    for (long long i = (long long)blockIdx.x * THREADS + threadIdx.x; i < n; i += (long long)gridDim.x * THREADS) {
-        float *out = r.out[i < n0 ? 0 : 1];
-        if (!out) continue;
-        float *to = out + (i < n0 ? i : i - n0);
-        const float *p = P.part + r.slot + i;
-        float sum = 0.0f;
-#pragma unroll 4
-        for (int s = 0; s < r.splits; ++s) sum += __ldcg(p + s * n);
-        *to = P.accumulate ? *to + sum : sum;
+    __shared__ U t[AD_PACK_TILE][AD_PACK_TILE + 4 / sizeof(U)];
+    int which = 0;
+    for (int hi = P.n - 1; which < hi;) {
+        const int mid = (which + hi + 1) >> 1;
+        if (P.item[mid].block0 <= (int)blockIdx.x) which = mid; else hi = mid - 1;
+    }
+    const PackItem &it = P.item[which];
+    const int tile = (int)blockIdx.x - it.block0, across = (int)((it.cols + AD_PACK_TILE - 1) / AD_PACK_TILE);
+    const long long r0 = (long long)(tile / across) * AD_PACK_TILE, c0 = (long long)(tile % across) * AD_PACK_TILE;
+    const int x = threadIdx.x % AD_PACK_TILE, y = threadIdx.x / AD_PACK_TILE;
+    pdl_launch_dependents();
+    const int rows = (int)min(it.rows - r0, (long long)AD_PACK_TILE), cols = (int)min(it.cols - c0, (long long)AD_PACK_TILE);
+    const U *src = (const U *)it.src + (r0 + y) * it.cols + c0 + x;
+    U v[AD_PACK_TILE / 4];
+#pragma unroll
+    for (int i = 0; i < AD_PACK_TILE / 4; ++i) {
+        v[i] = y + 4 * i < rows && x < cols ? *src : U(0);
+        src += 4 * it.cols;
+    }
+#pragma unroll
+    for (int i = 0; i < AD_PACK_TILE / 4; ++i) t[y + 4 * i][x] = v[i];
+    __syncthreads();
+    // rows of the result run along c (as given) or along r (transposed); their padding is written too
+    const int o_rows = it.trans ? cols : rows;
+    const long long o_row = it.trans ? c0 : r0, o_col = it.trans ? r0 : c0;
+    if (o_col + x >= it.ld) return;
+    U *dst = (U *)it.dst + (o_row + y) * it.ld + o_col + x;
+#pragma unroll
+    for (int i = 0; i < AD_PACK_TILE / 4; ++i) {
+        const int a = y + 4 * i;
+        if (a < o_rows) *dst = it.trans ? t[x][a] : t[a][x];
+        dst += 4 * it.ld;
     }
 }
 

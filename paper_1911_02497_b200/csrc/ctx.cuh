@@ -60,7 +60,9 @@ struct condensa_ctx {
     size_t prof_used = 0;                   // pairs recorded since the last read
     std::vector<double> prof_ms;            // accumulated per name
     std::vector<int64_t> prof_cnt;
-    uint64_t op_smem_set = 0;               // adapter kernels whose shared memory limit has been raised on this device
+    struct ClusterFit { const void *f; int size, count; };
+    std::vector<ClusterFit> cluster_fit;    // clusters of a kernel that the device holds at once
+    std::vector<const void *> op_smem_set;  // adapter kernels whose shared memory limit has been raised on this device
     // workspace of the list operators and the adapters (partial sums); apart from the C-step's
     char *op_ws = nullptr;
     size_t op_ws_bytes = 0;

@@ -124,7 +124,7 @@ class Adapter(C.Structure):
 class AdapterBatch(C.Structure):
     """Mirror of ``condensa_adapter_batch``."""
     _fields_ = [("adapters", C.c_void_p), ("n_adapters", C.c_int32), ("n_requests", C.c_int32), ("request_rows", C.c_void_p),
-                ("request_adapter", C.c_void_p), ("k", C.c_int64), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+                ("request_adapter", C.c_void_p), ("rows", C.c_int64), ("k", C.c_int64), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 class KernelTime(C.Structure):
@@ -339,13 +339,23 @@ def adapter_table(a, b, scale, grad_a=None, grad_b=None) -> AdapterTable:
     return AdapterTable(entries, len(a), k, n, dtype)
 
 
+_INT64, _INT32 = np.dtype(np.int64), np.dtype(np.int32)
+
+
+def _host_array(x, dtype):
+    if type(x) is np.ndarray and x.dtype == dtype and x.flags.c_contiguous:
+        return x
+    return np.ascontiguousarray(x, dtype=dtype)
+
+
 def _rows_of(x, rows: int, width: int, dtype, name: str):
     """Address and row stride of a [rows, width] matrix whose rows are contiguous."""
     if x is None:
         return None, 0
-    if x.dtype != dtype or x.dim() != 2 or x.shape[0] != rows or x.shape[1] < width or (width > 1 and x.stride(1) != 1):
+    shape, (ld, step) = x.shape, (x.stride() if x.dim() == 2 else (0, 0))
+    if x.dtype != dtype or len(shape) != 2 or shape[0] != rows or shape[1] < width or (width > 1 and step != 1):
         raise ValueError("%s must be a [%d, %d] matrix of %s with contiguous rows" % (name, rows, width, dtype))
-    return x.data_ptr(), (x.stride(0) if rows > 1 else max(width, x.stride(0)))
+    return x.data_ptr(), (ld if rows > 1 else max(width, ld))
 
 
 def _kept_rows(h, rows: int):
@@ -489,20 +499,21 @@ class Context:
         self._check(self._lib.condensa_grad_norm(self._h, tab.entries, tab.T, mu, tab.grad_dtype, grad_scale, max_norm,
                                                  _addr(clip), _addr(norms), _stream_handle(stream)))
 
-    def _adapter_batch(self, tab: AdapterTable, request_rows, request_adapter):
-        """The batch, its number of rows, and the arrays that must live through the call."""
-        rows = np.ascontiguousarray(request_rows, dtype=np.int64)
-        which = np.ascontiguousarray(request_adapter, dtype=np.int32)
-        if rows.shape != which.shape or rows.ndim != 1:
+    def _adapter_batch(self, tab: AdapterTable, request_rows, request_adapter, rows: int):
+        """The batch, and the arrays that must live through the call."""
+        lengths = _host_array(request_rows, _INT64)
+        which = _host_array(request_adapter, _INT32)
+        if lengths.shape != which.shape or lengths.ndim != 1:
             raise ValueError("request_rows and request_adapter need one entry per request")
-        return AdapterBatch(tab.address, tab.count, rows.size, rows.ctypes.data, which.ctypes.data, tab.k, tab.n, tab.code, 0), \
-            int(rows.sum()), (rows, which)
+        return AdapterBatch(tab.address, tab.count, lengths.size, lengths.__array_interface__["data"][0],
+                            which.__array_interface__["data"][0], rows, tab.k, tab.n, tab.code, 0), (lengths, which)
 
     def adapter_forward(self, tab: AdapterTable, request_rows, request_adapter, x, y, h=None, stream=None):
         """``y += scale (x A^T) B^T`` row by row, each request with its adapter (-1: none). ``request_rows`` and ``request_adapter``:
         host arrays; ``x`` [rows, k] and ``y`` [rows, n] of the table's type; ``h`` [rows, max rank] float32 receives x A^T for
         :meth:`adapter_backward`, or None."""
-        batch, m, keep = self._adapter_batch(tab, request_rows, request_adapter)
+        m = x.shape[0]
+        batch, keep = self._adapter_batch(tab, request_rows, request_adapter, m)
         px, ldx = _rows_of(x, m, tab.k, tab.dtype, "x")
         py, ldy = _rows_of(y, m, tab.n, tab.dtype, "y")
         ph, ldh = _kept_rows(h, m)
@@ -511,7 +522,8 @@ class Context:
     def adapter_backward(self, tab: AdapterTable, request_rows, request_adapter, x, dy, h=None, dx=None, accumulate=False, stream=None):
         """Gradients of :meth:`adapter_forward`: ``dx`` (may be None) is added to, the table's ``grad_a`` and ``grad_b`` are
         overwritten, or added to with ``accumulate``."""
-        batch, m, keep = self._adapter_batch(tab, request_rows, request_adapter)
+        m = dy.shape[0]
+        batch, keep = self._adapter_batch(tab, request_rows, request_adapter, m)
         px, ldx = _rows_of(x, m, tab.k, tab.dtype, "x")
         pdy, lddy = _rows_of(dy, m, tab.n, tab.dtype, "dy")
         pdx, lddx = _rows_of(dx, m, tab.k, tab.dtype, "dx")

@@ -385,6 +385,7 @@ def test_refusals(ctx):
             ctx.adapter_forward(B.table(), B.rows, B.which, x, B.y)
     with pytest.raises(ValueError):
         ctx.adapter_forward(B.table(), [5], B.which, B.x, B.y)
+    refused(bad, rows=[3, 1])
     with pytest.raises((TypeError, ValueError)):
         cstep.adapter_table([B.a[0].float()], [B.b[0]], [1.0])
     with pytest.raises(ValueError):
