@@ -148,7 +148,7 @@ int launch_cluster(condensa_ctx *ctx, const AdapterKernel &k, dim3 grid, dim3 cl
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3((unsigned)k.threads);
     cfg.dynamicSmemBytes = (size_t)k.smem;
     cfg.stream = stream;
     cudaLaunchAttribute at[2];
@@ -181,7 +181,7 @@ int resident_clusters(condensa_ctx *ctx, const AdapterKernel &k, int n, int &cou
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)n);
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3((unsigned)k.threads);
     cfg.dynamicSmemBytes = (size_t)k.smem;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;

@@ -863,68 +863,115 @@ struct WgradParams {
 };
 static_assert(sizeof(WgradParams) <= 4096, "kernel parameters");
 
-template <class T, int RP>
-struct WgGeom {
-    static constexpr int E = AdType<T>::E, R = AD_WG_ROWS;
-    static constexpr int WC = (E == 2 && RP <= 64) ? 256 : 128;        // columns of a strip
-    static constexpr int NTW = WC / 64;                                // 8-column tiles of a warp
-    static constexpr int X_STRIDE = WC * E + 16, F_STRIDE = RP * 4 + 16, C_STRIDE = RP * 2 + 16;
-    static constexpr int PARTS = std::is_same<T, __nv_bfloat16>::value ? 3 : std::is_same<T, __half>::value ? 2 : 0;
+// What the two kernels below share: a CTA's place, its rows by number, its copies, and the sum over the cluster.
+struct WgPlace {
+    int sd, rank, r16, n_rows, n_runs, t0, nt, wide;
+    long long col0;
+    const AdapterRun *runs;
+    float *out;
+    float scale;
+};
+__device__ __forceinline__ WgPlace wg_place(const WgradParams &P, int wc)
+{
+    WgPlace w;
+    const int C = (int)cluster_size(), c_rank = (int)cluster_rank();
+    const WgEntry *entries = reinterpret_cast<const WgEntry *>(P.blob);
+    const WgEntry &ent = entries[blockIdx.y / C];
+    w.sd = (int)blockIdx.x >= P.strips0 ? 1 : 0;
+    w.runs = reinterpret_cast<const AdapterRun *>(entries + P.n_entries) + ent.run0;
+    w.out = ent.out[w.sd];
+    w.scale = w.sd ? ent.scale : 1.0f;
+    w.rank = ent.rank;
+    w.r16 = (ent.rank + 15) & ~15;
+    w.n_rows = ent.n_rows;
+    w.n_runs = ent.n_runs;
+    w.col0 = (long long)((int)blockIdx.x - (w.sd ? P.strips0 : 0)) * wc;
+    w.wide = (int)min((long long)wc, P.side[w.sd].width - w.col0);
+    const int tiles = (ent.n_rows + AD_WG_ROWS - 1) / AD_WG_ROWS;
+    w.t0 = (int)((long long)c_rank * tiles / C);
+    w.nt = (int)((long long)(c_rank + 1) * tiles / C) - w.t0;
+    return w;
+}
+// Rows of the CTA's tile i, -1 past the end, into slot i & 3 of `srow`.
+__device__ __forceinline__ void wg_number_rows(const WgPlace &w, int *srow, int i)
+{
+    if ((int)threadIdx.x < AD_WG_ROWS && i < w.nt) {
+        const int r = (w.t0 + i) * AD_WG_ROWS + (int)threadIdx.x;
+        srow[(i & 3) * AD_WG_ROWS + threadIdx.x] = r < w.n_rows ? adapter_row(w.runs, w.n_runs, r) : -1;
+    }
+}
+// `so` [rank][stride]: this CTA's sums. Each CTA of the cluster adds its share of the columns, in order of the ranks.
+__device__ __forceinline__ void wg_finish(const WgradParams &P, const WgPlace &w, float *so, int stride, int wc)
+{
+    const int C = (int)cluster_size(), c_rank = (int)cluster_rank(), rank = w.rank;
+    cluster_arrive();
+    cluster_wait();
+    const u32 so_u = smem_u32(so);
+    const int quads = rank * (wc / 4);
+    for (int u = (int)threadIdx.x < THREADS ? c_rank * THREADS + (int)threadIdx.x : quads; u < quads; u += C * THREADS) {
+        // dA is written along its rows, dB (whose rows are `rank` numbers) along the ranks
+        const int m = w.sd ? u % rank : u / (wc / 4), c = (w.sd ? u / rank : u % (wc / 4)) * 4;
+        if (c >= w.wide) continue;
+        const u32 at = so_u + (m * stride + c) * 4;
+        float4 x[AD_MAX_CLUSTER], v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int p = 0; p < AD_MAX_CLUSTER; ++p)
+            if (p < C) x[p] = ld_cluster(at, (u32)p);
+#pragma unroll
+        for (int p = 0; p < AD_MAX_CLUSTER; ++p)
+            if (p < C) { v.x += x[p].x; v.y += x[p].y; v.z += x[p].z; v.w += x[p].w; }
+        const float o[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < w.wide) {
+                float *to = w.out + (w.sd ? (w.col0 + c + e) * rank + m : (long long)m * P.side[0].width + w.col0 + c + e);
+                *to = P.accumulate ? *to + o[e] : o[e];
+            }
+    }
+    if (w.sd) pdl_wait();       // no CTA leaves ahead of the kernel before
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();             // peers may still read this CTA's sums until here
+}
+
+// ---- fp32: TF32 parts on the warp-level instruction, operands from shared memory
+template <int RP>
+struct WgGeom32 {
+    static constexpr int R = AD_WG_ROWS, WC = 128, NTW = WC / 64;      // columns of a strip; 8-column tiles of a warp
+    static constexpr int X_STRIDE = WC * 4 + 16, F_STRIDE = RP * 4 + 16;
     static constexpr int STAGE = R * (X_STRIDE + F_STRIDE);
-    static constexpr int CONV = PARTS * R * C_STRIDE;
     static constexpr int O_STRIDE = WC + 4;                            // floats: this CTA's sums, [rank][column]
-    static constexpr int ROWS = 4 * R * 4;                             // row numbers of four tiles
-    static constexpr int FIXED = CONV + ROWS + 64;
-    static constexpr int STAGES = FIXED + 3 * STAGE <= 113 * 1024 ? 3 : FIXED + 2 * STAGE <= 113 * 1024 ? 2 : FIXED + 3 * STAGE <= 227 * 1024 ? 3 : 2;
+    static constexpr int FIXED = 4 * R * 4;                            // row numbers of four tiles
+    static constexpr int STAGES = FIXED + 2 * STAGE <= 113 * 1024 ? 2 : FIXED + 3 * STAGE <= 227 * 1024 ? 3 : 2;
     static constexpr int SMEM = FIXED + STAGES * STAGE;
-    static_assert(SMEM <= 227 * 1024 && STAGE % 16 == 0 && CONV % 16 == 0, "shared memory");
+    static_assert(SMEM <= 227 * 1024 && STAGE % 16 == 0, "shared memory");
     static_assert(RP * O_STRIDE * 4 <= STAGES * STAGE, "the sums lie where the stages were");
 };
 
-template <class T, int RP, int V>
-__global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant__ WgradParams P)
+template <int RP, int V>
+__global__ void __launch_bounds__(THREADS) k_adapter_wgrad32(const __grid_constant__ WgradParams P)
 {
-    using G = WgGeom<T, RP>;
-    constexpr int E = G::E, KSTEP = AdType<T>::KSTEP, NTW = G::NTW, R = G::R;
-    constexpr bool HALF = std::is_same<T, __half>::value;
+    using G = WgGeom32<RP>;
+    constexpr int NTW = G::NTW, R = G::R;
     extern __shared__ __align__(128) char sm[];
-    int *srow = reinterpret_cast<int *>(sm + G::CONV);                 // [4][R]
-    float *smax = reinterpret_cast<float *>(sm + G::CONV + G::ROWS);
-    const u32 ring = smem_u32(sm + G::FIXED), conv = smem_u32(sm);
+    int *srow = reinterpret_cast<int *>(sm);
+    const u32 ring = smem_u32(sm + G::FIXED);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int C = (int)cluster_size(), c_rank = (int)cluster_rank();
-    const int sd = (int)blockIdx.x >= P.strips0 ? 1 : 0;
-    const WgSide &S = P.side[sd];
-    const WgEntry *entries = reinterpret_cast<const WgEntry *>(P.blob);
-    const WgEntry &ent = entries[blockIdx.y / C];
-    const AdapterRun *runs = reinterpret_cast<const AdapterRun *>(entries + P.n_entries) + ent.run0;
-    float *out = ent.out[sd];
-    if (!out) {                                                        // (all CTAs of the cluster leave)
+    const WgPlace w = wg_place(P, G::WC);
+    if (!w.out) {                                                      // (all CTAs of the cluster leave)
         pdl_wait();
         return;
     }
-    const int rank = ent.rank, r16 = (rank + 15) & ~15, n_rows = ent.n_rows, n_runs = ent.n_runs;
-    const long long col0 = (long long)((int)blockIdx.x - (sd ? P.strips0 : 0)) * G::WC;
-    const int wide = (int)min((long long)G::WC, S.width - col0);
-    const int tiles = (n_rows + R - 1) / R;
-    const int t0 = (int)((long long)c_rank * tiles / C), nt = (int)((long long)(c_rank + 1) * tiles / C) - t0;
-
-    auto number_rows = [&](int i) {                                    // rows of this CTA's tile i, -1 past the end
-        if (tid < R && i < nt) {
-            const int r = (t0 + i) * R + tid;
-            srow[(i & 3) * R + tid] = r < n_rows ? adapter_row(runs, n_runs, r) : -1;
-        }
-    };
-    constexpr int XU = G::WC * E / 16, XN = R * XU / THREADS, FU = RP / 4, FN = R * FU / THREADS;
+    const WgSide &S = P.side[w.sd];
+    constexpr int XU = G::WC / 4, XN = R * XU / THREADS, FU = RP / 4, FN = R * FU / THREADS;
     const int xq = (tid % XU) * 16, xr = tid / XU, fq = (tid % FU) * 16, fr = tid / FU;
-    const int xn = min(max(wide * E - xq, 0), 16), fn = min(max(rank * 4 - fq, 0), 16);
+    const int xn = min(max(w.wide * 4 - xq, 0), 16), fn = min(max(w.rank * 4 - fq, 0), 16);
     const char *act = (const char *)S.act, *coef = (const char *)S.coef;
-    const char *xbase = act + col0 * E + xq;
-    const long long ldx = S.ld_act * E, ldf = S.ld_coef * 4;
-    const int vec_act = S.vec_act, vec_coef = S.vec_coef;             // (the latter at most 8: copied 8 bytes at a time)
-
+    const char *xbase = act + w.col0 * 4 + xq;
+    const long long ldx = S.ld_act * 4, ldf = S.ld_coef * 4;
+    const int vec_act = S.vec_act, vec_coef = S.vec_coef;
     auto issue = [&](int i) {
-        if (i >= nt) return;
+        if (i >= w.nt) return;
         const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE, sf = st + R * G::X_STRIDE;
         const int *rows = srow + (i & 3) * R;
 #pragma unroll
@@ -932,7 +979,7 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant
             const int r = xr + THREADS / XU * j, row = rows[r];
             copy_unit<V>(st + r * G::X_STRIDE + xq, xbase + row * ldx, act, row >= 0 ? xn : 0, vec_act);
         }
-        if (fq < r16 * 4) {
+        if (fq < w.r16 * 4) {
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 const int r = fr + THREADS / FU * j, row = rows[r];
@@ -940,7 +987,6 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant
             }
         }
     };
-
     float acc[RP / 16][NTW][4];
 #pragma unroll
     for (int m = 0; m < RP / 16; ++m)
@@ -948,13 +994,12 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant
         for (int n = 0; n < NTW; ++n)
 #pragma unroll
             for (int q = 0; q < 4; ++q) acc[m][n][q] = 0.0f;
-    float top = 0.0f, unit = 1.1754943508222875e-38f;        // binary16: largest coefficient so far, the power of two that goes with it
 #pragma unroll
-    for (int i = 0; i < G::STAGES; ++i) number_rows(i);
+    for (int i = 0; i < G::STAGES; ++i) wg_number_rows(w, srow, i);
     __syncthreads();
-    if (sd == 0) pdl_wait();                                           // u is the kernel before's; x, dy and h are not
+    if (w.sd == 0) pdl_wait();                                         // u is the kernel before's; x, dy and h are not
 #pragma unroll 1
-    for (int i = 1 - G::STAGES; i < nt; ++i) {
+    for (int i = 1 - G::STAGES; i < w.nt; ++i) {
         if (i >= 0) {
             cp_wait<G::STAGES - 2>();
             __syncthreads();
@@ -962,86 +1007,29 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant
         issue(i + G::STAGES - 1);
         cp_commit();
         if (i < 0) continue;
-        number_rows(i + G::STAGES);
-        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE;
-        const char *sf = sm + G::FIXED + (i % G::STAGES) * G::STAGE + R * G::X_STRIDE;
-        if constexpr (E == 2) {
-            float4 v[FN];
-            float inv = 1.0f, most = 0.0f;
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                v[j] = fq < r16 * 4 ? *reinterpret_cast<const float4 *>(sf + (fr + THREADS / FU * j) * G::F_STRIDE + fq) : make_float4(0.f, 0.f, 0.f, 0.f);
-                if (HALF) most = fmaxf(most, fmaxf(fmaxf(fabsf(v[j].x), fabsf(v[j].y)), fmaxf(fabsf(v[j].z), fabsf(v[j].w))));
-            }
-            if constexpr (HALF) {
-#pragma unroll
-                for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-                if (lane == 0) smax[warp] = most;
-                __syncthreads();
-#pragma unroll
-                for (int w = 0; w < WARPS; ++w) most = fmaxf(most, smax[w]);
-                if (most > top) {
-                    top = most;
-                    const float next = pow2_above(top), less = unit * pow2_inverse(next);        // at most 1
-                    unit = next;
-#pragma unroll
-                    for (int m = 0; m < RP / 16; ++m)
-#pragma unroll
-                        for (int n = 0; n < NTW; ++n)
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) acc[m][n][q] *= less;
-                }
-                inv = pow2_inverse(unit);
-            }
-            if (fq < r16 * 4) {
-#pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    const float x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-                    u16 p[4][G::PARTS];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) split16<T, G::PARTS>(HALF ? x[e] * inv : x[e], p[e]);
-#pragma unroll
-                    for (int s = 0; s < G::PARTS; ++s)
-                        *reinterpret_cast<uint2 *>(sm + (s * R + fr + THREADS / FU * j) * G::C_STRIDE + fq / 2) =
-                            make_uint2((u32)p[0][s] | ((u32)p[1][s] << 16), (u32)p[2][s] | ((u32)p[3][s] << 16));
-                }
-            }
-            __syncthreads();
-        }
+        wg_number_rows(w, srow, i + G::STAGES);
+        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE, sf = st + R * G::X_STRIDE;
         // 32 rows at a time, their sums apart from the others: the matrix instruction truncates
-        constexpr int HK = 32 / KSTEP;
+        constexpr int HK = 32 / 8;
 #pragma unroll 1
         for (int k0 = 0; k0 < R; k0 += 32) {
-            FragB<T> b[HK][NTW / 2][2];
+            FragB<float> b[HK][NTW / 2][2];
 #pragma unroll
             for (int k = 0; k < HK; ++k)
 #pragma unroll
-                for (int n = 0; n < NTW / 2; ++n)
-                    load_b2_t(b[k][n], st + (k0 + k * KSTEP) * G::X_STRIDE + (warp * NTW * 8 + n * 16) * E, G::X_STRIDE, lane);
+                for (int n = 0; n < NTW / 2; ++n) load_b2_t(b[k][n], st + (k0 + k * 8) * G::X_STRIDE + (warp * NTW * 8 + n * 16) * 4, G::X_STRIDE, lane);
 #pragma unroll
             for (int m = 0; m < RP / 16; ++m) {
-                if (m * 16 >= r16) break;
+                if (m * 16 >= w.r16) break;
                 float d[NTW][4];
 #pragma unroll
-                for (int n = 0; n < NTW; ++n)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) d[n][q] = 0.0f;
-#pragma unroll
                 for (int k = 0; k < HK; ++k) {
-                    const int row = k0 + k * KSTEP;
-                    if constexpr (E == 2) {
+                    FragA<float> a;
+                    load_a_t(a, sf + (k0 + k * 8) * G::F_STRIDE + m * 64, G::F_STRIDE, lane);
 #pragma unroll
-                        for (int s = G::PARTS - 1; s >= 0; --s) {
-                            FragA<T> a;
-                            load_a_t(a, conv + (s * R + row) * G::C_STRIDE + m * 32, G::C_STRIDE, lane);
-#pragma unroll
-                            for (int n = 0; n < NTW; ++n) mma_step(d[n], a, b[k][n >> 1][n & 1]);
-                        }
-                    } else {
-                        FragA<T> a;
-                        load_a_t(a, smem_u32(sf) + row * G::F_STRIDE + m * 64, G::F_STRIDE, lane);
-#pragma unroll
-                        for (int n = 0; n < NTW; ++n) mma_step(d[n], a, b[k][n >> 1][n & 1]);
+                    for (int n = 0; n < NTW; ++n) {
+                        if (k == 0) mma_first(d[n], a, b[k][n >> 1][n & 1]);
+                        else mma_step(d[n], a, b[k][n >> 1][n & 1]);
                     }
                 }
 #pragma unroll
@@ -1051,50 +1039,330 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad(const __grid_constant
             }
         }
     }
-    // ---- this CTA's sums into shared memory, then the cluster's, each CTA adding its share of the columns
     cp_wait<0>();
     __syncthreads();
     float *so = reinterpret_cast<float *>(sm + G::FIXED);
-    const float factor = (sd ? ent.scale : 1.0f) * (HALF ? unit : 1.0f);
     const int g = lane >> 2, t4 = lane & 3;
 #pragma unroll
     for (int m = 0; m < RP / 16; ++m) {
-        if (m * 16 >= r16) break;
+        if (m * 16 >= w.r16) break;
 #pragma unroll
         for (int n = 0; n < NTW; ++n)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 *reinterpret_cast<float2 *>(so + (m * 16 + g + 8 * h) * G::O_STRIDE + warp * NTW * 8 + n * 8 + 2 * t4) =
-                    make_float2(factor * acc[m][n][2 * h], factor * acc[m][n][2 * h + 1]);
+                    make_float2(w.scale * acc[m][n][2 * h], w.scale * acc[m][n][2 * h + 1]);
     }
-    cluster_arrive();
-    cluster_wait();
-    const u32 so_u = smem_u32(so);
-    const int quads = rank * (G::WC / 4);
-    for (int u = c_rank * THREADS + tid; u < quads; u += C * THREADS) {
-        // dA is written along its rows, dB (whose rows are `rank` numbers) along the ranks
-        const int m = sd ? u % rank : u / (G::WC / 4), c = (sd ? u / rank : u % (G::WC / 4)) * 4;
-        if (c >= wide) continue;
-        const u32 at = so_u + (m * G::O_STRIDE + c) * 4;
-        float4 x[AD_MAX_CLUSTER], v = make_float4(0.f, 0.f, 0.f, 0.f);
+    wg_finish(P, w, so, G::O_STRIDE, G::WC);
+}
+
+// ---- 16-bit types on tcgen05
+// Of 64 rows at a time, the products D[column][rank] = sum over rows of act[row][column] * coef[row][rank] have the rows
+// as their depth, and both operands lie in shared memory with the depth as the outer index (MN-major): a strip of 256
+// activation columns is two operands A of 128 columns, the coefficients' 16-bit parts are operands B of up to 128
+// ranks. Eight warps copy, convert the coefficients and take finished tiles from tensor memory; a ninth issues the
+// products of a tile (4 depth steps x 2 operands x 2 or 3 parts, smallest part first). They run while the next tile is
+// converted and the tile before is added to fp32 registers, with rounding (the tensor core's own sums are short: 64
+// rows). Two accumulators in tensor memory take turns. No warp waits for all others but for the row numbers.
+__device__ __forceinline__ void mbar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory"); }
+// Waits for the phase of parity `ph`, at most about a second; false when it did not come.
+__device__ __forceinline__ bool mbar_wait(u32 bar, u32 ph)
+{
+    for (int i = 0; i < (1 << 20); ++i) {
+        u32 done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(ph), "r"(1000u) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+template <class T>
+__device__ __forceinline__ constexpr u32 umma_idesc(int n)         // fp32 sums; A and B of type T, both MN-major; M = 128
+{
+    return (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | (1u << 15) | (1u << 16) | ((u32)(n >> 3) << 17) | (8u << 24);
+}
+// Shared memory descriptor: start, byte offset of the next group along M or N, of the next eight depth rows, swizzle
+// (2: 128 bytes, 4: 64, 6: 32).
+__device__ __forceinline__ u64 umma_desc(u32 addr, u32 lbo, u32 sbo, u32 swizzle)
+{
+    return (u64)((addr & 0x3FFFFu) >> 4) | ((u64)(lbo >> 4) << 16) | ((u64)(sbo >> 4) << 32) | (1ull << 46) | ((u64)swizzle << 61);
+}
+__device__ __forceinline__ void umma_f16(u32 d, u64 a, u64 b, u32 idesc, u32 add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(u32 addr, float (&v)[16])
+{
+    u32 r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-        for (int p = 0; p < AD_MAX_CLUSTER; ++p)
-            if (p < C) x[p] = ld_cluster(at, (u32)p);
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+template <int N> __device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "n"(N) : "memory"); }
+template <int N> __device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(N) : "memory"); }
+
+// 16-bit parts of two fp32 values, packed; a value that is not finite yields parts that are no numbers.
+__device__ __forceinline__ void split_pair(float &x, float &y, u32 &p, __nv_bfloat16)
+{
+    const __nv_bfloat162 q = __floats2bfloat162_rn(x, y);
+    p = *reinterpret_cast<const u32 *>(&q);
+    x -= __uint_as_float(p << 16);
+    y -= __uint_as_float(p & 0xFFFF0000u);
+}
+__device__ __forceinline__ void split_pair(float &x, float &y, u32 &p, __half)
+{
+    const __half2 q = __floats2half2_rn(x, y);
+    p = *reinterpret_cast<const u32 *>(&q);
+    const float2 f = __half22float2(q);
+    x -= f.x;
+    y -= f.y;
+}
+
+template <class T, int RP>
+struct WgGeom16 {
+    static constexpr int R = AD_WG_ROWS, WC = 256;                     // rows of a tile, columns of a strip
+    static constexpr int PARTS = std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
+    static constexpr int STAGE = R * WC * 2;                           // four blocks of 64 columns: [row][128 bytes], swizzled
+    static constexpr int C_ROW = RP >= 64 ? 128 : RP * 2;              // bytes of a row of B (more than 64 ranks: two blocks)
+    static constexpr int C_SWIZZLE = RP >= 64 ? 2 : RP == 32 ? 4 : 6;
+    static constexpr int C_PART = R * RP * 2;
+    static constexpr int CONV = PARTS * C_PART;                        // one of two
+    static constexpr int O_STRIDE = WC + 4;                            // floats: this CTA's sums, [rank][column]
+    static constexpr int ROWS = 4 * R * 4;
+    static constexpr int FIXED = 2 * CONV + ROWS + 128;                // (the swizzled parts first)
+    static constexpr int PAD = 1024;                                   // swizzle patterns start at multiples of 1024 bytes
+    static constexpr int HALF_SM = 113 * 1024, WHOLE_SM = 227 * 1024;
+    static constexpr int stages()
+    {
+        for (int s = 3; s >= 2; --s)
+            if (RP <= 64 && PAD + FIXED + s * STAGE <= HALF_SM) return s;
+        for (int s = 4; s >= 2; --s)
+            if (PAD + FIXED + s * STAGE <= WHOLE_SM) return s;
+        return 2;
+    }
+    static constexpr int STAGES = stages();
+    static constexpr int SMEM = PAD + FIXED + STAGES * STAGE;
+    static constexpr int TMEM = 4 * RP;                                // columns: two accumulators of two blocks of RP
+    static constexpr int CTAS = SMEM <= HALF_SM && TMEM <= 256 ? 2 : 1;
+    static constexpr int BLOCK = THREADS + 32;
+    static_assert(SMEM <= WHOLE_SM && STAGE % 1024 == 0 && C_PART % 1024 == 0, "shared memory");
+    static_assert(STAGES <= 3 || ROWS >= 4 * R * 4, "row numbers of four tiles");
+    static_assert(RP * O_STRIDE * 4 <= STAGES * STAGE + 2 * CONV, "the sums lie where the stages and the parts were");
+};
+
+template <class T, int RP, int V>
+__global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter_wgrad16(const __grid_constant__ WgradParams P)
+{
+    using G = WgGeom16<T, RP>;
+    constexpr int R = G::R, PARTS = G::PARTS;
+    constexpr bool HALF = std::is_same<T, __half>::value;
+    extern __shared__ char sm_raw[];
+    char *sm = sm_raw + ((1024u - (smem_u32(sm_raw) & 1023u)) & 1023u);
+    char *stages = sm, *conv = sm + G::STAGES * G::STAGE;              // [2][PARTS][row][C_ROW]
+    int *srow = reinterpret_cast<int *>(conv + 2 * G::CONV);           // [4][R]
+    u64 *bars = reinterpret_cast<u64 *>(reinterpret_cast<char *>(srow) + G::ROWS);
+    u32 *s_tmem = reinterpret_cast<u32 *>(bars + 2);
+    float *smax = reinterpret_cast<float *>(s_tmem + 4);
+    const u32 ring = smem_u32(stages), conv_u = smem_u32(conv), bar = smem_u32(bars);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const WgPlace w = wg_place(P, G::WC);
+    if (!w.out) {                                                      // (all CTAs of the cluster leave)
+        pdl_wait();
+        return;
+    }
+    const WgSide &S = P.side[w.sd];
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(s_tmem)), "r"((u32)G::TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (tid == 0) {
+        mbar_init(bar, 1);
+        mbar_init(bar + 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
 #pragma unroll
-        for (int p = 0; p < AD_MAX_CLUSTER; ++p)
-            if (p < C) { v.x += x[p].x; v.y += x[p].y; v.z += x[p].z; v.w += x[p].w; }
-        const float w[4] = {v.x, v.y, v.z, v.w};
+    for (int i = 0; i < G::STAGES; ++i) wg_number_rows(w, srow, i);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const u32 tmem = *s_tmem;
+
+    if (warp == WARPS) {                         // ---- the warp that issues the products
+        const u32 idesc = umma_idesc<T>(w.r16);
+        const u64 b0 = umma_desc(conv_u, R * 128, 8 * G::C_ROW, G::C_SWIZZLE);
+        int stage = 0;
+#pragma unroll 1
+        for (int i = 0; i < w.nt; ++i) {
+            bar_sync<G::BLOCK>(1 + (i & 1));
+            if (lane == 0) {
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const u64 a0 = umma_desc(ring + (u32)stage * G::STAGE, R * 128, 1024, 2);
+                const u64 bi = b0 + ((u32)(i & 1) * G::CONV >> 4);
+                const u32 d = tmem + (u32)(i & 1) * (2 * RP);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (c + e < wide) {
-                float *to = out + (sd ? (col0 + c + e) * rank + m : (long long)m * S.width + col0 + c + e);
-                *to = P.accumulate ? *to + w[e] : w[e];
+                for (int b = 0; b < 2; ++b) {
+                    if (b * 128 >= w.wide) break;
+#pragma unroll
+                    for (int s = PARTS - 1; s >= 0; --s)
+#pragma unroll
+                        for (int k = 0; k < R / 16; ++k)
+                            umma_f16(d + b * RP, a0 + ((b * (2 * R * 128) + k * 2048) >> 4), bi + ((s * G::C_PART + k * 16 * G::C_ROW) >> 4), idesc,
+                                     s < PARTS - 1 || k > 0);
+                }
+                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar + 8 * (i & 1)) : "memory");
             }
+            __syncwarp();
+            if (++stage == G::STAGES) stage = 0;
+        }
+        __syncthreads();                         // (the workers' last products are in their registers)
+        __syncthreads();                         // (their sums are in shared memory)
+        wg_finish(P, w, reinterpret_cast<float *>(stages), G::O_STRIDE, G::WC);
+        return;
     }
-    if (sd) pdl_wait();         // no CTA leaves ahead of the kernel before
-    __syncwarp();
-    cluster_arrive();
-    cluster_wait();             // peers may still read this CTA's sums until here
+
+    // ---- the workers
+    constexpr int XU = G::WC * 2 / 16, XN = R * XU / THREADS, FU = RP / 4, FN = R * FU / THREADS;
+    const int xc = tid % XU, xr = tid / XU, fq = (tid % FU) * 4, fr = tid / FU;          // fq: first of four ranks
+    const int xn = min(max(w.wide * 2 - xc * 16, 0), 16);
+    const char *act = (const char *)S.act;
+    const char *xbase = act + w.col0 * 2 + xc * 16;
+    const float *coef = S.coef + fq;
+    const long long ldx = S.ld_act * 2, ldf = S.ld_coef;
+    const int vec_act = S.vec_act;
+    const bool has_f = fq < w.r16, whole_f = fq + 4 <= w.rank, vec_f = S.vec_coef == 16;
+    const u32 x_to = (xc >> 3) * (R * 128) + xr * 128 + (((xc & 7) ^ (xr & 7)) << 4);     // (rows of a thread are 8 apart: one swizzle)
+    static_assert(THREADS / XU == 8, "rows of a thread");
+    auto issue = [&](int i) {                    // activations of tile i
+        if (i >= w.nt) return;
+        const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE + x_to;
+        const int *rows = srow + (i & 3) * R + xr;
+#pragma unroll
+        for (int j = 0; j < XN; ++j) {           // (rows that do not exist become zero: they are summed over)
+            const int row = rows[8 * j];
+            copy_unit<V>(st + j * 1024, xbase + row * ldx, act, row >= 0 ? xn : 0, vec_act);
+        }
+    };
+    float4 v[FN];
+    auto load_coef = [&](int i) {                // coefficients of tile i
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i >= w.nt || !has_f) continue;
+            const int row = srow[(i & 3) * R + fr + THREADS / FU * j];
+            if (row < 0) continue;
+            const float *p = coef + row * ldf;
+            if (vec_f && whole_f) v[j] = *reinterpret_cast<const float4 *>(p);
+            else {
+                if (fq < w.rank) v[j].x = p[0];
+                if (fq + 1 < w.rank) v[j].y = p[1];
+                if (fq + 2 < w.rank) v[j].z = p[2];
+                if (fq + 3 < w.rank) v[j].w = p[3];
+            }
+        }
+    };
+    // four ranks are 8 bytes: block of 64 ranks, 16-byte unit (moved by the swizzle), half of it
+    u32 c_to[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int r = fr + THREADS / FU * j, by = fq * 2, blk = by >> 7, un = (by & 127) >> 4;
+        const int sw = RP >= 64 ? un ^ (r & 7) : RP == 32 ? un ^ ((r >> 1) & 3) : un ^ ((r >> 2) & 1);
+        c_to[j] = blk * (R * 128) + r * G::C_ROW + (sw << 4) + (by & 8);
+    }
+    // this thread's column of the strip, `rank` sums of it
+    float acc[RP];
+#pragma unroll
+    for (int m = 0; m < RP; ++m) acc[m] = 0.0f;
+    bool fine = true;
+    float unit = 1.0f, unit_before = 1.0f;       // binary16: the power of two that a tile's coefficients are divided by
+    auto collect = [&](int i, float f) {         // tile i's sums from tensor memory
+        const u32 at = tmem + (u32)(i & 1) * (2 * RP) + (u32)(warp >> 2) * RP + ((u32)(warp & 3) << 21);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < RP / 16; ++q) {
+            if (q && q * 16 >= w.r16) break;
+            float t[16];
+            tmem_ld16(at + q * 16, t);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[q * 16 + e] = HALF ? fmaf(f, t[e], acc[q * 16 + e]) : acc[q * 16 + e] + t[e];
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    };
+    if (w.sd == 0) pdl_wait();                   // u is the kernel before's; x, dy and h are not
+    load_coef(0);
+#pragma unroll 1
+    for (int i = 0; i < G::STAGES - 1; ++i) {
+        issue(i);
+        cp_commit();
+    }
+#pragma unroll 1
+    for (int i = 0; i < w.nt; ++i) {
+        float inv = 1.0f;
+        if constexpr (HALF) {
+            float most = 0.0f;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) most = fmaxf(most, fmaxf(fmaxf(fabsf(v[j].x), fabsf(v[j].y)), fmaxf(fabsf(v[j].z), fabsf(v[j].w))));
+#pragma unroll
+            for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+            if (lane == 0) smax[(i & 1) * WARPS + warp] = most;
+            bar_sync<THREADS>(3);
+#pragma unroll
+            for (int q = 0; q < WARPS; ++q) most = fmaxf(most, smax[(i & 1) * WARPS + q]);
+            unit_before = unit;
+            unit = pow2_above(most);
+            inv = pow2_inverse(unit);
+        }
+        char *cv = conv + (i & 1) * G::CONV;
+        if (has_f) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                float x0 = HALF ? v[j].x * inv : v[j].x, x1 = HALF ? v[j].y * inv : v[j].y, x2 = HALF ? v[j].z * inv : v[j].z, x3 = HALF ? v[j].w * inv : v[j].w;
+#pragma unroll
+                for (int s = 0; s < PARTS; ++s) {
+                    uint2 p;
+                    split_pair(x0, x1, p.x, T());
+                    split_pair(x2, x3, p.y, T());
+                    *reinterpret_cast<uint2 *>(cv + s * G::C_PART + c_to[j]) = p;
+                }
+            }
+        }
+        cp_wait<G::STAGES - 2>();                                      // this thread's share of tile i is there
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the tensor core reads it)
+        bar_arrive<G::BLOCK>(1 + (i & 1));
+        load_coef(i + 1);
+        // the tile before is complete: its buffers are free for the next copies, its sums can be taken
+        if (i > 0) fine = mbar_wait(bar + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1) && fine;
+        issue(i + G::STAGES - 1);
+        cp_commit();
+        wg_number_rows(w, srow, i + G::STAGES);                        // (nobody reads this slot now; the next pass does)
+        bar_sync<THREADS>(3);
+        if (i > 0) collect(i - 1, unit_before);
+    }
+    if (w.nt > 0) {
+        fine = mbar_wait(bar + 8 * ((w.nt - 1) & 1), ((w.nt - 1) >> 1) & 1) && fine;
+        collect(w.nt - 1, unit);
+    }
+    cp_wait<0>();
+    __syncthreads();
+    // tensor memory goes back before anything waits for another CTA
+    if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"((u32)G::TMEM) : "memory");
+    }
+    float *so = reinterpret_cast<float *>(stages);
+    const int col = (warp >> 2) * 128 + (warp & 3) * 32 + lane;
+    const float factor = fine ? w.scale : __uint_as_float(0x7FC00000u);         // a product that never came must not go unseen
+#pragma unroll
+    for (int m = 0; m < RP; ++m) {
+        if (m % 16 == 0 && m && m >= w.r16) break;
+        so[m * G::O_STRIDE + col] = factor * acc[m];
+    }
+    __syncthreads();
+    wg_finish(P, w, so, G::O_STRIDE, G::WC);
 }
 
 // A and B laid out anew ahead of the row kernel, rows padded with zeros to 16 bytes: for the backward pass transposed (it

@@ -8,7 +8,7 @@ template <class T, int TM, int RP, int V>
 AdapterKernel row_instance()
 {
     using G = AdGeom<T, TM, RP>;
-    return {(const void *)k_adapter<T, TM, RP, V>, G::SMEM, G::CTAS};
+    return {(const void *)k_adapter<T, TM, RP, V>, G::SMEM, G::CTAS, THREADS};
 }
 
 template <class T, int TM, int V>
@@ -36,9 +36,15 @@ AdapterKernel row_kernel(const RowShape &s)
 template <class T, int RP, int V>
 AdapterKernel wgrad_instance(int &strip)
 {
-    using G = WgGeom<T, RP>;
-    strip = G::WC;
-    return {(const void *)k_adapter_wgrad<T, RP, V>, G::SMEM, G::SMEM <= 113 * 1024 ? 2 : 1};
+    if constexpr (sizeof(T) == 4) {
+        using G = WgGeom32<RP>;
+        strip = G::WC;
+        return {(const void *)k_adapter_wgrad32<RP, V>, G::SMEM, G::SMEM <= 113 * 1024 ? 2 : 1, THREADS};
+    } else {
+        using G = WgGeom16<T, RP>;
+        strip = G::WC;
+        return {(const void *)k_adapter_wgrad16<T, RP, V>, G::SMEM, G::CTAS, G::BLOCK};
+    }
 }
 
 template <class T, int V>

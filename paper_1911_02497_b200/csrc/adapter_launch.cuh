@@ -8,7 +8,7 @@ namespace cs {
 // A kernel instance: its function, shared memory, and how many CTAs an SM holds.
 struct AdapterKernel {
     const void *f;
-    int smem, per_sm;
+    int smem, per_sm, threads;
 };
 
 // Shape of the row kernel's instances: by tile height, largest rank, access width.
