@@ -406,14 +406,20 @@ int run_wgrad(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &ro
         const AdapterKernel kernel = wgrad_kernel_of(b->dtype, rank, vec, strip);
         P.strips0 = (int)((b->k + strip - 1) / strip);
         const int strips = P.strips0 + (int)((b->n + strip - 1) / strip);
-        // CTAs that share an adapter's rows: the number whose rounds of the SMs take least, a CTA's time going with its
-        // tiles and some fixed work
+        // CTAs that share an adapter's rows: what a simple account makes least. A CTA's time is its tiles and about four
+        // tiles' worth of fixed work; two on an SM take 1.3 times as long as one; CTAs past the first round follow as places
+        // free up. Measured on 4 adapters of 2048 rows, 32 strips: 1: 79, 2: 53, 3: 49, 4: 49, 8: 63 us; on 6 of 430 rows,
+        // 30 strips: 1: 53, 2: 45, 3: 50, 4: 63 us.
         int cluster = 1;
         double best = 0.0;
         for (int n = 1; n <= std::min(AD_MAX_CLUSTER, most_tiles); ++n) {
-            const long long slots = (long long)ctx->num_sms * kernel.per_sm / n;
-            const double t = (double)(((long long)strips * P.n_entries + slots - 1) / slots) * ((double)((most_tiles + n - 1) / n) + 2.0);
-            if (n == 1 || t < best) {
+            int fit = 0;
+            int rc = resident_clusters(ctx, kernel, n, fit);
+            if (rc) return rc;
+            const long long ctas = (long long)strips * P.n_entries * n;
+            const double rounds = std::max(1.0, (double)ctas / ((double)fit * n));
+            const double t = rounds * ((double)((most_tiles + n - 1) / n) + 4.0) * (ctas > ctx->num_sms ? 1.3 : 1.0);
+            if (n == 1 || t < 0.999 * best) {
                 best = t;
                 cluster = n;
             }

@@ -892,12 +892,20 @@ __device__ __forceinline__ WgPlace wg_place(const WgradParams &P, int wc)
     w.nt = (int)((long long)(c_rank + 1) * tiles / C) - w.t0;
     return w;
 }
-// Rows of the CTA's tile i, -1 past the end, into slot i & 3 of `srow`.
-__device__ __forceinline__ void wg_number_rows(const WgPlace &w, int *srow, int i)
+// Rows of the CTA's tile i, -1 past the end, into slot i & 7 of `srow`. By threads t, t + 32, ... of a warp, or the first 64.
+__device__ __forceinline__ void wg_number_rows(const WgPlace &w, int *srow, int i, int t, int step)
 {
-    if ((int)threadIdx.x < AD_WG_ROWS && i < w.nt) {
-        const int r = (w.t0 + i) * AD_WG_ROWS + (int)threadIdx.x;
-        srow[(i & 3) * AD_WG_ROWS + threadIdx.x] = r < w.n_rows ? adapter_row(w.runs, w.n_runs, r) : -1;
+    if (i >= w.nt) return;
+    if (w.n_runs == 1) {
+        for (; t < AD_WG_ROWS; t += step) {
+            const int r = (w.t0 + i) * AD_WG_ROWS + t;
+            srow[(i & 7) * AD_WG_ROWS + t] = r < w.n_rows ? w.runs[0].first + r : -1;
+        }
+        return;
+    }
+    for (; t < AD_WG_ROWS; t += step) {
+        const int r = (w.t0 + i) * AD_WG_ROWS + t;
+        srow[(i & 7) * AD_WG_ROWS + t] = r < w.n_rows ? adapter_row(w.runs, w.n_runs, r) : -1;
     }
 }
 // `so` [rank][stride]: this CTA's sums. Each CTA of the cluster adds its share of the columns, in order of the ranks.
@@ -941,7 +949,7 @@ struct WgGeom32 {
     static constexpr int X_STRIDE = WC * 4 + 16, F_STRIDE = RP * 4 + 16;
     static constexpr int STAGE = R * (X_STRIDE + F_STRIDE);
     static constexpr int O_STRIDE = WC + 4;                            // floats: this CTA's sums, [rank][column]
-    static constexpr int FIXED = 4 * R * 4;                            // row numbers of four tiles
+    static constexpr int FIXED = 8 * R * 4;                            // row numbers of eight tiles
     static constexpr int STAGES = FIXED + 2 * STAGE <= 113 * 1024 ? 2 : FIXED + 3 * STAGE <= 227 * 1024 ? 3 : 2;
     static constexpr int SMEM = FIXED + STAGES * STAGE;
     static_assert(SMEM <= 227 * 1024 && STAGE % 16 == 0, "shared memory");
@@ -973,7 +981,7 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad32(const __grid_consta
     auto issue = [&](int i) {
         if (i >= w.nt) return;
         const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE, sf = st + R * G::X_STRIDE;
-        const int *rows = srow + (i & 3) * R;
+        const int *rows = srow + (i & 7) * R;
 #pragma unroll
         for (int j = 0; j < XN; ++j) {           // (rows that do not exist become zero: they are summed over)
             const int r = xr + THREADS / XU * j, row = rows[r];
@@ -995,7 +1003,7 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad32(const __grid_consta
 #pragma unroll
             for (int q = 0; q < 4; ++q) acc[m][n][q] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < G::STAGES; ++i) wg_number_rows(w, srow, i);
+    for (int i = 0; i < G::STAGES; ++i) wg_number_rows(w, srow, i, tid, THREADS);
     __syncthreads();
     if (w.sd == 0) pdl_wait();                                         // u is the kernel before's; x, dy and h are not
 #pragma unroll 1
@@ -1007,7 +1015,7 @@ __global__ void __launch_bounds__(THREADS) k_adapter_wgrad32(const __grid_consta
         issue(i + G::STAGES - 1);
         cp_commit();
         if (i < 0) continue;
-        wg_number_rows(w, srow, i + G::STAGES);
+        wg_number_rows(w, srow, i + G::STAGES, tid, THREADS);
         const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE, sf = st + R * G::X_STRIDE;
         // 32 rows at a time, their sums apart from the others: the matrix instruction truncates
         constexpr int HK = 32 / 8;
@@ -1092,17 +1100,22 @@ __device__ __forceinline__ void umma_f16(u32 d, u64 a, u64 b, u32 idesc, u32 add
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
 }
+// 16 columns of this warp's lanes of tensor memory; complete only behind tmem_ld_wait().
 __device__ __forceinline__ void tmem_ld16(u32 addr, float (&v)[16])
 {
-    u32 r[16];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+                   "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]) : "r"(addr));
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait(float (&v)[N][16])
+{
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+    for (int s = 0; s < N; ++s)          // (no use of the values may move ahead of the wait)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) asm volatile("" : "+f"(v[s][i]));
 }
-
 template <int N> __device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "n"(N) : "memory"); }
 template <int N> __device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(N) : "memory"); }
 
@@ -1128,12 +1141,15 @@ struct WgGeom16 {
     static constexpr int R = AD_WG_ROWS, WC = 256;                     // rows of a tile, columns of a strip
     static constexpr int PARTS = std::is_same<T, __nv_bfloat16>::value ? 3 : 2;
     static constexpr int STAGE = R * WC * 2;                           // four blocks of 64 columns: [row][128 bytes], swizzled
-    static constexpr int C_ROW = RP >= 64 ? 128 : RP * 2;              // bytes of a row of B (more than 64 ranks: two blocks)
-    static constexpr int C_SWIZZLE = RP >= 64 ? 2 : RP == 32 ? 4 : 6;
+    // At low ranks the parts lie side by side in one operand (and their sums in tensor memory), so that A is read once
+    // for all of them: up to 64 columns of B take the tensor core the same time (53 cycles measured; 68 for 128).
+    static constexpr bool SIDE = 4 * PARTS * RP <= 256;
+    static constexpr int C_ROW = SIDE || RP >= 64 ? 128 : RP * 2;      // bytes of a row of B (more than 64 ranks: two blocks)
+    static constexpr int C_SWIZZLE = SIDE || RP >= 64 ? 2 : RP == 32 ? 4 : 6;
     static constexpr int C_PART = R * RP * 2;
-    static constexpr int CONV = PARTS * C_PART;                        // one of two
+    static constexpr int CONV = SIDE ? R * 128 : PARTS * C_PART;       // one of two
     static constexpr int O_STRIDE = WC + 4;                            // floats: this CTA's sums, [rank][column]
-    static constexpr int ROWS = 4 * R * 4;
+    static constexpr int ROWS = 8 * R * 4;
     static constexpr int FIXED = 2 * CONV + ROWS + 128;                // (the swizzled parts first)
     static constexpr int PAD = 1024;                                   // swizzle patterns start at multiples of 1024 bytes
     static constexpr int HALF_SM = 113 * 1024, WHOLE_SM = 227 * 1024;
@@ -1147,7 +1163,8 @@ struct WgGeom16 {
     }
     static constexpr int STAGES = stages();
     static constexpr int SMEM = PAD + FIXED + STAGES * STAGE;
-    static constexpr int TMEM = 4 * RP;                                // columns: two accumulators of two blocks of RP
+    static constexpr int D = SIDE ? PARTS * RP : RP;                   // columns of an accumulator block
+    static constexpr int TMEM = 4 * D <= 64 ? 64 : 4 * D <= 128 ? 128 : 4 * D <= 256 ? 256 : 512;    // two accumulators of two blocks
     static constexpr int CTAS = SMEM <= HALF_SM && TMEM <= 256 ? 2 : 1;
     static constexpr int BLOCK = THREADS + 32;
     static_assert(SMEM <= WHOLE_SM && STAGE % 1024 == 0 && C_PART % 1024 == 0, "shared memory");
@@ -1164,7 +1181,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
     extern __shared__ char sm_raw[];
     char *sm = sm_raw + ((1024u - (smem_u32(sm_raw) & 1023u)) & 1023u);
     char *stages = sm, *conv = sm + G::STAGES * G::STAGE;              // [2][PARTS][row][C_ROW]
-    int *srow = reinterpret_cast<int *>(conv + 2 * G::CONV);           // [4][R]
+    int *srow = reinterpret_cast<int *>(conv + 2 * G::CONV);           // [8][R]
     u64 *bars = reinterpret_cast<u64 *>(reinterpret_cast<char *>(srow) + G::ROWS);
     u32 *s_tmem = reinterpret_cast<u32 *>(bars + 2);
     float *smax = reinterpret_cast<float *>(s_tmem + 4);
@@ -1186,38 +1203,44 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
 #pragma unroll
-    for (int i = 0; i < G::STAGES; ++i) wg_number_rows(w, srow, i);
+    for (int i = 0; i <= G::STAGES; ++i) wg_number_rows(w, srow, i, tid, THREADS);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const u32 tmem = *s_tmem;
 
+    // Barriers 1 and 2: a tile is ready to be multiplied (workers arrive, the ninth warp waits); 3 and 4: the row numbers
+    // further on are there (the other way round). Each pair takes turns: the side that only arrives may be one tile
+    // ahead, never two, since it waits for the other side's barrier (or the products) of the tile between.
     if (warp == WARPS) {                         // ---- the warp that issues the products
-        const u32 idesc = umma_idesc<T>(w.r16);
+        constexpr int GROUPS = G::SIDE ? 1 : PARTS;
+        const u32 idesc = umma_idesc<T>(G::SIDE ? PARTS * w.r16 : w.r16);
         const u64 b0 = umma_desc(conv_u, R * 128, 8 * G::C_ROW, G::C_SWIZZLE);
         int stage = 0;
 #pragma unroll 1
         for (int i = 0; i < w.nt; ++i) {
+            bar_arrive<G::BLOCK>(3 + (i & 1));                         // (the row numbers of tile i + STAGES are there)
             bar_sync<G::BLOCK>(1 + (i & 1));
             if (lane == 0) {
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const u64 a0 = umma_desc(ring + (u32)stage * G::STAGE, R * 128, 1024, 2);
                 const u64 bi = b0 + ((u32)(i & 1) * G::CONV >> 4);
-                const u32 d = tmem + (u32)(i & 1) * (2 * RP);
+                const u32 d = tmem + (u32)(i & 1) * (2 * G::D);
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     if (b * 128 >= w.wide) break;
 #pragma unroll
-                    for (int s = PARTS - 1; s >= 0; --s)
+                    for (int s = GROUPS - 1; s >= 0; --s)
 #pragma unroll
                         for (int k = 0; k < R / 16; ++k)
-                            umma_f16(d + b * RP, a0 + ((b * (2 * R * 128) + k * 2048) >> 4), bi + ((s * G::C_PART + k * 16 * G::C_ROW) >> 4), idesc,
-                                     s < PARTS - 1 || k > 0);
+                            umma_f16(d + b * G::D, a0 + ((b * (2 * R * 128) + k * 2048) >> 4), bi + ((s * G::C_PART + k * 16 * G::C_ROW) >> 4), idesc,
+                                     s < GROUPS - 1 || k > 0);
                 }
                 asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar + 8 * (i & 1)) : "memory");
             }
             __syncwarp();
             if (++stage == G::STAGES) stage = 0;
+            wg_number_rows(w, srow, i + G::STAGES + 1, lane, 32);      // (while they run; nobody reads this slot now)
         }
         __syncthreads();                         // (the workers' last products are in their registers)
         __syncthreads();                         // (their sums are in shared memory)
@@ -1240,10 +1263,20 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
     auto issue = [&](int i) {                    // activations of tile i
         if (i >= w.nt) return;
         const u32 st = ring + (u32)(i % G::STAGES) * G::STAGE + x_to;
-        const int *rows = srow + (i & 3) * R + xr;
+        const int *rows = srow + (i & 7) * R;
+        const int first = rows[0], last = rows[R - 1];
+        if (last - first == R - 1) {             // 64 rows that follow one another, as most tiles' do
+            const char *p = xbase + (first + xr) * ldx;
+#pragma unroll
+            for (int j = 0; j < XN; ++j) {
+                copy_unit<V>(st + j * 1024, p, act, xn, vec_act);
+                p += 8 * ldx;
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < XN; ++j) {           // (rows that do not exist become zero: they are summed over)
-            const int row = rows[8 * j];
+            const int row = rows[xr + 8 * j];
             copy_unit<V>(st + j * 1024, xbase + row * ldx, act, row >= 0 ? xn : 0, vec_act);
         }
     };
@@ -1253,7 +1286,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         for (int j = 0; j < FN; ++j) {
             v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (i >= w.nt || !has_f) continue;
-            const int row = srow[(i & 3) * R + fr + THREADS / FU * j];
+            const int row = srow[(i & 7) * R + fr + THREADS / FU * j];
             if (row < 0) continue;
             const float *p = coef + row * ldf;
             if (vec_f && whole_f) v[j] = *reinterpret_cast<const float4 *>(p);
@@ -1265,13 +1298,15 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
             }
         }
     };
-    // four ranks are 8 bytes: block of 64 ranks, 16-byte unit (moved by the swizzle), half of it
-    u32 c_to[FN];
+    // four ranks are 8 bytes: block of 64, 16-byte unit (moved by the swizzle), half of it. (A thread's rows lie a
+    // multiple of eight apart: one swizzle)
+    static_assert(THREADS / FU % 8 == 0, "rows of a thread");
+    u32 c_to[PARTS];
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-        const int r = fr + THREADS / FU * j, by = fq * 2, blk = by >> 7, un = (by & 127) >> 4;
-        const int sw = RP >= 64 ? un ^ (r & 7) : RP == 32 ? un ^ ((r >> 1) & 3) : un ^ ((r >> 2) & 1);
-        c_to[j] = blk * (R * 128) + r * G::C_ROW + (sw << 4) + (by & 8);
+    for (int s = 0; s < PARTS; ++s) {
+        const int by = (G::SIDE ? s * w.r16 + fq : fq) * 2, un = (by & 127) >> 4;
+        const int sw = G::C_ROW == 128 ? un ^ (fr & 7) : G::C_ROW == 64 ? un ^ ((fr >> 1) & 3) : un ^ ((fr >> 2) & 1);
+        c_to[s] = (G::SIDE ? 0 : s * G::C_PART) + (by >> 7) * (R * 128) + fr * G::C_ROW + (sw << 4) + (by & 8);
     }
     // this thread's column of the strip, `rank` sums of it
     float acc[RP];
@@ -1280,13 +1315,22 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
     bool fine = true;
     float unit = 1.0f, unit_before = 1.0f;       // binary16: the power of two that a tile's coefficients are divided by
     auto collect = [&](int i, float f) {         // tile i's sums from tensor memory
-        const u32 at = tmem + (u32)(i & 1) * (2 * RP) + (u32)(warp >> 2) * RP + ((u32)(warp & 3) << 21);
+        const u32 at = tmem + (u32)(i & 1) * (2 * G::D) + (u32)(warp >> 2) * G::D + ((u32)(warp & 3) << 21);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int q = 0; q < RP / 16; ++q) {
             if (q && q * 16 >= w.r16) break;
-            float t[16];
-            tmem_ld16(at + q * 16, t);
+            constexpr int SUMS = G::SIDE ? PARTS : 1;
+            float part[SUMS][16], t[16];
+#pragma unroll
+            for (int s = 0; s < SUMS; ++s) tmem_ld16(at + s * w.r16 + q * 16, part[s]);
+            tmem_ld_wait(part);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {       // the parts' sums, smallest first
+                t[e] = part[SUMS - 1][e];
+#pragma unroll
+                for (int s = SUMS - 2; s >= 0; --s) t[e] += part[s][e];
+            }
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[q * 16 + e] = HALF ? fmaf(f, t[e], acc[q * 16 + e]) : acc[q * 16 + e] + t[e];
         }
@@ -1309,7 +1353,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
 #pragma unroll
             for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
             if (lane == 0) smax[(i & 1) * WARPS + warp] = most;
-            bar_sync<THREADS>(3);
+            bar_sync<THREADS>(5);
 #pragma unroll
             for (int q = 0; q < WARPS; ++q) most = fmaxf(most, smax[(i & 1) * WARPS + q]);
             unit_before = unit;
@@ -1326,7 +1370,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
                     uint2 p;
                     split_pair(x0, x1, p.x, T());
                     split_pair(x2, x3, p.y, T());
-                    *reinterpret_cast<uint2 *>(cv + s * G::C_PART + c_to[j]) = p;
+                    *reinterpret_cast<uint2 *>(cv + c_to[s] + j * (THREADS / FU) * G::C_ROW) = p;
                 }
             }
         }
@@ -1338,8 +1382,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         if (i > 0) fine = mbar_wait(bar + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1) && fine;
         issue(i + G::STAGES - 1);
         cp_commit();
-        wg_number_rows(w, srow, i + G::STAGES);                        // (nobody reads this slot now; the next pass does)
-        bar_sync<THREADS>(3);
+        bar_sync<G::BLOCK>(3 + (i & 1));                               // (the row numbers of tile i + STAGES are there)
         if (i > 0) collect(i - 1, unit_before);
     }
     if (w.nt > 0) {
