@@ -413,11 +413,8 @@ int run_wgrad(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &ro
         int cluster = 1;
         double best = 0.0;
         for (int n = 1; n <= std::min(AD_MAX_CLUSTER, most_tiles); ++n) {
-            int fit = 0;
-            int rc = resident_clusters(ctx, kernel, n, fit);
-            if (rc) return rc;
             const long long ctas = (long long)strips * P.n_entries * n;
-            const double rounds = std::max(1.0, (double)ctas / ((double)fit * n));
+            const double rounds = std::max(1.0, (double)ctas / (double)(ctx->num_sms * kernel.per_sm / n * n));
             const double t = rounds * ((double)((most_tiles + n - 1) / n) + 4.0) * (ctas > ctx->num_sms ? 1.3 : 1.0);
             if (n == 1 || t < 0.999 * best) {
                 best = t;
