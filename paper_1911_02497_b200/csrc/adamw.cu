@@ -183,12 +183,12 @@ int adamw(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float mu, c
     s.eps = opt->eps;
     s.clip = (const float *)clip;
     s.copy_type = opt->w_h_dtype;
-    const int grid_max = ctx->num_sms * 3;
+    const int per_sm = eight ? 4 : 3, grid_max = ctx->num_sms * per_sm;
     for (int t0 = 0; t0 < T; t0 += LIST_LARGE) {
         const int n = std::min(T - t0, LIST_LARGE);
         if ((rc = set_items(ctx, d.data() + t0, n, grid_max, s)) != 0) return rc;
         if (s.n_items == 0) continue;
-        const int grid = stream_grid(ctx, s.n_items, 3);
+        const int grid = stream_grid(ctx, s.n_items, per_sm);
         const int pa_ = prof_begin(ctx, eight ? "k_adamw_8" : "k_adamw_32", stream);
         if (n <= LIST_SMALL) launch_adamw_cap<LIST_SMALL>(opt->grad_dtype, eight, pen, s, d.data() + t0, grid, stream);
         else launch_adamw_cap<LIST_LARGE>(opt->grad_dtype, eight, pen, s, d.data() + t0, grid, stream);
@@ -211,7 +211,7 @@ int grad_norm(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float m
     if (rc) return rc;
     if (pen && (!(mu >= 0.0f) || !std::isfinite(mu))) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "mu must be finite and >= 0");
     CU_TRY(ctx, cudaSetDevice(ctx->device));
-    const int grid_max = ctx->num_sms * 4;
+    const int grid_max = std::min(ctx->num_sms * 4, NORM_GRID_MAX);
     const size_t slots = (size_t)grid_max + LIST_LARGE;
     rc = op_workspace(ctx, 256 + sizeof(double) * (slots + (size_t)T), stream);
     if (rc) return rc;
@@ -232,7 +232,7 @@ int grad_norm(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float m
         if ((rc = set_items(ctx, d.data() + t0, n, grid_max, s)) != 0) return rc;
         N.t0 = t0;
         N.last = t0 + n == T;
-        const int grid = stream_grid(ctx, s.n_items, 4);
+        const int grid = std::max(1, std::min(grid_max, (int)s.n_items));
         const int pa_ = prof_begin(ctx, "k_grad_norm", stream);
         if (n <= LIST_SMALL) launch_norm_cap<LIST_SMALL>(grad_dtype, pen, s, d.data() + t0, N, grid, stream);
         else launch_norm_cap<LIST_LARGE>(grad_dtype, pen, s, d.data() + t0, N, grid, stream);
