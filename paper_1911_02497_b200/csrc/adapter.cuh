@@ -410,13 +410,15 @@ struct AdGeom {
     static constexpr int RG = TM / 16, KW = WARPS / RG;
     static constexpr int KB = 4 * U, NT = U / 2;                     // columns of a block; 8-column product tiles of one
     static constexpr int NB = RP <= 16 ? 2 : 1;                      // source blocks of a step of the first loop
-    static constexpr bool AHEAD = RP <= 32;                          // A and B, too, are loaded a step ahead; else half a step
+    // A and B, too, are loaded a step ahead; else half a step. (Short tiles, a decoding step's, are bound by latency
+    // alone and leave registers to spare)
+    static constexpr bool AHEAD = RP <= 32 || (TM == 16 && RP == 64);
     static constexpr int HP_STRIDE = RP + 4;                         // floats
     static constexpr int HP = (KW > 1 ? KW / 2 : 1) * TM * HP_STRIDE * 4;    // partial sums
     static constexpr int HO_STRIDE = RP * E + (RP * E == 32 ? 0 : 32);       // operand of the expansion: four rows meet all banks
     static constexpr int HO = TM * HO_STRIDE * AdType<T>::PARTS;
     static constexpr int SMEM = HP + HO + TM * 8;
-    static constexpr int CTAS = RP <= 64 ? 2 : 1;                    // resident on an SM, at least
+    static constexpr int CTAS = RP <= 32 || (TM == 64 && RP == 64) ? 2 : 1;                    // resident on an SM, at least
     static_assert(HP % 16 == 0 && HO % 16 == 0 && SMEM <= 227 * 1024, "shared memory");
 };
 
@@ -425,7 +427,6 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
 {
     using G = AdGeom<T, TM, RP>;
     constexpr int E = G::E, U = G::U, NT = G::NT, NB = G::NB, KB = G::KB, KW = G::KW, KSTEP = AdType<T>::KSTEP, PARTS = AdType<T>::PARTS;
-    constexpr int WV = V == 8 ? 8 : 16;                              // access to A (laid out anew where it allows less)
     constexpr int JT = RP / 8, ST = RP / KSTEP;                      // tiles and steps of the rank
     constexpr int BLOCK = KB * E;                                    // bytes of a block: 64
     extern __shared__ __align__(128) char sm[];
@@ -440,11 +441,9 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
     const AdapterEntry *entries = reinterpret_cast<const AdapterEntry *>(P.blob);
     const AdapterRun *runs = reinterpret_cast<const AdapterRun *>(entries + P.n_entries);
     const int tile = (int)blockIdx.x / (C * P.splits), split = (int)blockIdx.x / C % P.splits;
-    int which = 0;
-    for (int hi = P.n_entries - 1; which < hi;) {
-        const int mid = (which + hi + 1) >> 1;
-        if (entries[mid].tile0 <= tile) which = mid; else hi = mid - 1;
-    }
+    // the tile's adapter: entries are in order of their first tiles (all looked at together: one load's latency)
+    int which = -1;
+    for (int e = lane; e - lane < P.n_entries; e += 32) which += __popc(__ballot_sync(0xFFFFFFFFu, e < P.n_entries && entries[e].tile0 <= tile));
     const AdapterEntry &ent = entries[which];
     const int row0 = (tile - ent.tile0) * TM, count = min(TM, ent.n_rows - row0), rank = ent.rank, r16 = (rank + 15) & ~15;
     // (places without a row take the tile's first: what they yield is dropped)
@@ -496,7 +495,12 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
         for (int j = 0; j < JH; ++j) {
             if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) s.w[b][j] = load_unit<WV, E, false>(pw + w_off[j0 + j] + b * BLOCK);
+            for (int b = 0; b < NB; ++b) {
+                // (a matrix laid out anew allows 16 bytes; A as it is where V is 8, only 8)
+                const char *p = pw + w_off[j0 + j] + b * BLOCK;
+                if (V != 8 || P.scale_h) s.w[b][j] = load_unit<16, E, false>(p);
+                else s.w[b][j] = load_unit<8, E, false>(p);
+            }
         }
         if (j0 + JH == JT) pw += NB * BLOCK;
     };
