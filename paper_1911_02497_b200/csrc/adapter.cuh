@@ -454,7 +454,8 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
     const int KBT = (ws + KB - 1) / KB, NBT = P.dst ? (wd + KB - 1) / KB : 0;
     // this warp's source blocks, and its destination blocks (kw, kw + KW, ... of the CTA's)
     const int kparts = C * KW, kpart = c_rank * KW + kw;
-    const int kb0 = (int)((long long)kpart * KBT / kparts), kb1 = (int)((long long)(kpart + 1) * KBT / kparts);
+    const int KST = (KBT + NB - 1) / NB;                             // (whole steps of NB blocks, but at the very end)
+    const int kb0 = NB * (int)((long long)kpart * KST / kparts), kb1 = min(KBT, NB * (int)((long long)(kpart + 1) * KST / kparts));
     const int part = split * C + c_rank, parts = C * P.splits;
     const int nb0 = (int)((long long)part * NBT / parts) + kw, nb1 = (int)((long long)(part + 1) * NBT / parts);
     const char *px[2];
@@ -579,9 +580,10 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
 #pragma unroll 1
         for (int kb = kb0 + steps * NB; kb < kb1; ++kb) {
             const int n = min(max(ws - kb * KB - t4 * U, 0), U);
+            const bool whole = (kb + 1) * KB <= ws;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                x0.x[0][h] = load_some<E>(px[h], n);
+                x0.x[0][h] = whole ? load_unit<V, E, true>(px[h]) : load_some<E>(px[h], n);
                 px[h] += BLOCK;
             }
 #pragma unroll
@@ -589,7 +591,7 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
 #pragma unroll
                 for (int j = 0; j < JH; ++j) {
                     if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
-                    w0.w[0][j] = load_some<E>(pw + w_off[j0 + j], n);
+                    w0.w[0][j] = whole ? load_unit<8, E, false>(pw + w_off[j0 + j]) : load_some<E>(pw + w_off[j0 + j], n);
                 }
                 multiply(x0, w0, 1, j0);
             }
