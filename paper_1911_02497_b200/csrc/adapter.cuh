@@ -156,10 +156,11 @@ template <class T> struct FragB { u32 r[2]; };
 template <> struct FragA<float> { u32 hi[4], lo[4]; };       // two TF32 parts: 22 bits of the operand
 template <> struct FragB<float> { u32 hi[2], lo[2]; };
 
-// (the instruction reads the upper 19 bits of an operand: the second part needs no rounding of its own)
+// (the instruction reads the upper 19 bits of an operand: the second part, at most 2^-12 of the value, is cut there.
+// No number stays one: its rest is no number.)
 __device__ __forceinline__ void split_tf32(float x, u32 &hi, u32 &lo)
 {
-    hi = __float_as_uint(x) & 0xFFFFE000u;
+    hi = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
     lo = __float_as_uint(x - __uint_as_float(hi));
 }
 

@@ -247,10 +247,16 @@ _DTYPES = {"float32": DTYPE_FP32, "float16": DTYPE_FP16, "bfloat16": DTYPE_BF16,
            "uint8": DTYPE_FP8_E4M3}
 
 
-def _dtype_code(x, allowed, what: str) -> int:
-    code = _DTYPES.get(str(x.dtype).replace("torch.", ""))
+_codes = {}                     # type object (torch's or numpy's) -> code
+
+
+def _dtype_code(x, allowed, what: str, *args) -> int:
+    dtype = x.dtype
+    code = _codes.get(dtype)
+    if code is None:
+        code = _codes[dtype] = _DTYPES.get(str(dtype).replace("torch.", ""), -1)
     if code not in allowed:
-        raise TypeError("%s: type %s is not supported" % (what, x.dtype))
+        raise TypeError((what + ": type %s is not supported") % (args + (dtype,)))
     return code
 
 
@@ -288,7 +294,7 @@ def adamw_table(w, grad, m=None, v=None, m_scale=None, v_scale=None, theta=None,
             x = group[t] if group is not None else None
             if x is None:
                 continue
-            code = _dtype_code(x, allowed, "tensor %d: %s" % (t, name))
+            code = _dtype_code(x, allowed, "tensor %d: %s", t, name)
             want = -(-n // STATE_BLOCK) if name.endswith("_scale") else n
             if _numel(x) != want or not _contiguous(x):
                 raise ValueError("tensor %d: %s must be contiguous and hold %d elements" % (t, name, want))
@@ -329,7 +335,7 @@ def adapter_table(a, b, scale, grad_a=None, grad_b=None) -> AdapterTable:
                 wanted.append((name, group[i], shape, None))
         for name, x, shape, kind in wanted:
             if kind is None:
-                _dtype_code(x, (DTYPE_FP32,), "adapter %d: %s" % (i, name))
+                _dtype_code(x, (DTYPE_FP32,), "adapter %d: %s", i, name)
             elif x.dtype != kind:
                 raise TypeError("adapter %d: %s has type %s, the table's is %s" % (i, name, x.dtype, kind))
             if tuple(x.shape) != shape or not _contiguous(x):
@@ -361,7 +367,8 @@ def _rows_of(x, rows: int, width: int, dtype, name: str):
 def _kept_rows(h, rows: int):
     if h is None:
         return None, 0
-    if _DTYPES.get(str(h.dtype).replace("torch.", "")) != DTYPE_FP32 or h.dim() != 2 or h.shape[0] != rows or (h.shape[1] > 1 and h.stride(1) != 1):
+    _dtype_code(h, (DTYPE_FP32,), "h")
+    if h.dim() != 2 or h.shape[0] != rows or (h.shape[1] > 1 and h.stride(1) != 1):
         raise ValueError("h must be a float32 matrix of %d contiguous rows" % rows)
     return h.data_ptr(), (h.stride(0) if rows > 1 else max(h.shape[1], h.stride(0)))
 
