@@ -305,7 +305,8 @@ CONDENSA_API int condensa_lstep_update(condensa_ctx *ctx, const condensa_opt_ten
  * magnitude, at least 2^-126; code = E4M3(x / scale), round to nearest even. A positive r never
  * becomes 0 (its code is at least 1, i.e. scale * 2^-9), so that a small second moment cannot turn into a
  * division by eps; a value that is not finite becomes NaN. w' is formed from m' and r' before they
- * are rounded. Zero states are zero bytes with any finite scale. */
+ * are rounded, its quotient to within 2 units in the last place. Zero states are zero bytes with any
+ * finite scale. */
 #define CONDENSA_STATE_BLOCK 256
 enum { CONDENSA_DTYPE_FP32 = 0 };
 
@@ -348,8 +349,9 @@ CONDENSA_API int condensa_lstep_adamw(condensa_ctx *ctx, const condensa_adamw_te
 
 /* Norm of the gradient g (before clipping) that condensa_lstep_adamw() would form from the same
  * arguments: reads grad and, where theta is given, w, theta and lambda; the other fields are
- * not looked at. Squares are summed in fp64 in an order that depends on the list and the device
- * only, so equal inputs give equal bits. `clip` (DEVICE) receives the record, `norms` (DEVICE, T
+ * not looked at. Squares are summed in fp32 by groups of eight (in fp64 where they leave its
+ * range) and the groups in fp64, in an order that depends on the list and the device only, so
+ * equal inputs give equal bits. `clip` (DEVICE) receives the record, `norms` (DEVICE, T
  * floats, may be NULL) the norm of each tensor (0 for an empty one). A norm beyond fp32 reads as
  * infinite. max_norm <= 0: the norm is only measured. A captured call must not run while another
  * call of the context runs. */
@@ -370,15 +372,20 @@ CONDENSA_API int condensa_grad_norm(condensa_ctx *ctx, const condensa_adamw_tens
  * fp32 and rounded once. Rows without an adapter are neither read nor written.
  *
  * x, y, dy, dx, A and B share one type (CONDENSA_DTYPE_FP32, _FP16, _BF16); h, dA and dB are fp32.
- * Rows may lie `ld` elements apart; A, B, dA and dB are contiguous. Products of 16-bit types
+ * Rows may lie `ld` elements apart; A, B, dA and dB are contiguous. 16-byte alignment is fastest, 8 bytes
+ * next; anything less costs more. Products of 16-bit types
  * are exact and summed in fp32; h and u enter the second product as sums of two (gradients of
  * bfloat16: three) 16-bit parts, fp32 operands as two TF32 parts, so nothing is rounded to 16 bits but
  * the results. Sums run in an order that depends on the shapes, the requests and the device only.
+ * Rows do not mix: what is not finite in a row stays in its h, y and dx (and enters its adapter's
+ * gradients); an infinity may come out as NaN.
  *
  * The request lists and the adapter table are HOST arrays and are used up when the call returns.
  * Nothing is copied to the device ahead of the kernels (the lists travel as kernel parameters), so
- * calls may be captured into a CUDA graph; a captured backward call must not run while another
- * backward call of the context runs (they share a workspace of partial sums). */
+ * calls may be captured into a CUDA graph after one plain call of the same shape. Backward calls, and
+ * forward calls whose A or B must be laid out anew (rows of A that are not 16- resp. 8-byte aligned like
+ * those of x and y, ranks that are not whole quads of 8 bytes), use a workspace of the context: a captured
+ * one must not run while another call of the context runs. */
 #define CONDENSA_ADAPTER_MAX_RANK 128
 
 typedef struct {
