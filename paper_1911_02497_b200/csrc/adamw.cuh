@@ -309,6 +309,17 @@ __global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) k_adamw(const __grid_c
             if (left <= 0) break;
             const bool vec = d.vec_ok && left >= LIST_CHUNK;
             const long long blk = e0 / LIST_CHUNK;
+            // the warp's next chunk, of this item or of the CTA's next one where that is the same tensor's, is asked for
+            // ahead: a line per lane, of w (8), the gradient (8 or 4), the codes (2 + 2). (Moments in 8 bits leave fewer
+            // bytes in flight than those in 32: 456 -> 401 us on 135.9 M elements, and no register)
+            const long long e1 = k + 1 < s.chunks ? e0 + WARPS * LIST_CHUNK : first + (long long)gridDim.x * s.chunks * (WARPS * LIST_CHUNK);
+            if (EIGHT && d.numel - e1 >= LIST_CHUNK) {
+                constexpr int GL = GT == GT_F32 ? 8 : 4;
+                const char *p = lane < 8 ? (const char *)(d.w + e1) + lane * 128
+                              : lane < 8 + GL ? (const char *)d.grad + e1 * (GT == GT_F32 ? 4 : 2) + (lane - 8) * 128
+                              : lane < 10 + GL ? (const char *)d.m + e1 + (lane - 8 - GL) * 128 : (const char *)d.v + e1 + (lane - 10 - GL) * 128;
+                if (lane < 12 + GL) asm volatile("prefetch.global.L2 [%0];" :: "l"(p));
+            }
             Oct w = load_f32(d.w + e0, lane, left, vec);
             Oct g = load_grad<GT>(d.grad, e0, lane, left, vec);
             Oct th, lam, m, v;
