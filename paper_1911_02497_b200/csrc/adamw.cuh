@@ -290,6 +290,9 @@ __device__ __forceinline__ float total_gradient(const ListScalars &s, float gr, 
 
 // AdamW. Bytes per element: w 8, gradient 4 or 2, theta and lambda 8 with the penalty, moments 16
 // (fp32) or 4 + 16/256 (8 bits), copy 2: bound by memory, and every byte is moved once.
+// Measured on 135.9 M elements (shares of a plain copy's 6530 GB/s): fp32 gradients and moments with the penalty, 36 bytes
+// an element, 773 us (0.97); bfloat16 gradients and copies with 8-bit moments, 16 bytes, 401 us (0.83, with some 65
+// instructions an element beside it). 1.9 M elements in 32 tensors: 9 us, a launch and one round of the CTAs.
 template <int CAP, int GT, bool EIGHT, bool PEN>
 __global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) k_adamw(const __grid_constant__ ListParams<CAP> P)
 {
@@ -381,8 +384,9 @@ __global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) k_adamw(const __grid_c
 
 // ------------------------------------------------------------------ norm
 // Squares are summed in fp32 by groups of eight values, the groups in fp64. Bound by memory; the loads run a batch ahead
-// of the sums (135.9 M values of bfloat16: 83 us without that, 53 us with it). Each CTA takes a contiguous range of the work items and leaves one fp64 partial sum per tensor
-// that it meets. CTA b's sum for tensor t goes to slot b + t: both only grow along the list, so no
+// of the sums (135.9 M values of bfloat16: 83 us without that, 53 us with it, 0.78 of a copy's rate; 58 tensors of
+// 0.85 M values in all: 12.5 us, most of it the launch and the last CTA's sums). Each CTA takes a contiguous range of the
+// work items and leaves one fp64 partial sum per tensor that it meets. CTA b's sum for tensor t goes to slot b + t: both only grow along the list, so no
 // two pairs share a slot. The CTA that finishes last adds the slots of each tensor in order.
 struct NormOut {
     double *slot;           // grid + T of them
