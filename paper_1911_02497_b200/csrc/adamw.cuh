@@ -291,7 +291,7 @@ __device__ __forceinline__ float total_gradient(const ListScalars &s, float gr, 
 // AdamW. Bytes per element: w 8, gradient 4 or 2, theta and lambda 8 with the penalty, moments 16
 // (fp32) or 4 + 16/256 (8 bits), copy 2: bound by memory, and every byte is moved once.
 // Measured on 135.9 M elements (shares of a plain copy's 6530 GB/s): fp32 gradients and moments with the penalty, 36 bytes
-// an element, 773 us (0.97); bfloat16 gradients and copies with 8-bit moments, 16 bytes, 401 us (0.83, with some 65
+// an element, 773 us (0.97); bfloat16 gradients and copies with 8-bit moments, 16 bytes, 401 us (0.83, with 79
 // instructions an element beside it). 1.9 M elements in 32 tensors: 9 us, a launch and one round of the CTAs.
 template <int CAP, int GT, bool EIGHT, bool PEN>
 __global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) k_adamw(const __grid_constant__ ListParams<CAP> P)

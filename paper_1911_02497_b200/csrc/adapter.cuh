@@ -425,7 +425,7 @@ struct AdGeom {
 
 // Measured: 6011 rows of 9216 -> 4096, rank 16, bf16: 52 us, 0.57 of a copy's rate; a load of 16 bytes a lane touches 8
 // rows, so L1 looks up 8 lines for it, and that is the bound. 700 rows of 1500 -> 33278, fp32, accesses of 8 bytes: 69 us
-// (0.44). Backward, 8192 rows of 4096 and 4096 columns: 41 us (floor 31). Decoding, 64 rows of 4096 -> 4096, ranks to
+// (0.44). Backward, 8192 rows of 4096 and 4096 columns: 43 us (floor 31). Decoding, 64 rows of 4096 -> 4096, ranks to
 // 64, fp16: 11 us, the latency of few warps' dependent instructions.
 template <class T, int TM, int RP, int V>
 __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(const __grid_constant__ AdapterParams P)
