@@ -290,6 +290,8 @@ CONDENSA_API int condensa_lstep_update(condensa_ctx *ctx, const condensa_opt_ten
  * for the next forward pass, one launch for the list (one per 360 tensors). No call here copies
  * anything from the host or allocates, except that condensa_grad_norm() grows a small workspace
  * (partial sums) the first time; both can be captured into a CUDA graph after one plain call.
+ * Graphs stay valid when later calls outgrow that workspace: a block that a capture was given is
+ * kept until condensa_destroy(), beside the larger one. No replay may follow condensa_destroy().
  *
  * Per element, in this order of single fp32 operations (`grad` widened to fp32 first):
  *     g = grad_scale * grad;    [theta given:  d = w - theta;  p = mu*d;  q = p - lambda;  g = g + q]
@@ -385,7 +387,8 @@ CONDENSA_API int condensa_grad_norm(condensa_ctx *ctx, const condensa_adamw_tens
  * calls may be captured into a CUDA graph after one plain call of the same shape. Backward calls, and
  * forward calls whose A or B must be laid out anew (rows of A that are not 16- resp. 8-byte aligned like
  * those of x and y, ranks that are not whole quads of 8 bytes), use a workspace of the context: a captured
- * one must not run while another call of the context runs. */
+ * one must not run while another call of the context runs. (A block of it that a capture was given is kept
+ * until condensa_destroy(), so later calls may outgrow it.) */
 #define CONDENSA_ADAPTER_MAX_RANK 128
 
 typedef struct {

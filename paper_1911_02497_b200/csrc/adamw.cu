@@ -216,8 +216,8 @@ int grad_norm(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float m
     rc = op_workspace(ctx, 256 + sizeof(double) * (slots + (size_t)T), stream);
     if (rc) return rc;
     NormOut N;
-    N.done = (u32 *)ctx->op_ws;
-    N.slot = (double *)(ctx->op_ws + 256);
+    N.done = (u32 *)ctx->op.p;
+    N.slot = (double *)(ctx->op.p + 256);
     N.square = N.slot + slots;
     N.norms = norms;
     N.clip = (float *)clip;

@@ -510,7 +510,7 @@ int forward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, l
     char *ws = nullptr;
     if (pk.bytes) {
         if ((rc = op_workspace(ctx, 256 + pk.bytes, stream)) != 0) return rc;
-        ws = ctx->op_ws + 256;
+        ws = ctx->op.p + 256;
         if ((rc = run_packing(ctx, b, rows, pk, ws, stream)) != 0) return rc;
     }
     if ((rc = run_rows(ctx, b, rows, pk, ws, call, stream)) != 0) return rc;
@@ -556,8 +556,8 @@ int backward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, 
     char *pk_ws = nullptr;
     if (u_bytes + pk.bytes) {
         if ((rc = op_workspace(ctx, 256 + u_bytes + pk.bytes, stream)) != 0) return rc;
-        u_ws = need_a ? (float *)(ctx->op_ws + 256) : nullptr;
-        pk_ws = ctx->op_ws + 256 + u_bytes;
+        u_ws = need_a ? (float *)(ctx->op.p + 256) : nullptr;
+        pk_ws = ctx->op.p + 256 + u_bytes;
     }
     if (pk.bytes && (rc = run_packing(ctx, b, rows, pk, pk_ws, stream)) != 0) return rc;
     if (row_kernel && (rc = run_rows(ctx, b, rows, pk, pk_ws, row_call(dy, dx, u_ws, lddy, lddx, ldu, true, e), stream)) != 0) return rc;

@@ -840,8 +840,7 @@ int condensa_destroy(condensa_ctx *ctx)
     cudaDeviceSynchronize();
     if (ctx->ws) cudaFree(ctx->ws);
     if (ctx->mirror.buf) cudaFree(ctx->mirror.buf);
-    if (ctx->op_ws) cudaFree(ctx->op_ws);
-    if (ctx->op_ev) cudaEventDestroy(ctx->op_ev);
+    op_workspace_destroy(ctx->op);
     if (ctx->h_stage) cudaFreeHost(ctx->h_stage);
     if (ctx->stage_ev) cudaEventDestroy(ctx->stage_ev);
     if (ctx->tail_ev) cudaEventDestroy(ctx->tail_ev);

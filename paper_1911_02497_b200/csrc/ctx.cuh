@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "op_workspace.h"
 
 using cs::Ctl;
 
@@ -63,13 +64,7 @@ struct condensa_ctx {
     struct ClusterFit { const void *f; int size, count; };
     std::vector<ClusterFit> cluster_fit;    // clusters of a kernel that the device holds at once
     std::vector<const void *> op_smem_set;  // adapter kernels whose shared memory limit has been raised on this device
-    // workspace of the list operators and the adapters (partial sums); apart from the C-step's
-    char *op_ws = nullptr;
-    size_t op_ws_bytes = 0;
-    cudaEvent_t op_ev = nullptr;            // recorded behind the last call that used it
-    cudaStream_t op_stream = nullptr;
-    bool op_recorded = false;
-    bool op_capturing = false;              // the call under way is being captured
+    OpWorkspace op;                         // of the list operators and the adapters; apart from the C-step's
 };
 
 inline int fail(condensa_ctx *c, int code, const char *fmt, ...)
@@ -192,48 +187,22 @@ inline bool ranges_clash(std::vector<Interval> &iv)
     return false;
 }
 
-// Room for `bytes` in the operators' workspace, ordered behind its last user on another stream.
-// The first 256 bytes hold counters that are zero between calls. Growing waits for the device once,
-// so it cannot happen inside a stream capture; a captured call is not ordered behind other streams
-// (the event would belong to work outside the graph): its replays must not overlap other calls.
+// Room for `bytes` in the operators' workspace (op_workspace.h).
 inline int op_workspace(condensa_ctx *ctx, size_t bytes, cudaStream_t stream)
 {
-    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
-    CU_TRY(ctx, cudaStreamIsCapturing(stream, &st));
-    ctx->op_capturing = st != cudaStreamCaptureStatusNone;
-    if (ctx->op_capturing) {
-        if (bytes > ctx->op_ws_bytes)
-            return fail(ctx, CONDENSA_ERR_WORKSPACE, "the workspace must grow, which a stream capture does not allow: make the call once before");
-        return CONDENSA_OK;
+    cudaError_t e = cudaSuccess;
+    switch (op_workspace_take(ctx->op, bytes, stream, e)) {
+    case OP_WS_OK: return CONDENSA_OK;
+    case OP_WS_CAPTURE:
+        return fail(ctx, CONDENSA_ERR_WORKSPACE, "the workspace must grow, which a stream capture does not allow: make the call once before");
+    case OP_WS_MEMORY: return fail(ctx, CONDENSA_ERR_WORKSPACE, "cannot allocate a workspace for %zu bytes: %s", bytes, cudaGetErrorString(e));
+    default: return fail(ctx, CONDENSA_ERR_CUDA, "workspace: %s", cudaGetErrorString(e));
     }
-    if (!ctx->op_ev) CU_TRY(ctx, cudaEventCreateWithFlags(&ctx->op_ev, cudaEventDisableTiming));
-    if (bytes > ctx->op_ws_bytes) {
-        CU_TRY(ctx, cudaDeviceSynchronize());
-        if (ctx->op_ws) cudaFree(ctx->op_ws);
-        ctx->op_ws = nullptr;
-        ctx->op_ws_bytes = 0;
-        ctx->op_recorded = false;
-        const size_t want = align_up(bytes + bytes / 4, 1 << 20);
-        const cudaError_t e = cudaMalloc((void **)&ctx->op_ws, want);
-        if (e != cudaSuccess) {
-            cudaGetLastError();
-            ctx->op_ws = nullptr;
-            return fail(ctx, CONDENSA_ERR_WORKSPACE, "cannot allocate %zu bytes of workspace: %s", want, cudaGetErrorString(e));
-        }
-        ctx->op_ws_bytes = want;
-        CU_TRY(ctx, cudaMemsetAsync(ctx->op_ws, 0, 256, stream));
-    } else if (ctx->op_recorded && ctx->op_stream != stream) {
-        CU_TRY(ctx, cudaStreamWaitEvent(stream, ctx->op_ev, 0));
-    }
-    ctx->op_stream = stream;
-    return CONDENSA_OK;
 }
 
 // Behind the last launch of a call that used the operators' workspace.
 inline int op_workspace_done(condensa_ctx *ctx, cudaStream_t stream)
 {
-    if (ctx->op_capturing) return CONDENSA_OK;
-    CU_TRY(ctx, cudaEventRecord(ctx->op_ev, stream));
-    ctx->op_recorded = true;
+    CU_TRY(ctx, op_workspace_leave(ctx->op, stream));
     return CONDENSA_OK;
 }
