@@ -213,7 +213,8 @@ int grad_norm(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float m
     CU_TRY(ctx, cudaSetDevice(ctx->device));
     const int grid_max = std::min(ctx->num_sms * 4, NORM_GRID_MAX);
     const size_t slots = (size_t)grid_max + LIST_LARGE;
-    rc = op_workspace(ctx, 256 + sizeof(double) * (slots + (size_t)T), stream);
+    OpWorkspaceUse use;
+    rc = op_workspace(ctx, 256 + sizeof(double) * (slots + (size_t)T), stream, use);
     if (rc) return rc;
     NormOut N;
     N.done = (u32 *)ctx->op.p;
@@ -239,7 +240,7 @@ int grad_norm(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float m
         LAUNCH_CHECK(ctx);
         prof_end(ctx, pa_, stream);
     }
-    return op_workspace_done(ctx, stream);
+    return op_workspace_done(ctx, use);
 }
 
 }  // namespace

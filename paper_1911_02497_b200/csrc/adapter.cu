@@ -508,13 +508,14 @@ int forward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, l
     Packed pk;
     plan_packing(b, rows, false, call.vec, pk);
     char *ws = nullptr;
+    OpWorkspaceUse use;
     if (pk.bytes) {
-        if ((rc = op_workspace(ctx, 256 + pk.bytes, stream)) != 0) return rc;
+        if ((rc = op_workspace(ctx, 256 + pk.bytes, stream, use)) != 0) return rc;
         ws = ctx->op.p + 256;
         if ((rc = run_packing(ctx, b, rows, pk, ws, stream)) != 0) return rc;
     }
     if ((rc = run_rows(ctx, b, rows, pk, ws, call, stream)) != 0) return rc;
-    return pk.bytes ? op_workspace_done(ctx, stream) : CONDENSA_OK;
+    return op_workspace_done(ctx, use);
 }
 
 int backward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, long long ldx, const void *dy, long long lddy, const float *h,
@@ -554,15 +555,16 @@ int backward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, 
     const size_t u_bytes = need_a ? align_up(sizeof(float) * (size_t)(rows.total * ldu), 256) : 0;
     float *u_ws = nullptr;
     char *pk_ws = nullptr;
+    OpWorkspaceUse use;
     if (u_bytes + pk.bytes) {
-        if ((rc = op_workspace(ctx, 256 + u_bytes + pk.bytes, stream)) != 0) return rc;
+        if ((rc = op_workspace(ctx, 256 + u_bytes + pk.bytes, stream, use)) != 0) return rc;
         u_ws = need_a ? (float *)(ctx->op.p + 256) : nullptr;
         pk_ws = ctx->op.p + 256 + u_bytes;
     }
     if (pk.bytes && (rc = run_packing(ctx, b, rows, pk, pk_ws, stream)) != 0) return rc;
     if (row_kernel && (rc = run_rows(ctx, b, rows, pk, pk_ws, row_call(dy, dx, u_ws, lddy, lddx, ldu, true, e), stream)) != 0) return rc;
     if ((rc = run_wgrad(ctx, b, rows, {x, dy, u_ws, h, ldx, lddy, ldu, ldh, accumulate != 0, row_kernel}, stream)) != 0) return rc;
-    return u_bytes + pk.bytes ? op_workspace_done(ctx, stream) : CONDENSA_OK;
+    return op_workspace_done(ctx, use);
 }
 
 }  // namespace

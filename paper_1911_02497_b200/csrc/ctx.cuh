@@ -187,11 +187,11 @@ inline bool ranges_clash(std::vector<Interval> &iv)
     return false;
 }
 
-// Room for `bytes` in the operators' workspace (op_workspace.h).
-inline int op_workspace(condensa_ctx *ctx, size_t bytes, cudaStream_t stream)
+// Room for `bytes` in the operators' workspace (op_workspace.h); `use` lives to the end of the call.
+inline int op_workspace(condensa_ctx *ctx, size_t bytes, cudaStream_t stream, OpWorkspaceUse &use)
 {
     cudaError_t e = cudaSuccess;
-    switch (op_workspace_take(ctx->op, bytes, stream, e)) {
+    switch (op_workspace_take(ctx->op, bytes, stream, e, use)) {
     case OP_WS_OK: return CONDENSA_OK;
     case OP_WS_CAPTURE:
         return fail(ctx, CONDENSA_ERR_WORKSPACE, "the workspace must grow, which a stream capture does not allow: make the call once before");
@@ -200,9 +200,9 @@ inline int op_workspace(condensa_ctx *ctx, size_t bytes, cudaStream_t stream)
     }
 }
 
-// Behind the last launch of a call that used the operators' workspace.
-inline int op_workspace_done(condensa_ctx *ctx, cudaStream_t stream)
+// Behind the last launch of a call that may have used it.
+inline int op_workspace_done(condensa_ctx *ctx, OpWorkspaceUse &use)
 {
-    CU_TRY(ctx, op_workspace_leave(ctx->op, stream));
+    CU_TRY(ctx, op_workspace_leave(use));
     return CONDENSA_OK;
 }

@@ -49,8 +49,12 @@ inline OpWorkspaceStatus op_workspace_take(OpWorkspace &w, size_t want, cudaStre
             w.p = nullptr;
             return OP_WS_MEMORY;
         }
+        if ((e = cudaMemsetAsync(w.p, 0, 256, stream)) != cudaSuccess) {
+            cudaFree(w.p);
+            w.p = nullptr;
+            return OP_WS_CUDA;
+        }
         w.bytes = room;
-        if ((e = cudaMemsetAsync(w.p, 0, 256, stream)) != cudaSuccess) return OP_WS_CUDA;
     } else if (w.recorded && w.stream != stream) {
         if ((e = cudaStreamWaitEvent(stream, w.ev, 0)) != cudaSuccess) return OP_WS_CUDA;
     }
@@ -65,6 +69,38 @@ inline cudaError_t op_workspace_leave(OpWorkspace &w, cudaStream_t stream)
     const cudaError_t e = cudaEventRecord(w.ev, stream);
     if (e == cudaSuccess) w.recorded = true;
     return e;
+}
+
+// A call's use of the workspace: left at the end of the call however it ends, so that what it has launched by then is
+// waited for.
+struct OpWorkspaceUse {
+    OpWorkspace *w = nullptr;
+    cudaStream_t stream = nullptr;
+    OpWorkspaceUse() = default;
+    OpWorkspaceUse(const OpWorkspaceUse &) = delete;
+    OpWorkspaceUse &operator=(const OpWorkspaceUse &) = delete;
+    ~OpWorkspaceUse()
+    {
+        if (w) op_workspace_leave(*w, stream);
+    }
+};
+
+inline OpWorkspaceStatus op_workspace_take(OpWorkspace &w, size_t want, cudaStream_t stream, cudaError_t &e, OpWorkspaceUse &use)
+{
+    const OpWorkspaceStatus s = op_workspace_take(w, want, stream, e);
+    if (s == OP_WS_OK) {
+        use.w = &w;
+        use.stream = stream;
+    }
+    return s;
+}
+
+inline cudaError_t op_workspace_leave(OpWorkspaceUse &use)
+{
+    if (!use.w) return cudaSuccess;
+    OpWorkspace &w = *use.w;
+    use.w = nullptr;
+    return op_workspace_leave(w, use.stream);
 }
 
 inline void op_workspace_destroy(OpWorkspace &w)

@@ -120,3 +120,34 @@ def test_calls_are_ordered_across_streams_and_captures_are_not(run):
         CHECK(op_workspace_take(w, 64 << 20, A, e) == OP_WS_CAPTURE && log_ == "");
         op_workspace_destroy(w);
     """)
+
+
+def test_a_call_that_fails_midway_is_still_ordered(run):
+    """Whatever a call has launched by then uses the block: the next call on another stream waits for it."""
+    run(r"""
+        {
+            OpWorkspaceUse use;
+            CHECK(op_workspace_take(w, 1000, A, e, use) == OP_WS_OK);
+        }                                   // an error return between the launches
+        CHECK(log_ == "sync;zero256;record1;" && w.recorded);
+        log_ = "";
+        {
+            OpWorkspaceUse use;
+            CHECK(op_workspace_take(w, 1000, B, e, use) == OP_WS_OK && log_ == "wait2;");
+            CHECK(op_workspace_leave(use) == cudaSuccess && log_ == "wait2;record2;");
+        }
+        CHECK(log_ == "wait2;record2;");    // once
+        log_ = "";
+        {
+            OpWorkspaceUse use;             // a call that needs no workspace
+            CHECK(op_workspace_leave(use) == cudaSuccess);
+        }
+        captured.insert(A);
+        {
+            OpWorkspaceUse use;
+            CHECK(op_workspace_take(w, 1000, A, e, use) == OP_WS_OK);
+            CHECK(op_workspace_take(w, 64 << 20, A, e, use) == OP_WS_CAPTURE);
+        }
+        CHECK(log_ == "");
+        op_workspace_destroy(w);
+    """)
