@@ -316,6 +316,7 @@ class AdapterTable:
         self.entries, self.count, self.k, self.n, self.dtype = entries, count, k, n, dtype
         self.code = _DTYPES[str(dtype).replace("torch.", "")]
         self.address = C.addressof(entries)
+        self.max_rank = max(entries[i].rank for i in range(count))
 
 
 def adapter_table(a, b, scale, grad_a=None, grad_b=None) -> AdapterTable:
@@ -364,13 +365,23 @@ def _rows_of(x, rows: int, width: int, dtype, name: str):
     return x.data_ptr(), (ld if rows > 1 else max(width, ld))
 
 
-def _kept_rows(h, rows: int):
+def _kept_rows(h, rows: int, tab, batch, backward: bool):
+    """Address and row stride of h, which has a column for every rank of the adapters that the call uses it for."""
     if h is None:
         return None, 0
     _dtype_code(h, (DTYPE_FP32,), "h")
     if h.dim() != 2 or h.shape[0] != rows or (h.shape[1] > 1 and h.stride(1) != 1):
         raise ValueError("h must be a float32 matrix of %d contiguous rows" % rows)
-    return h.data_ptr(), (h.stride(0) if rows > 1 else max(h.shape[1], h.stride(0)))
+    width = h.shape[1]
+    if width < tab.max_rank:            # (the library sees the stride alone, which may be a wider matrix's)
+        lengths, which = batch
+        used = (tab.entries[a] for a in set(which[lengths > 0].tolist()) if 0 <= a < tab.count)
+        need = max([e.rank for e in used if not backward or e.grad_b] or [0])
+        if width < need:
+            raise CondensaError(ERR_INVALID_ARG, "h has %d columns, the adapters' ranks go to %d" % (width, need))
+        if need == 0:
+            return h.data_ptr(), max(width, h.stride(0))
+    return h.data_ptr(), (h.stride(0) if rows > 1 else width)
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -523,7 +534,7 @@ class Context:
         batch, keep = self._adapter_batch(tab, request_rows, request_adapter, m)
         px, ldx = _rows_of(x, m, tab.k, tab.dtype, "x")
         py, ldy = _rows_of(y, m, tab.n, tab.dtype, "y")
-        ph, ldh = _kept_rows(h, m)
+        ph, ldh = _kept_rows(h, m, tab, keep, False)
         self._check(self._lib.condensa_adapter_forward(self._h, C.byref(batch), px, ldx, py, ldy, ph, ldh, _stream_handle(stream)))
 
     def adapter_backward(self, tab: AdapterTable, request_rows, request_adapter, x, dy, h=None, dx=None, accumulate=False, stream=None):
@@ -534,7 +545,7 @@ class Context:
         px, ldx = _rows_of(x, m, tab.k, tab.dtype, "x")
         pdy, lddy = _rows_of(dy, m, tab.n, tab.dtype, "dy")
         pdx, lddx = _rows_of(dx, m, tab.k, tab.dtype, "dx")
-        ph, ldh = _kept_rows(h, m)
+        ph, ldh = _kept_rows(h, m, tab, keep, True)
         self._check(self._lib.condensa_adapter_backward(self._h, C.byref(batch), px, ldx, pdy, lddy, ph, ldh, pdx, lddx,
                                                         1 if accumulate else 0, _stream_handle(stream)))
 

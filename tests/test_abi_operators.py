@@ -79,3 +79,62 @@ def test_host_arrays_of_requests():
     assert cstep._host_array(x, cstep._INT64) is x
     assert cstep._host_array([1, 2], cstep._INT32).dtype == np.int32
     assert cstep._host_array(x[::2], cstep._INT64).flags.c_contiguous
+
+
+class _Recorder:
+    """Stands in for the library: keeps the calls, launches nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or 0
+
+
+def _context():
+    from paper_1911_02497_b200 import cstep
+    ctx = cstep.Context.__new__(cstep.Context)
+    ctx._lib, ctx._h = _Recorder(), None
+    return ctx
+
+
+def _adapter_calls(ctx, tab, rows, which, h):
+    """Both calls with this h; the row stride of h that each passed on."""
+    import torch
+    m = int(sum(rows))
+    x, y = (torch.zeros(m, w, dtype=torch.float16) for w in (tab.k, tab.n))
+    ctx._lib.calls.clear()
+    ctx.adapter_forward(tab, rows, which, x, y, h)
+    ctx.adapter_backward(tab, rows, which, x, y, h, torch.zeros_like(x))
+    (_, f), (_, b) = ctx._lib.calls
+    return f[7], b[7]
+
+
+def test_h_narrower_than_the_ranks_is_refused_before_the_library_is_called():
+    """A view of few columns has the row stride of the matrix that it was taken from, which says nothing of its width."""
+    import torch
+    from paper_1911_02497_b200 import cstep
+    ranks, k, n = [4, 8, 100], 64, 48
+    a, b = [torch.zeros(r, k).half() for r in ranks], [torch.zeros(n, r).half() for r in ranks]
+    tab = cstep.adapter_table(a, b, [1.0] * 3, [torch.zeros(r, k) for r in ranks], [torch.zeros(n, r) for r in ranks])
+    big, ctx = torch.zeros(5, 64), _context()
+    for rows, which, h in (([3, 2], [0, 1], big[:, :4]), ([3, 2], [0, 1], big[:, 57:]), ([3, 2], [0, 1], torch.zeros(5, 4)),
+                           ([1], [1], big[:1, :4]), ([1], [1], torch.zeros(1, 64)[:, 60:]), ([1, 0, 4], [0, 2, 2], big)):
+        ctx._lib.calls.clear()
+        x, y = (torch.zeros(sum(rows), w).half() for w in (k, n))
+        for call in (lambda: ctx.adapter_forward(tab, rows, which, x, y, h), lambda: ctx.adapter_backward(tab, rows, which, x, y, h)):
+            with pytest.raises(cstep.CondensaError) as e:
+                call()
+            assert e.value.code == cstep.ERR_INVALID_ARG
+        assert not ctx._lib.calls
+    # as wide as the adapters that have rows is enough
+    assert _adapter_calls(ctx, tab, [3, 2], [0, 1], big[:, :8]) == (64, 64)
+    assert _adapter_calls(ctx, tab, [3, 0, 2], [0, 2, -1], big[:, :4]) == (64, 64)
+    assert _adapter_calls(ctx, tab, [1], [1], big[:1, :8])[0] >= 8
+    assert _adapter_calls(ctx, tab, [3, 2], [0, 1], None) == (0, 0)
+    # backward reads h for the gradients of B alone
+    tab = cstep.adapter_table(a, b, [1.0] * 3, [torch.zeros(r, k) for r in ranks])
+    x, y = torch.zeros(5, k).half(), torch.zeros(5, n).half()
+    ctx._lib.calls.clear()
+    ctx.adapter_backward(tab, [3, 2], [0, 1], x, y, big[:, :4])
+    assert len(ctx._lib.calls) == 1
