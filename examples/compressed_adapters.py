@@ -2,8 +2,8 @@
 
 A gate projection of the 1500-wide LSTM language model (1500 -> 6000) is pruned and rounded to bfloat16 by one C-step and
 stays as it is. What it lost is trained back with low-rank adapters beside it, one per task, all tasks in one batch: forward,
-gradients, the norm that clips them, an AdamW step with 8-bit states that also writes the bfloat16 copies which the next
-forward pass reads. At the end a decoding step serves the tasks' requests, a token each, with and without an adapter.
+gradients, the norm that clips them, an AdamW step with 8-bit states (rounded by chance, from a seed) that also writes the
+bfloat16 copies which the next forward pass reads. At the end a decoding step serves the tasks' requests, a token each, with and without an adapter.
 
     python examples/compressed_adapters.py [steps]
 """
@@ -69,7 +69,7 @@ def train(steps=150, tasks=3, rank=16, k=1500, n=6000, rows=256, seed=0, lr=4e-3
         dy = (miss * (2.0 / rows)).bfloat16()
         ctx.adapter_backward(ad.table, length, which, x, dy, h, stream=stream)
         ctx.grad_norm(ad.optimizer, 0.0, 10.0, ad.clip, stream=stream)
-        ctx.lstep_adamw(ad.optimizer, lr=lr, weight_decay=0.0, step=step, clip=ad.clip, stream=stream)
+        ctx.lstep_adamw(ad.optimizer, lr=lr, weight_decay=0.0, step=step, clip=ad.clip, state_seed=seed + 1, stream=stream)
     # a decoding step: a token per request, in any order, one of them without an adapter
     which = np.array([t % tasks for t in range(4 * tasks)] + [-1], dtype=np.int32)
     length = np.ones(len(which), dtype=np.int64)

@@ -304,11 +304,24 @@ CONDENSA_API int condensa_lstep_update(condensa_ctx *ctx, const condensa_opt_ten
  * States in 8 bits (state_dtype CONDENSA_DTYPE_FP8_E4M3): m and r = sqrt(v) are held as E4M3 codes in
  * blocks of CONDENSA_STATE_BLOCK elements (counted from the tensor's start; the last may be shorter)
  * under one fp32 power of two each: scale = 2^(e-7), e the exponent of the block's largest finite
- * magnitude, at least 2^-126; code = E4M3(x / scale), round to nearest even. A positive r never
- * becomes 0 (its code is at least 1, i.e. scale * 2^-9), so that a small second moment cannot turn into a
- * division by eps; a value that is not finite becomes NaN. w' is formed from m' and r' before they
- * are rounded, its quotient to within 2 units in the last place. Zero states are zero bytes with any
- * finite scale. */
+ * magnitude, at least 2^-126; code = E4M3(x / scale). A positive r never becomes 0 (its code is at
+ * least 1, i.e. scale * 2^-9), so that a small second moment cannot turn into a division by eps; a
+ * value that is not finite becomes NaN. w' is formed from m' and r' before they are rounded, its
+ * quotient to within 2 units in the last place. Zero states are zero bytes with any finite scale.
+ * How a code is rounded is state_seed's to say:
+ *   state_seed != 0: by chance, up or down in proportion to the distance. This is the one to train with: over
+ *     many steps the moments keep the mean that 32-bit states have (r a little more: up to 3 % at
+ *     rest). 16 random bits b per code come from a hash, so equal calls give equal bits: with F(z) the
+ *     output function of splitmix64 (z ^= z>>30; z *= 0xBF58476D1CE4E5B9; z ^= z>>27;
+ *     z *= 0x94D049BB133111EB; z ^= z>>31), element i of tensor t of the list has
+ *     Z = F( F( F( F(state_seed) ^ step ) ^ t ) ^ (i/2) ), its m bits 16*(i%2) and up, its r bits
+ *     32 + 16*(i%2) and up. With y = |x / scale| (a positive r: at least 2^-9), q = 2^-6 where y < 2^-6, else 0: the fp32
+ *     pattern of y + q, plus 16*b + 8, has its low 20 bits cleared; less q, that is the code's magnitude.
+ *   state_seed == 0: to nearest even. One step is the best that a code can hold, but the moments do NOT follow
+ *     the gradients over many: a value that a step changes by less than half a code's step (3 to 6 %)
+ *     stays where it was, and a step lets r fall by sqrt(beta2) at most (0.05 % for 0.999). r then only ever
+ *     rises within its block, or stalls far below its value. For single steps, and for states that
+ *     have to be the same on every rounding of the same value. */
 #define CONDENSA_STATE_BLOCK 256
 enum { CONDENSA_DTYPE_FP32 = 0 };
 
@@ -332,7 +345,7 @@ typedef struct {
     int32_t grad_dtype;     /* CONDENSA_DTYPE_FP32, _FP16 or _BF16                                 */
     int32_t state_dtype;    /* CONDENSA_DTYPE_FP32 or _FP8_E4M3                                    */
     int32_t w_h_dtype;      /* CONDENSA_DTYPE_FP16 or _BF16; read where a w_h is given             */
-    int32_t reserved;       /* 0                                                                   */
+    uint32_t state_seed;    /* rounding of 8-bit states: a seed (by chance), 0 (to nearest)        */
 } condensa_adamw;
 
 /* What condensa_grad_norm() leaves on the device. */

@@ -105,28 +105,29 @@ int set_items(condensa_ctx *ctx, ListDesc *d, int T, int grid_max, ListScalars &
     return CONDENSA_OK;
 }
 
-template <int CAP, int GT, bool EIGHT, bool PEN>
+template <int CAP, int GT, int STATES, bool PEN>
 void launch_adamw(const ListScalars &s, const ListDesc *d, int grid, cudaStream_t stream)
 {
     ListParams<CAP> P;
     P.s = s;
     memcpy(P.d, d, sizeof(ListDesc) * (size_t)s.T);
-    k_adamw<CAP, GT, EIGHT, PEN><<<grid, THREADS, 0, stream>>>(P);
+    k_adamw<CAP, GT, STATES, PEN><<<grid, THREADS, 0, stream>>>(P);
 }
 
 template <int CAP, int GT>
-void launch_adamw_of(bool eight, bool pen, const ListScalars &s, const ListDesc *d, int grid, cudaStream_t stream)
+void launch_adamw_of(int states, bool pen, const ListScalars &s, const ListDesc *d, int grid, cudaStream_t stream)
 {
-    if (eight) pen ? launch_adamw<CAP, GT, true, true>(s, d, grid, stream) : launch_adamw<CAP, GT, true, false>(s, d, grid, stream);
-    else pen ? launch_adamw<CAP, GT, false, true>(s, d, grid, stream) : launch_adamw<CAP, GT, false, false>(s, d, grid, stream);
+    if (states == ST_8_NEAREST) pen ? launch_adamw<CAP, GT, ST_8_NEAREST, true>(s, d, grid, stream) : launch_adamw<CAP, GT, ST_8_NEAREST, false>(s, d, grid, stream);
+    else if (states == ST_8_STOCHASTIC) pen ? launch_adamw<CAP, GT, ST_8_STOCHASTIC, true>(s, d, grid, stream) : launch_adamw<CAP, GT, ST_8_STOCHASTIC, false>(s, d, grid, stream);
+    else pen ? launch_adamw<CAP, GT, ST_32, true>(s, d, grid, stream) : launch_adamw<CAP, GT, ST_32, false>(s, d, grid, stream);
 }
 
 template <int CAP>
-void launch_adamw_cap(int gt, bool eight, bool pen, const ListScalars &s, const ListDesc *d, int grid, cudaStream_t stream)
+void launch_adamw_cap(int gt, int states, bool pen, const ListScalars &s, const ListDesc *d, int grid, cudaStream_t stream)
 {
-    if (gt == GT_F32) launch_adamw_of<CAP, GT_F32>(eight, pen, s, d, grid, stream);
-    else if (gt == GT_F16) launch_adamw_of<CAP, GT_F16>(eight, pen, s, d, grid, stream);
-    else launch_adamw_of<CAP, GT_BF16>(eight, pen, s, d, grid, stream);
+    if (gt == GT_F32) launch_adamw_of<CAP, GT_F32>(states, pen, s, d, grid, stream);
+    else if (gt == GT_F16) launch_adamw_of<CAP, GT_F16>(states, pen, s, d, grid, stream);
+    else launch_adamw_of<CAP, GT_BF16>(states, pen, s, d, grid, stream);
 }
 
 template <int CAP, int GT, bool PEN>
@@ -160,7 +161,6 @@ int adamw(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float mu, c
     if (!(opt->beta1 >= 0.0f && opt->beta1 < 1.0f) || !(opt->beta2 >= 0.0f && opt->beta2 < 1.0f) || opt->step < 1 || !(opt->eps >= 0.0f) ||
         !std::isfinite(opt->eps))
         return fail(ctx, CONDENSA_ERR_INVALID_ARG, "AdamW needs 0 <= beta < 1, eps >= 0 and step >= 1");
-    if (opt->reserved != 0) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "reserved must be 0");
     if ((uintptr_t)clip % 4) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "clip is not 4-byte aligned");
     std::vector<ListDesc> d;
     bool pen = false;
@@ -183,15 +183,18 @@ int adamw(condensa_ctx *ctx, const condensa_adamw_tensor *ts, int T, float mu, c
     s.eps = opt->eps;
     s.clip = (const float *)clip;
     s.copy_type = opt->w_h_dtype;
-    const int per_sm = eight ? 4 : 3, grid_max = ctx->num_sms * per_sm;
+    s.key = mix64(mix64(opt->state_seed) ^ (u64)opt->step);
+    const int states = !eight ? ST_32 : opt->state_seed ? ST_8_STOCHASTIC : ST_8_NEAREST;
+    const int per_sm = adamw_ctas(states, pen), grid_max = ctx->num_sms * per_sm;
     for (int t0 = 0; t0 < T; t0 += LIST_LARGE) {
         const int n = std::min(T - t0, LIST_LARGE);
         if ((rc = set_items(ctx, d.data() + t0, n, grid_max, s)) != 0) return rc;
         if (s.n_items == 0) continue;
+        s.t0 = t0;
         const int grid = stream_grid(ctx, s.n_items, per_sm);
         const int pa_ = prof_begin(ctx, eight ? "k_adamw_8" : "k_adamw_32", stream);
-        if (n <= LIST_SMALL) launch_adamw_cap<LIST_SMALL>(opt->grad_dtype, eight, pen, s, d.data() + t0, grid, stream);
-        else launch_adamw_cap<LIST_LARGE>(opt->grad_dtype, eight, pen, s, d.data() + t0, grid, stream);
+        if (n <= LIST_SMALL) launch_adamw_cap<LIST_SMALL>(opt->grad_dtype, states, pen, s, d.data() + t0, grid, stream);
+        else launch_adamw_cap<LIST_LARGE>(opt->grad_dtype, states, pen, s, d.data() + t0, grid, stream);
         LAUNCH_CHECK(ctx);
         prof_end(ctx, pa_, stream);
     }

@@ -20,6 +20,7 @@ constexpr int NORM_GRID_MAX = 640;       // CTAs of the norm
 constexpr int LIST_SMALL = 40, LIST_LARGE = 360;     // tensors whose descriptors fit 4 KB resp. 32 KB of parameters
 
 enum { GT_F32 = 0, GT_F16 = 1, GT_BF16 = 2 };        // CONDENSA_DTYPE_*
+enum { ST_32 = 0, ST_8_NEAREST = 1, ST_8_STOCHASTIC = 2 };   // moments, and how those in 8 bits are rounded
 
 struct ListDesc {
     float *w;
@@ -44,6 +45,8 @@ struct ListScalars {
     u32 n_items;
     int chunks;             // chunks of LIST_CHUNK elements per warp in a work item
     int copy_type;          // of w_h
+    int t0;                 // the launch's first tensor in the list
+    u64 key;                // of the call's random bits (stochastic rounding of the 8-bit states)
 };
 
 template <int CAP>
@@ -62,6 +65,12 @@ __device__ __forceinline__ int list_owner(const P &p, u32 item)
         if (p.d[mid].item0 <= item) lo = mid; else hi = mid - 1;
     }
     return lo;
+}
+
+// CTAs of k_adamw that an SM holds: four where 64 registers hold a step without spilling.
+__host__ __device__ constexpr int adamw_ctas(int states, bool penalty)
+{
+    return states == ST_32 || (states == ST_8_STOCHASTIC && penalty) ? 3 : 4;
 }
 
 // Eight values of a warp's chunk that this lane holds: elements 4l..4l+3 and 128+4l..128+4l+3,
@@ -234,10 +243,22 @@ __device__ __forceinline__ void decode(const u32 (&c)[2], float scale, Oct &o)
     }
 }
 
-// Codes of the warp's block, and its scale. A power of two: scaling is exact, and a floating code
-// loses nothing by it but one binade of its range. FLOOR: what is positive keeps a code of at least 1 (2^-9).
-template <bool FLOOR>
-__device__ __forceinline__ float encode(const Oct &o, u32 (&c)[2])
+// A scaled value (below 256 in magnitude) moved to the E4M3 value above or below it in magnitude, to the one above with
+// the probability of its fraction of the step between them: 16 random bits `b`, added (with half a unit more) below the
+// three bits of the significand that stay. Under 2^-6 the steps are those of that binade, which adding 2^-6 brings about.
+__device__ __forceinline__ float round_by_chance(float y, u32 b)
+{
+    const float a = fabsf(y), lift = a < 0x1p-6f ? 0x1p-6f : 0.0f;
+    const u32 t = (__float_as_uint(__fadd_rn(a, lift)) + ((b << 4) | 8u)) & 0xFFF00000u;
+    return copysignf(__fsub_rn(__uint_as_float(t), lift), y);
+}
+
+// Codes of the warp's block, and its scale. A power of two, so that scaling is exact. FLOOR: what is positive keeps a
+// code of at least 1 (2^-9). The code is the nearest one, or with CHANCE one of the two around the value
+// (`random`: two values' bits in a word). To nearest, a value that changes by less than half a step a call never moves: three
+// bits of significand make that 3 to 6 %, and sqrt(beta2) is far nearer to 1. By chance, the mean moves as it should.
+template <bool FLOOR, bool CHANCE>
+__device__ __forceinline__ float encode(const Oct &o, u32 (&c)[2], const u32 (&random)[4])
 {
     constexpr u32 INF = 0x7F800000u;
     u32 most = 0;
@@ -267,6 +288,10 @@ __device__ __forceinline__ float encode(const Oct &o, u32 (&c)[2])
                 if (a > 0.0f) x = fmaxf(x, 0x1p-9f);
                 if (b > 0.0f) y = fmaxf(y, 0x1p-9f);
             }
+            if (CHANCE) {
+                x = round_by_chance(x, random[2 * j + i] & 0xFFFFu);
+                y = round_by_chance(y, random[2 * j + i] >> 16);
+            }
             // the second source goes to the low byte
             asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q[i]) : "f"(y), "f"(x));
         }
@@ -292,10 +317,12 @@ __device__ __forceinline__ float total_gradient(const ListScalars &s, float gr, 
 // (fp32) or 4 + 16/256 (8 bits), copy 2: bound by memory, and every byte is moved once.
 // Measured on 135.9 M elements (shares of a plain copy's 6530 GB/s): fp32 gradients and moments with the penalty, 36 bytes
 // an element, 773 us (0.97); bfloat16 gradients and copies with 8-bit moments, 16 bytes, 401 us (0.83, with 79
-// instructions an element beside it). 1.9 M elements in 32 tensors: 9 us, a launch and one round of the CTAs.
-template <int CAP, int GT, bool EIGHT, bool PEN>
-__global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) k_adamw(const __grid_constant__ ListParams<CAP> P)
+// instructions an element beside it) to nearest and 589 us by chance (the hash and two roundings more, bound by
+// instructions). 1.9 M elements in 32 tensors: 9 us, a launch and one round of the CTAs.
+template <int CAP, int GT, int STATES, bool PEN>
+__global__ void __launch_bounds__(THREADS, adamw_ctas(STATES, PEN)) k_adamw(const __grid_constant__ ListParams<CAP> P)
 {
+    constexpr bool EIGHT = STATES != ST_32, CHANCE = STATES == ST_8_STOCHASTIC;
     const ListScalars &s = P.s;
     float coef = 1.0f;
     if (s.clip) {
@@ -306,6 +333,7 @@ __global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) k_adamw(const __grid_c
     for (u32 item = blockIdx.x; item < s.n_items; item += gridDim.x) {
         const int t = list_owner(P, item);
         const ListDesc &d = P.d[t];
+        const u64 key = CHANCE ? mix64(s.key ^ (u64)(s.t0 + t)) : 0;
         const long long first = ((long long)(item - d.item0) * s.chunks * WARPS + warp) * LIST_CHUNK;
         for (int k = 0; k < s.chunks; ++k) {
             const long long e0 = first + (long long)k * WARPS * LIST_CHUNK, left = d.numel - e0;
@@ -365,8 +393,17 @@ __global__ void __launch_bounds__(THREADS, EIGHT ? 4 : 3) k_adamw(const __grid_c
             if (d.w_h) store_copy(d.w_h + e0, w, s.copy_type, lane, left, vec);
             if (EIGHT) {
                 // (places past the tensor's end hold 0 or NaN, which leave the block's scale alone)
-                sm = encode<false>(m, cm);
-                sv = encode<true>(root, cv);
+                u32 rm[4] = {0, 0, 0, 0}, rv[4] = {0, 0, 0, 0};
+                if (CHANCE) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {       // 64 bits for two elements: elements 2i and 2i + 1 of the pair of quads
+                        const u64 z = mix64(key ^ (u64)((e0 + (i >> 1) * 128 + 4 * lane + 2 * (i & 1)) >> 1));
+                        rm[i] = (u32)z;
+                        rv[i] = (u32)(z >> 32);
+                    }
+                }
+                sm = encode<false, CHANCE>(m, cm, rm);
+                sv = encode<true, CHANCE>(root, cv, rv);
                 store_codes((uint8_t *)d.m + e0, cm, lane, left, vec);
                 store_codes((uint8_t *)d.v + e0, cv, lane, left, vec);
                 __syncwarp();                       // every lane has read the old scales

@@ -366,8 +366,8 @@ __device__ __forceinline__ void widen4(const unsigned short *h, const float *x, 
     }
 }
 
-// splitmix64 output function: position hash of the sampler.
-__device__ __forceinline__ u64 mix64(u64 z)
+// splitmix64 output function: position hash of the sampler, random bits of the 8-bit states.
+__host__ __device__ __forceinline__ u64 mix64(u64 z)
 {
     z ^= z >> 30; z *= 0xBF58476D1CE4E5B9ull;
     z ^= z >> 27; z *= 0x94D049BB133111EBull;

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import warnings
 from typing import Optional, Sequence
 
 import numpy as np
@@ -109,7 +110,7 @@ class Adamw(C.Structure):
     """Mirror of ``condensa_adamw``."""
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("weight_decay", C.c_float), ("grad_scale", C.c_float), ("step", C.c_int64),
-                ("grad_dtype", C.c_int32), ("state_dtype", C.c_int32), ("w_h_dtype", C.c_int32), ("reserved", C.c_int32)]
+                ("grad_dtype", C.c_int32), ("state_dtype", C.c_int32), ("w_h_dtype", C.c_int32), ("state_seed", C.c_uint32)]
 
 
 ADAPTER_MAX_RANK = 128
@@ -428,6 +429,8 @@ def noalloc_status():
 class Context:
     """Owns a ``condensa_ctx`` (workspace and descriptor cache of one device)."""
 
+    _told_rounding = False
+
     def __init__(self, device: int = 0, workspace_bytes: int = 0):
         self._lib = load()
         h = C.c_void_p()
@@ -505,9 +508,16 @@ class Context:
                                                     _stream_handle(stream)))
 
     def lstep_adamw(self, tab: AdamwTable, mu=0.0, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step=1,
-                    grad_scale=1.0, clip=None, stream=None):
-        """One AdamW step over the list. ``clip``: the device record of :meth:`grad_norm` (4 float32), or None."""
-        o = Adamw(lr, beta1, beta2, eps, weight_decay, grad_scale, step, tab.grad_dtype, tab.state_dtype, tab.w_h_dtype, 0)
+                    grad_scale=1.0, clip=None, stream=None, state_seed=0):
+        """One AdamW step over the list. ``clip``: the device record of :meth:`grad_norm` (4 float32), or None. ``state_seed``: 8-bit
+        states are rounded by chance with this seed (1 to 2^32 - 1; any number, the same for all steps), as training needs; with
+        0 to nearest, where moments do not follow the gradients over many steps (a warning says so once)."""
+        if not 0 <= state_seed < 1 << 32:
+            raise ValueError("state_seed must lie in 0 .. 2^32 - 1")
+        if not state_seed and step > 1 and tab.state_dtype == DTYPE_FP8_E4M3 and not self._told_rounding:
+            self._told_rounding = True
+            warnings.warn("8-bit moments rounded to nearest do not follow the gradients over many steps: pass a state_seed to train", stacklevel=2)
+        o = Adamw(lr, beta1, beta2, eps, weight_decay, grad_scale, step, tab.grad_dtype, tab.state_dtype, tab.w_h_dtype, state_seed)
         self._check(self._lib.condensa_lstep_adamw(self._h, tab.entries, tab.T, mu, C.byref(o), _addr(clip),
                                                    _stream_handle(stream)))
 
