@@ -292,6 +292,9 @@ CONDENSA_API int condensa_lstep_update(condensa_ctx *ctx, const condensa_opt_ten
  * (partial sums) the first time; both can be captured into a CUDA graph after one plain call.
  * Graphs stay valid when later calls outgrow that workspace: a block that a capture was given is
  * kept until condensa_destroy(), beside the larger one. No replay may follow condensa_destroy().
+ * A captured step keeps the numbers of its call: every replay uses the same lr, step (and with it the
+ * same bias corrections and the same random bits for 8-bit states), mu and grad_scale. For a run of steps make the
+ * call anew, or capture it with one step and no 8-bit states once the bias corrections are 1.
  *
  * Per element, in this order of single fp32 operations (`grad` widened to fp32 first):
  *     g = grad_scale * grad;    [theta given:  d = w - theta;  p = mu*d;  q = p - lambda;  g = g + q]

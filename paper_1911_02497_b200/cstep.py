@@ -511,7 +511,8 @@ class Context:
                     grad_scale=1.0, clip=None, stream=None, state_seed=0):
         """One AdamW step over the list. ``clip``: the device record of :meth:`grad_norm` (4 float32), or None. ``state_seed``: 8-bit
         states are rounded by chance with this seed (1 to 2^32 - 1; any number, the same for all steps), as training needs; with
-        0 to nearest, where moments do not follow the gradients over many steps (a warning says so once)."""
+        0 to nearest, where moments do not follow the gradients over many steps (a warning says so once). A captured call keeps
+        its ``lr``, ``step`` and seed in every replay."""
         if not 0 <= state_seed < 1 << 32:
             raise ValueError("state_seed must lie in 0 .. 2^32 - 1")
         if not state_seed and step > 1 and tab.state_dtype == DTYPE_FP8_E4M3 and not self._told_rounding:
