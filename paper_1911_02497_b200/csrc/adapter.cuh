@@ -414,6 +414,9 @@ struct AdGeom {
     // A and B, too, are loaded a step ahead; else half a step. (Short tiles, a decoding step's, are bound by latency
     // alone and leave registers to spare)
     static constexpr bool AHEAD = RP <= 32 || (TM == 16 && RP == 64);
+    // Tiles of the rank whose sums of a step are kept apart at a time: all, or two where registers are short (four at 64
+    // ranks spill 300 to 600 bytes, two under 140)
+    static constexpr int APART = RP <= 32 ? RP / 8 : 2;
     static constexpr int HP_STRIDE = RP + 4;                         // floats
     static constexpr int HP = (KW > 1 ? KW / 2 : 1) * TM * HP_STRIDE * 4;    // partial sums
     static constexpr int HO_STRIDE = RP * E + (RP * E == 32 ? 0 : 32);       // operand of the expansion: four rows meet all banks
@@ -510,35 +513,37 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
         }
         if (j0 + JH == JT) pw += NB * BLOCK;
     };
+    // The matrix instruction truncates its sums: those of a step (4 products in a row, fp32: 12) are kept apart and added with
+    // rounding, or the loss would grow with the width (9216 columns of one sign, rank 64, fp32: 1.2e-5 of the sum, so 9e-8; the time
+    // of a call changes by -3 to 3 %). JG tiles at a time, as registers allow.
     auto multiply = [&](const SrcX &x, const SrcW &w, int blocks, int j0) {
-        // the matrix instruction truncates its sums: at low ranks (whose registers suffice) a few steps' are kept
-        // apart and added with rounding
-        constexpr bool APART = RP <= 32;
-        float d[APART ? JT : 1][4];
+        constexpr int JG = G::APART < JH ? G::APART : JH;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            if (b >= blocks) break;
+        for (int jg = 0; jg < JH; jg += JG) {
+            if (j0 + jg >= 2 && (j0 + jg) * 8 >= r16) break;
+            float d[JG][4];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                FragA<T> a;
-                frag_a(a, x.x[b][0], x.x[b][1], t);
+            for (int b = 0; b < NB; ++b) {
+                if (b >= blocks) break;
 #pragma unroll
-                for (int j = 0; j < JH; ++j) {
-                    if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
-                    FragB<T> f;
-                    frag_b(f, t ? w.w[b][j].z : w.w[b][j].x, t ? w.w[b][j].w : w.w[b][j].y);
-                    if constexpr (!APART) mma_step(acc[j0 + j], a, f);
-                    else if (b == 0 && t == 0) mma_first(d[j], a, f);
-                    else mma_step(d[j], a, f);
+                for (int t = 0; t < 2; ++t) {
+                    FragA<T> a;
+                    frag_a(a, x.x[b][0], x.x[b][1], t);
+#pragma unroll
+                    for (int j = jg; j < jg + JG; ++j) {
+                        if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
+                        FragB<T> f;
+                        frag_b(f, t ? w.w[b][j].z : w.w[b][j].x, t ? w.w[b][j].w : w.w[b][j].y);
+                        if (b == 0 && t == 0) mma_first(d[j - jg], a, f);
+                        else mma_step(d[j - jg], a, f);
+                    }
                 }
             }
-        }
-        if constexpr (APART) {
 #pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                if (j >= 2 && j * 8 >= r16) break;
+            for (int j = jg; j < jg + JG; ++j) {
+                if (j0 + j >= 2 && (j0 + j) * 8 >= r16) break;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) acc[j][q] += d[j][q];
+                for (int q = 0; q < 4; ++q) acc[j0 + j][q] += d[j - jg][q];
             }
         }
     };

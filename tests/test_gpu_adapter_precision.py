@@ -1,0 +1,83 @@
+"""Errors of the adapters that do not show where terms cancel: sums of one sign, against 64 bits.
+
+The matrix instruction truncates its sums. Of the S products that follow one another in a sum, each loses at most 2^-23 of what
+has been summed by then, half of the whole on average: S * 2^-24 of the sum. What is kept apart so is added with rounding, at random
+signs. An fp32 operand is two TF32 parts, the second cut below 2^-22 of it: two operands and the product of both second parts are
+3 * 2^-22 at most. These losses all go one way, so they show in the mean over many results; the largest error has the rounded
+sums beside it (six standard deviations of N of them, each at most 2^-24)."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+PARTS = {"float32": 3 * 2.0 ** -22, "float16": 0.0, "bfloat16": 0.0}
+
+
+def _torch():
+    import torch
+    return torch
+
+
+@pytest.fixture()
+def ctx():
+    from paper_1911_02497_b200 import cstep
+    c = cstep.Context(0)
+    yield c
+    c.close()
+
+
+def matrix(rows, width, dtype, pad=0, low=0.5, high=1.0):
+    """Values of one sign on the device, rows ``pad`` elements apart and one element off where there is a ``pad``."""
+    torch = _torch()
+    off = 1 if pad else 0
+    room = torch.empty(off + rows * (width + pad), device="cuda", dtype=getattr(torch, dtype))
+    v = torch.as_strided(room, (rows, width), (width + pad, 1), off)
+    for i in range(0, rows, 4096):
+        part = v[i:i + 4096]
+        part.copy_(torch.rand(part.shape, device="cuda") * (high - low) + low)
+    return v
+
+
+def check(got, want, bias, largest, what):
+    r = (got.double() - want) / want
+    assert abs(float(r.mean())) <= bias, (what, float(r.mean()), bias)
+    assert float(r.abs().max()) <= largest, (what, float(r.abs().max()), largest)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("rank,pad", [(8, 0), (8, 1), (8, 4), (32, 0), (40, 0), (64, 2), (100, 0), (128, 0), (128, 3)])
+def test_h_of_a_wide_row(ctx, dtype, rank, pad):
+    """Whatever the rank and however the rows lie: rows enough that a CTA has the whole width of its tile."""
+    torch = _torch()
+    from paper_1911_02497_b200 import cstep
+    k, n, rows = 9216, 64, 19200
+    torch.manual_seed(rank + pad)
+    x, y, h = matrix(rows, k, dtype, pad), matrix(rows, n, dtype, pad), torch.zeros(rows, rank, device="cuda")
+    a, b = matrix(rank, k, dtype), matrix(n, rank, dtype)
+    ctx.adapter_forward(cstep.adapter_table([a], [b], [1.0]), [rows], [0], x, y, h)
+    torch.cuda.synchronize()
+    want = torch.cat([x[i:i + 4096].double() @ a.double().t() for i in range(0, rows, 4096)])
+    # a step is at most 128 bytes of a row: 4 products of 16 terms, or 4 times 3 of 8
+    S = 12 if dtype == "float32" else 4
+    loss, sums = S * EPS + PARTS[dtype], k * x.element_size() / 64
+    check(h, want, loss + EPS / 4, 2 * loss + 6 * np.sqrt(sums) * EPS, (dtype, rank, pad))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+def test_h_does_not_depend_on_the_other_adapters_of_the_call(ctx, dtype):
+    """An adapter of rank 8 in a call with one of rank 128 is as exact as alone."""
+    torch = _torch()
+    from paper_1911_02497_b200 import cstep
+    k, n, rows = 9216, 64, 9600
+    torch.manual_seed(1)
+    x, y, h = matrix(2 * rows, k, dtype), matrix(2 * rows, n, dtype), torch.zeros(2 * rows, 128, device="cuda")
+    a, b = [matrix(r, k, dtype) for r in (8, 128)], [matrix(n, r, dtype) for r in (8, 128)]
+    ctx.adapter_forward(cstep.adapter_table(a, b, [1.0, 1.0]), [rows, rows], [0, 1], x, y, h)
+    torch.cuda.synchronize()
+    S = 12 if dtype == "float32" else 4
+    loss = S * EPS + PARTS[dtype]
+    for i in (0, 1):
+        at = slice(i * rows, (i + 1) * rows)
+        want = torch.cat([x[at][j:j + 4096].double() @ a[i].double().t() for j in range(0, rows, 4096)])
+        check(h[at][:, :a[i].shape[0]], want, loss + EPS / 4, 2 * loss + 6 * np.sqrt(k * x.element_size() / 64) * EPS, (dtype, i))
