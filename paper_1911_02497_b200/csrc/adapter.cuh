@@ -758,11 +758,16 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) load_h(hold[s][p], s, p);
     }
+    // (fp32, whose result is not rounded to 16 bits: the truncated sums of two steps, 6 products, are added with rounding)
+    constexpr int GROUP = E == 4 ? 2 : ST;
+    static_assert(SH % 2 == 0 || SH == ST, "whole groups");
     float d[NT][4];
     auto expand = [&](const DstB &x, int s0) {
+        float e[NT][4];
 #pragma unroll
         for (int s = 0; s < SH; ++s) {
             if (s0 + s && (s0 + s) * KSTEP >= r16) break;
+            const bool later = s0 + s >= GROUP, opens = (s0 + s) % GROUP == 0;
             FragB<T> b[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) frag_b(b[j], x.b[s][j].x, x.b[s][j].y);
@@ -773,9 +778,15 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
                 else load_h(a, s0 + s, p);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    if (s0 + s == 0 && p == PARTS - 1) mma_first(d[j], a, b[j]);
-                    else mma_step(d[j], a, b[j]);
+                    if (opens && p == PARTS - 1) mma_first(later ? e[j] : d[j], a, b[j]);
+                    else mma_step(later ? e[j] : d[j], a, b[j]);
                 }
+            }
+            if (later && (s0 + s) % GROUP == GROUP - 1) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) d[j][q] += e[j][q];
             }
         }
     };

@@ -81,3 +81,26 @@ def test_h_does_not_depend_on_the_other_adapters_of_the_call(ctx, dtype):
         at = slice(i * rows, (i + 1) * rows)
         want = torch.cat([x[at][j:j + 4096].double() @ a[i].double().t() for j in range(0, rows, 4096)])
         check(h[at][:, :a[i].shape[0]], want, loss + EPS / 4, 2 * loss + 6 * np.sqrt(k * x.element_size() / 64) * EPS, (dtype, i))
+
+
+@pytest.mark.parametrize("rank", [8, 16, 17, 32, 64, 100, 128])
+def test_expansion_in_fp32(ctx, rank):
+    """y = B h and dx = A^T u at ranks up to the largest, beside the h and u that they were formed from."""
+    torch = _torch()
+    from paper_1911_02497_b200 import cstep
+    k, n, rows = 64, 2048, 4096
+    torch.manual_seed(rank)
+    x, h = matrix(rows, k, "float32"), torch.zeros(rows, rank, device="cuda")
+    y, dy, dx = torch.zeros(rows, n, device="cuda"), matrix(rows, n, "float32"), torch.zeros(rows, k, device="cuda")
+    a, b, ga = matrix(rank, k, "float32"), matrix(n, rank, "float32"), torch.zeros(rank, k, device="cuda")
+    tab = cstep.adapter_table([a], [b], [1.0], [ga])
+    ctx.adapter_forward(tab, [rows], [0], x, y, h)
+    ctx.adapter_backward(tab, [rows], [0], x, dy, None, dx)
+    torch.cuda.synchronize()
+    S, sums = 6, rank / 16 + 1              # 3 products of 8 terms, twice, before a rounded sum; y and dx start at 0
+    most, mean = PARTS["float32"], 2.0 ** -22       # what is cut off an operand is half of the most on average, and 2 operands lose it
+    loss = S * EPS + mean
+    check(y, h.double() @ b.double().t(), loss, 2 * S * EPS + most + 6 * np.sqrt(sums) * EPS, ("y", rank))
+    u_loss = 12 * EPS + mean                # (u is not handed out: its own loss comes first)
+    want = (dy.double() @ b.double()) @ a.double()
+    check(dx, want, loss + u_loss + EPS, 2 * (S + 12) * EPS + 2 * most + 12 * np.sqrt(sums + n / 16) * EPS, ("dx", rank))
