@@ -863,7 +863,7 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
 // rows, 64 at a time; the CTAs that share an adapter's rows are a cluster and add their sums over distributed
 // shared memory, in order, so there are neither atomics nor a second launch. The coefficients are fp32 and the
 // results too, so they enter the products with their whole precision: three 16-bit parts in bfloat16, two in
-// binary16 under a power of two that follows the largest seen so far.
+// binary16 under a power of two per rank and tile.
 struct WgEntry {
     float *out[2];           // dA, dB; NULL: not formed
     float scale;
@@ -1128,21 +1128,26 @@ __device__ __forceinline__ void umma_f16(u32 d, u64 a, u64 b, u32 idesc, u32 add
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
 }
-// 16 columns of this warp's lanes of tensor memory; complete only behind tmem_ld_wait().
-__device__ __forceinline__ void tmem_ld16(u32 addr, float (&v)[16])
+// 8 or 16 columns of this warp's lanes of tensor memory; complete only behind tmem_ld_wait().
+__device__ __forceinline__ void tmem_ld(u32 addr, float (&v)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ld(u32 addr, float (&v)[16])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
                    "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]) : "r"(addr));
 }
-template <int N>
-__device__ __forceinline__ void tmem_ld_wait(float (&v)[N][16])
+template <int N, int C>
+__device__ __forceinline__ void tmem_ld_wait(float (&v)[N][C])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int s = 0; s < N; ++s)          // (no use of the values may move ahead of the wait)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) asm volatile("" : "+f"(v[s][i]));
+        for (int i = 0; i < C; ++i) asm volatile("" : "+f"(v[s][i]));
 }
 template <int N> __device__ __forceinline__ void bar_arrive(int id) { asm volatile("bar.arrive %0, %1;" :: "r"(id), "n"(N) : "memory"); }
 template <int N> __device__ __forceinline__ void bar_sync(int id) { asm volatile("bar.sync %0, %1;" :: "r"(id), "n"(N) : "memory"); }
@@ -1178,7 +1183,9 @@ struct WgGeom16 {
     static constexpr int CONV = SIDE ? R * 128 : PARTS * C_PART;       // one of two
     static constexpr int O_STRIDE = WC + 4;                            // floats: this CTA's sums, [rank][column]
     static constexpr int ROWS = 8 * R * 4;
-    static constexpr int FIXED = 2 * CONV + ROWS + 128;                // (the swizzled parts first)
+    // binary16: largest coefficients of a tile by rank (three tiles take turns), and the units that follow from them (two)
+    static constexpr int UNITS = std::is_same<T, __half>::value ? (3 + 2) * RP * 4 : 0;
+    static constexpr int FIXED = 2 * CONV + ROWS + 128 + UNITS;        // (the swizzled parts first)
     static constexpr int PAD = 1024;                                   // swizzle patterns start at multiples of 1024 bytes
     static constexpr int HALF_SM = 113 * 1024, WHOLE_SM = 227 * 1024;
     static constexpr int stages()
@@ -1194,6 +1201,10 @@ struct WgGeom16 {
     static constexpr int D = SIDE ? PARTS * RP : RP;                   // columns of an accumulator block
     static constexpr int TMEM = 4 * D <= 64 ? 64 : 4 * D <= 128 ? 128 : 4 * D <= 256 ? 256 : 512;    // two accumulators of two blocks
     static constexpr int CTAS = SMEM <= HALF_SM && TMEM <= 256 ? 2 : 1;
+    // Two CTAs of 64 ranks are short of registers: ranks are taken from tensor memory 8 at a time, not 16, and the next tile's
+    // coefficients are loaded behind that, not ahead of it (2777 rows of ranks 40 to 63: 91 -> 87 us for the call)
+    static constexpr bool SHORT = CTAS == 2 && RP == 64;
+    static constexpr int TAKE = SHORT ? 8 : 16;
     static constexpr int BLOCK = THREADS + 32;
     static_assert(SMEM <= WHOLE_SM && STAGE % 1024 == 0 && C_PART % 1024 == 0, "shared memory");
     static_assert(STAGES <= 3 || ROWS >= 4 * R * 4, "row numbers of four tiles");
@@ -1215,7 +1226,8 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
     int *srow = reinterpret_cast<int *>(conv + 2 * G::CONV);           // [8][R]
     u64 *bars = reinterpret_cast<u64 *>(reinterpret_cast<char *>(srow) + G::ROWS);
     u32 *s_tmem = reinterpret_cast<u32 *>(bars + 2);
-    float *smax = reinterpret_cast<float *>(s_tmem + 4);
+    u32 *smax = reinterpret_cast<u32 *>(bars + 16);                    // [3][rank], patterns of magnitudes
+    float *sunit = reinterpret_cast<float *>(smax + 3 * RP);           // [2][rank]
     const u32 ring = smem_u32(stages), conv_u = smem_u32(conv), bar = smem_u32(bars);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const WgPlace w = wg_place(P, G::WC);
@@ -1233,6 +1245,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         mbar_init(bar + 8, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (HALF && tid < RP) smax[tid] = 0;
 #pragma unroll
     for (int i = 0; i <= G::STAGES; ++i) wg_number_rows(w, srow, i, tid, THREADS);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -1344,26 +1357,36 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
 #pragma unroll
     for (int m = 0; m < RP; ++m) acc[m] = 0.0f;
     bool fine = true;
-    float unit = 1.0f, unit_before = 1.0f;       // binary16: the power of two that a tile's coefficients are divided by
-    auto collect = [&](int i, float f) {         // tile i's sums from tensor memory
+    int which = 0;                               // place of the tile's largest coefficients
+    auto collect = [&](int i) {                  // tile i's sums from tensor memory
         const u32 at = tmem + (u32)(i & 1) * (2 * G::D) + (u32)(warp >> 2) * G::D + ((u32)(warp & 3) << 21);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        constexpr int SUMS = G::SIDE ? PARTS : 1, CH = G::TAKE;
 #pragma unroll
-        for (int q = 0; q < RP / 16; ++q) {
-            if (q && q * 16 >= w.r16) break;
-            constexpr int SUMS = G::SIDE ? PARTS : 1;
-            float part[SUMS][16], t[16];
+        for (int q = 0; q < RP; q += CH) {
+            if (q && q >= w.r16) break;
+            float part[SUMS][CH], t[CH];
 #pragma unroll
-            for (int s = 0; s < SUMS; ++s) tmem_ld16(at + s * w.r16 + q * 16, part[s]);
+            for (int s = 0; s < SUMS; ++s) tmem_ld(at + s * w.r16 + q, part[s]);
             tmem_ld_wait(part);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {       // the parts' sums, smallest first
+            for (int e = 0; e < CH; ++e) {       // the parts' sums, smallest first
                 t[e] = part[SUMS - 1][e];
 #pragma unroll
                 for (int s = SUMS - 2; s >= 0; --s) t[e] += part[s][e];
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[q * 16 + e] = HALF ? fmaf(f, t[e], acc[q * 16 + e]) : acc[q * 16 + e] + t[e];
+            for (int e = 0; e < CH; e += 4) {
+                float *to = acc + q + e;
+                if constexpr (HALF) {
+                    const float4 u = *reinterpret_cast<const float4 *>(sunit + (i & 1) * RP + q + e);
+                    to[0] = fmaf(u.x, t[e], to[0]); to[1] = fmaf(u.y, t[e + 1], to[1]);
+                    to[2] = fmaf(u.z, t[e + 2], to[2]); to[3] = fmaf(u.w, t[e + 3], to[3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[j] += t[e + j];
+                }
+            }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     };
@@ -1376,26 +1399,46 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
     }
 #pragma unroll 1
     for (int i = 0; i < w.nt; ++i) {
-        float inv = 1.0f;
+        // binary16 has not fp32's range: each rank's coefficients of a tile are divided by a power of two of their own, so
+        // that two parts hold 22 bits of the largest, however the ranks differ (one is not finite: its rank's sums are not)
+        float inv[4] = {1.0f, 1.0f, 1.0f, 1.0f};
         if constexpr (HALF) {
-            float most = 0.0f;
+            float most[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < FN; ++j) most = fmaxf(most, fmaxf(fmaxf(fabsf(v[j].x), fabsf(v[j].y)), fmaxf(fabsf(v[j].z), fabsf(v[j].w))));
+            for (int j = 0; j < FN; ++j) {
+                const float x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
-            for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-            if (lane == 0) smax[(i & 1) * WARPS + warp] = most;
+                for (int e = 0; e < 4; ++e) most[e] = fmaxf(most[e], fabsf(x[e]));
+            }
+#pragma unroll
+            for (int o = 16; o >= FU; o >>= 1)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most[e] = fmaxf(most[e], __shfl_xor_sync(0xFFFFFFFFu, most[e], o));
+            u32 *at = smax + which * RP + fq;
+            which = which == 2 ? 0 : which + 1;
+            if (lane < FU)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) atomicMax(at + e, __float_as_uint(most[e]));
             bar_sync<THREADS>(5);
+            const uint4 all = *reinterpret_cast<const uint4 *>(at);
+            most[0] = __uint_as_float(all.x); most[1] = __uint_as_float(all.y); most[2] = __uint_as_float(all.z); most[3] = __uint_as_float(all.w);
+            // (the next tile's place: last read ahead of this barrier 5, added to behind the next barrier 3 or 4)
+            if (tid < RP) smax[which * RP + tid] = 0;
+            float unit[4];
 #pragma unroll
-            for (int q = 0; q < WARPS; ++q) most = fmaxf(most, smax[(i & 1) * WARPS + q]);
-            unit_before = unit;
-            unit = pow2_above(most);
-            inv = pow2_inverse(unit);
+            for (int e = 0; e < 4; ++e) {
+                unit[e] = pow2_above(most[e]);
+                inv[e] = pow2_inverse(unit[e]);
+            }
+            // (read behind the next barrier; written again behind the barrier 5 that follows the last reader)
+            if (tid < FU) *reinterpret_cast<float4 *>(sunit + (i & 1) * RP + fq) = make_float4(unit[0], unit[1], unit[2], unit[3]);
         }
         char *cv = conv + (i & 1) * G::CONV;
         if (has_f) {
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                float x0 = HALF ? v[j].x * inv : v[j].x, x1 = HALF ? v[j].y * inv : v[j].y, x2 = HALF ? v[j].z * inv : v[j].z, x3 = HALF ? v[j].w * inv : v[j].w;
+                float x0 = HALF ? v[j].x * inv[0] : v[j].x, x1 = HALF ? v[j].y * inv[1] : v[j].y;
+                float x2 = HALF ? v[j].z * inv[2] : v[j].z, x3 = HALF ? v[j].w * inv[3] : v[j].w;
 #pragma unroll
                 for (int s = 0; s < PARTS; ++s) {
                     uint2 p;
@@ -1408,17 +1451,18 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         cp_wait<G::STAGES - 2>();                                      // this thread's share of tile i is there
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the tensor core reads it)
         bar_arrive<G::BLOCK>(1 + (i & 1));
-        load_coef(i + 1);
+        if constexpr (!G::SHORT) load_coef(i + 1);
         // the tile before is complete: its buffers are free for the next copies, its sums can be taken
         if (i > 0) fine = mbar_wait(bar + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1) && fine;
         issue(i + G::STAGES - 1);
         cp_commit();
         bar_sync<G::BLOCK>(3 + (i & 1));                               // (the row numbers of tile i + STAGES are there)
-        if (i > 0) collect(i - 1, unit_before);
+        if (i > 0) collect(i - 1);
+        if constexpr (G::SHORT) load_coef(i + 1);
     }
     if (w.nt > 0) {
         fine = mbar_wait(bar + 8 * ((w.nt - 1) & 1), ((w.nt - 1) >> 1) & 1) && fine;
-        collect(w.nt - 1, unit);
+        collect(w.nt - 1);
     }
     cp_wait<0>();
     __syncthreads();

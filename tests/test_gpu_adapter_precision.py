@@ -104,3 +104,52 @@ def test_expansion_in_fp32(ctx, rank):
     u_loss = 12 * EPS + mean                # (u is not handed out: its own loss comes first)
     want = (dy.double() @ b.double()) @ a.double()
     check(dx, want, loss + u_loss + EPS, 2 * (S + 12) * EPS + 2 * most + 12 * np.sqrt(sums + n / 16) * EPS, ("dx", rank))
+
+
+def gradients(ctx, dtype, x, dy, a, b, h, scale=1.0):
+    torch = _torch()
+    from paper_1911_02497_b200 import cstep
+    rank, k, n = a.shape[0], a.shape[1], b.shape[0]
+    ga, gb = torch.zeros(rank, k, device="cuda"), torch.zeros(n, rank, device="cuda")
+    ctx.adapter_backward(cstep.adapter_table([a], [b], [scale], [ga], [gb]), [x.shape[0]], [0], x, dy, h)
+    torch.cuda.synchronize()
+    return ga, gb
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("rank,rows", [(4, 64), (16, 1000), (31, 130), (50, 700), (64, 64), (128, 300)])
+def test_gradients_of_ranks_that_differ_by_powers_of_two(ctx, dtype, rank, rows):
+    """Columns of B (which make u) and of h down to 2^-30 of one another: AdamW divides each by its own size."""
+    torch = _torch()
+    k, n = 264, 200
+    torch.manual_seed(rank)
+    size = 2.0 ** (10 - 10 * (torch.arange(rank, device="cuda") % 4).float())       # 2^10 .. 2^-20, as binary16 holds them
+    x, dy, a = matrix(rows, k, dtype), matrix(rows, n, dtype), matrix(rank, k, dtype)
+    # (values of B that binary16 holds exactly under every size: 1, 1.25 or 1.5, of 2^-20 too)
+    b = ((1 + 0.25 * torch.randint(0, 3, (n, rank), device="cuda")) * size).to(getattr(torch, dtype))
+    h = matrix(rows, rank, "float32") * size
+    ga, gb = gradients(ctx, dtype, x, dy, a, b, h)
+    u = dy.double() @ b.double()
+    # per sum: the row kernel's u (dA only), then tiles of 64 rows, 8 products of 16-bit parts in a row (fp32: 12) each
+    S, parts = (12, PARTS["float32"]) if dtype == "float32" else (12, 2.0 ** -21)
+    largest = 2 * 2 * S * EPS + 2 * parts + 6 * np.sqrt(rows / 32 + n / 16 + 16) * EPS
+    for name, got, want in (("dA", ga, u.t() @ x.double()), ("dB", gb, dy.double().t() @ h.double())):
+        check(got, want, 2 * S * EPS + parts, largest, (name, dtype, rank))
+
+
+@pytest.mark.parametrize("rank", [8, 24, 50, 100])
+def test_an_infinite_coefficient_leaves_the_other_ranks_alone(ctx, rank):
+    """binary16: beside it stand coefficients above 65504 and far below 6e-8."""
+    torch = _torch()
+    rows, k, n = 200, 72, 136
+    torch.manual_seed(rank)
+    x, dy, a, b = matrix(rows, k, "float16"), matrix(rows, n, "float16"), matrix(rank, k, "float16"), matrix(n, rank, "float16")
+    h = matrix(rows, rank, "float32") * 10.0 ** (6 - 6 * (torch.arange(rank, device="cuda") % 3).float())
+    bad = h.clone()
+    bad[70, 0] = float("inf")
+    _, want = gradients(ctx, "float16", x, dy, a, b, h)
+    _, got = gradients(ctx, "float16", x, dy, a, b, bad)
+    assert torch.isfinite(want).all() and not torch.isfinite(got[:, 0]).any()
+    assert torch.equal(got[:, 1:], want[:, 1:])
+    exact = dy.double().t() @ h.double()
+    check(want, exact, 12 * EPS + 2.0 ** -21, 24 * EPS + 2.0 ** -20 + 6 * np.sqrt(rows / 32 + 16) * EPS, rank)
