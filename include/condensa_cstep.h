@@ -395,7 +395,7 @@ CONDENSA_API int condensa_grad_norm(condensa_ctx *ctx, const condensa_adamw_tens
  * are exact and summed in fp32; h and u enter the second product as sums of two (gradients of
  * bfloat16: three) 16-bit parts, fp32 operands as two TF32 parts, so nothing is rounded to 16 bits but
  * the results. Parts in binary16, which has not fp32's range, are taken under a power of two: two of them hold 22 bits, and
- * nothing below 2^-25 of the largest coefficient of the row (y, dx) resp. of the rank in 64 rows (gradients). Sums run in an order that depends on the shapes, the requests and the device only.
+ * nothing below 2^-38 of the largest coefficient of the row (y, dx) resp. of the rank in 64 rows (gradients). Sums run in an order that depends on the shapes, the requests and the device only.
  * Rows do not mix: what is not finite in a row stays in its h, y and dx (and enters its adapter's
  * gradients); an infinity may come out as NaN.
  *

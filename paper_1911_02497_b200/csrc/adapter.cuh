@@ -250,11 +250,12 @@ __device__ __forceinline__ void split16(float x, u16 (&p)[PARTS])
     }
 }
 
-// Power of two whose inverse brings |x| <= most below 2 (1 where there is nothing to scale).
-__device__ __forceinline__ float pow2_above(float most)
+// Power of two whose inverse brings `most` into [2^13, 2^14): as far up as sums allow, since binary16 ends 2^-24 above zero. (1
+// where `most` is not finite; values below 2^-113 stay as far below 2^13.)
+__device__ __forceinline__ float pow2_unit(float most)
 {
     const u32 e = (__float_as_uint(most) >> 23) & 0xFFu;
-    return (e == 0u || e >= 254u) ? (e == 0u ? 1.1754943508222875e-38f : 1.0f) : __uint_as_float(e << 23);
+    return e == 255u ? 1.0f : __uint_as_float((max(e, 14u) - 13u) << 23);
 }
 __device__ __forceinline__ float pow2_inverse(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
 
@@ -716,7 +717,7 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
         if (std::is_same<T, __half>::value) {       // binary16 has not fp32's range: a power of two per row
 #pragma unroll
             for (int o = TPR / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-            const float p2 = pow2_above(most);
+            const float p2 = pow2_unit(most);
             inv = pow2_inverse(p2);
             if (sub == 0) sfac[r] = p2;
         }
@@ -1400,7 +1401,8 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
 #pragma unroll 1
     for (int i = 0; i < w.nt; ++i) {
         // binary16 has not fp32's range: each rank's coefficients of a tile are divided by a power of two of their own, so
-        // that two parts hold 22 bits of the largest, however the ranks differ (one is not finite: its rank's sums are not)
+        // that two parts hold 22 bits of it down to 2^-16 of the largest, however the ranks differ (one is not finite: its
+        // rank's sums are not)
         float inv[4] = {1.0f, 1.0f, 1.0f, 1.0f};
         if constexpr (HALF) {
             float most[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1427,7 +1429,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
             float unit[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                unit[e] = pow2_above(most[e]);
+                unit[e] = pow2_unit(most[e]);
                 inv[e] = pow2_inverse(unit[e]);
             }
             // (read behind the next barrier; written again behind the barrier 5 that follows the last reader)

@@ -153,3 +153,36 @@ def test_an_infinite_coefficient_leaves_the_other_ranks_alone(ctx, rank):
     assert torch.equal(got[:, 1:], want[:, 1:])
     exact = dy.double().t() @ h.double()
     check(want, exact, 12 * EPS + 2.0 ** -21, 24 * EPS + 2.0 ** -20 + 6 * np.sqrt(rows / 32 + 16) * EPS, rank)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("rows", [7, 300])
+@pytest.mark.parametrize("rank", [6, 30, 64, 100])
+def test_small_ranks_of_a_row_with_columns_of_their_own(ctx, dtype, rows, rank):
+    """h of some ranks 2^-10 and 2^-20 of the others'; each column of y hangs on ranks of one size alone, and so does dx."""
+    torch = _torch()
+    from paper_1911_02497_b200 import cstep
+    k = n = 240
+    torch.manual_seed(rank)
+    t = getattr(torch, dtype)
+    kind = torch.arange(rank, device="cuda") % 3
+    own = (torch.arange(n, device="cuda")[:, None] % 3 == kind[None, :]).float()
+    down, up = 2.0 ** (5 - 10 * kind.float()), 2.0 ** (10 * kind.float() - 12)
+    shrink, expand = (torch.rand(rank, k, device="cuda") * 0.5 + 0.5) * down[:, None], (torch.rand(n, rank, device="cuda") * 0.5 + 0.5) * up * own
+    x, h = matrix(rows, k, dtype), torch.zeros(rows, rank, device="cuda")
+    # forward with A = shrink, B = expand; backward with B^T = shrink, A^T = expand, so u takes h's part
+    a, b, y = shrink.to(t), expand.to(t), torch.zeros(rows, n, device="cuda", dtype=t)
+    ctx.adapter_forward(cstep.adapter_table([a], [b], [1.0]), [rows], [0], x, y, h)
+    at, bt, dx = expand.t().contiguous().to(t), shrink.t().contiguous().to(t), torch.zeros(rows, n, device="cuda", dtype=t)
+    ctx.adapter_backward(cstep.adapter_table([at], [bt], [1.0]), [rows], [0], x, x, None, dx)
+    torch.cuda.synchronize()
+    hw = x.double() @ a.double().t()
+    want = hw @ b.double().t()
+    # parts of h: 2^-16 (bfloat16) or 2^-21 of each, and 2^-38 of the row's largest in binary16; sums: S as above; one rounding to the type
+    part = {"float32": 2.0 ** -21, "float16": 2.0 ** -21, "bfloat16": 2.0 ** -16}[dtype]
+    floor = 2.0 ** -38 * hw.max(dim=1, keepdim=True).values * b.double().sum(dim=1)[None, :] if dtype == "float16" else 0.0
+    half = {"float32": EPS, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}[dtype]
+    allowed = (2 * part + 48 * EPS + half) * want + floor
+    for name, got in (("y", y), ("dx", dx)):
+        off = (got.double() - want).abs()
+        assert bool((off <= allowed).all()), (name, float((off / allowed).max()))
