@@ -397,7 +397,8 @@ CONDENSA_API int condensa_grad_norm(condensa_ctx *ctx, const condensa_adamw_tens
  * the results. Parts in binary16, which has not fp32's range, are taken under a power of two: two of them hold 22 bits, and
  * nothing below 2^-38 of the largest coefficient of the row (y, dx) resp. of the rank in 64 rows (gradients). Sums run in an order that depends on the shapes, the requests and the device only.
  * Rows do not mix: what is not finite in a row stays in its h, y and dx (and enters its adapter's
- * gradients); an infinity may come out as NaN.
+ * gradients); an infinity may come out as NaN. What rounds up to infinity in its first part counts as one: fp32
+ * operands of 2^128 - 2^116 or more in magnitude, and with bfloat16 coefficients (h, u) of 2^128 - 2^119 or more.
  *
  * The request lists and the adapter table are HOST arrays and are used up when the call returns.
  * Nothing is copied to the device ahead of the kernels (the lists travel as kernel parameters), so

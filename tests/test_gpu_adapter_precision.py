@@ -186,3 +186,29 @@ def test_small_ranks_of_a_row_with_columns_of_their_own(ctx, dtype, rows, rank):
     for name, got in (("y", y), ("dx", dx)):
         off = (got.double() - want).abs()
         assert bool((off <= allowed).all()), (name, float((off / allowed).max()))
+
+
+@pytest.mark.parametrize("dtype,top", [("float32", 0x7F7FEFFF), ("bfloat16", 0x7F7F7FFF), ("float16", 0x7F7FFFFF)])
+def test_values_at_the_top_of_fp32_that_are_still_numbers(ctx, dtype, top):
+    """The largest fp32 operand, and the largest h beside 16-bit operands, that the header calls a number; under a small factor."""
+    torch = _torch()
+    from paper_1911_02497_b200 import cstep
+    rows, k, n, rank = 70, 40, 24, 3
+    value = float(np.array([top], np.uint32).view(np.float32)[0])
+    t = getattr(torch, dtype)
+    a, b = torch.full((rank, k), 2.0 ** -8, device="cuda", dtype=t), torch.full((n, rank), 2.0 ** -8, device="cuda", dtype=t)
+    dy, h = torch.full((rows, n), 2.0 ** -8, device="cuda", dtype=t), torch.zeros(rows, rank, device="cuda")
+    h[:, 1], h[66] = -2.0, 0.25
+    h[:, 0] = torch.where(torch.arange(rows, device="cuda") == 66, value, 1.0)
+    x = torch.zeros(rows, k, device="cuda", dtype=t)
+    if dtype == "float32":
+        x[5, 7] = value
+        y, hx = torch.zeros(rows, n, device="cuda"), torch.zeros(rows, rank, device="cuda")
+        ctx.adapter_forward(cstep.adapter_table([a], [b], [1.0]), [rows], [0], x, y, hx)
+        torch.cuda.synchronize()
+        check(hx[5], torch.full((rank,), value * 2.0 ** -8, device="cuda").double(), 2.0 ** -21, 2.0 ** -21, "h")
+        check(y[5], torch.full((n,), 3 * value * 2.0 ** -16, device="cuda").double(), 2.0 ** -19, 2.0 ** -19, "y")
+        assert bool((y[:5] == 0).all()) and bool((y[6:] == 0).all())
+    _, gb = gradients(ctx, dtype, x, dy, a, b, h)
+    want = 2.0 ** -8 * h.double().sum(dim=0).expand(n, rank)
+    check(gb, want, 2.0 ** -19, 2.0 ** -19, "dB")
