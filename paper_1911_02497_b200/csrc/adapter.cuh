@@ -1455,8 +1455,9 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the tensor core reads it)
         bar_arrive<G::BLOCK>(1 + (i & 1));
         if constexpr (!G::SHORT) load_coef(i + 1);
-        // the tile before is complete: its buffers are free for the next copies, its sums can be taken
-        if (i > 0) fine = mbar_wait(bar + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1) && fine;
+        // the tile before is complete: its buffers are free for the next copies, its sums can be taken. (A wait that ran out
+        // makes the gradients no numbers; nothing more is waited for)
+        if (i > 0) fine = fine && mbar_wait(bar + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1);
         issue(i + G::STAGES - 1);
         cp_commit();
         bar_sync<G::BLOCK>(3 + (i & 1));                               // (the row numbers of tile i + STAGES are there)
@@ -1464,7 +1465,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         if constexpr (G::SHORT) load_coef(i + 1);
     }
     if (w.nt > 0) {
-        fine = mbar_wait(bar + 8 * ((w.nt - 1) & 1), ((w.nt - 1) >> 1) & 1) && fine;
+        fine = fine && mbar_wait(bar + 8 * ((w.nt - 1) & 1), ((w.nt - 1) >> 1) & 1);
         collect(w.nt - 1);
     }
     cp_wait<0>();
