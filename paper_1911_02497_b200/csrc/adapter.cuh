@@ -741,6 +741,7 @@ __global__ void __launch_bounds__(THREADS, AdGeom<T, TM, RP>::CTAS) k_adapter(co
             }
         }
     }
+    __syncwarp();               // (stores above diverge; the barrier wants whole warps)
     cluster_arrive();           // this CTA has read its peers' sums
     __syncthreads();
     // ---- expand: a lane has U neighbouring columns of each of its two rows
@@ -1265,6 +1266,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         int stage = 0;
 #pragma unroll 1
         for (int i = 0; i < w.nt; ++i) {
+            __syncwarp();
             bar_arrive<G::BLOCK>(3 + (i & 1));                         // (the row numbers of tile i + STAGES are there)
             bar_sync<G::BLOCK>(1 + (i & 1));
             if (lane == 0) {
@@ -1422,6 +1424,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
             if (lane < FU)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) atomicMax(at + e, __float_as_uint(most[e]));
+            __syncwarp();
             bar_sync<THREADS>(5);
             const uint4 all = *reinterpret_cast<const uint4 *>(at);
             most[0] = __uint_as_float(all.x); most[1] = __uint_as_float(all.y); most[2] = __uint_as_float(all.z); most[3] = __uint_as_float(all.w);
@@ -1453,6 +1456,7 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         }
         cp_wait<G::STAGES - 2>();                                      // this thread's share of tile i is there
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the tensor core reads it)
+        __syncwarp();                                                  // (barriers and tensor memory want whole warps: where lanes went apart they meet first)
         bar_arrive<G::BLOCK>(1 + (i & 1));
         if constexpr (!G::SHORT) load_coef(i + 1);
         // the tile before is complete: its buffers are free for the next copies, its sums can be taken. (A wait that ran out
@@ -1460,12 +1464,14 @@ __global__ void __launch_bounds__(THREADS + 32, WgGeom16<T, RP>::CTAS) k_adapter
         if (i > 0) fine = fine && mbar_wait(bar + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1);
         issue(i + G::STAGES - 1);
         cp_commit();
+        __syncwarp();
         bar_sync<G::BLOCK>(3 + (i & 1));                               // (the row numbers of tile i + STAGES are there)
         if (i > 0) collect(i - 1);
         if constexpr (G::SHORT) load_coef(i + 1);
     }
     if (w.nt > 0) {
         fine = fine && mbar_wait(bar + 8 * ((w.nt - 1) & 1), ((w.nt - 1) >> 1) & 1);
+        __syncwarp();
         collect(w.nt - 1);
     }
     cp_wait<0>();
