@@ -390,7 +390,8 @@ CONDENSA_API int condensa_grad_norm(condensa_ctx *ctx, const condensa_adamw_tens
  * fp32 and rounded once. Rows without an adapter are neither read nor written.
  *
  * x, y, dy, dx, A and B share one type (CONDENSA_DTYPE_FP32, _FP16, _BF16); h, dA and dB are fp32.
- * Rows may lie `ld` elements apart; A, B, dA and dB are contiguous. 16-byte alignment is fastest, 8 bytes
+ * Rows may lie `ld` elements apart, also beside another matrix of the call in one buffer (column slices, which share their
+ * row stride; otherwise an output may lie nowhere inside another's range); A, B, dA and dB are contiguous. 16-byte alignment is fastest, 8 bytes
  * next; anything less costs more. Products of 16-bit types
  * are exact and summed in fp32; h and u enter the second product as sums of two (gradients of
  * bfloat16: three) 16-bit parts, fp32 operands as two TF32 parts, so nothing is rounded to 16 bits but

@@ -13,13 +13,13 @@ OBJ = os.path.join(HERE, "build")
 API_H = os.path.join("..", "..", "include", "condensa_cstep.h")
 # each source with the headers it includes (they are compiled side by side)
 SOURCES = {
-    "api.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "elementwise.cuh", "select.cuh", "structured.cuh", "fused.cuh", "fused_fast.cuh",
+    "api.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "elementwise.cuh", "select.cuh", "structured.cuh", "fused.cuh", "fused_fast.cuh",
                "fused_blockg.cuh", "sample.cuh", "lstep.cuh", "thin.cuh", "small_select.cuh", "small_prune.cuh", API_H],
-    "adapter.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "adapter.cuh", "adapter_launch.cuh", API_H],
-    "adapter_bf16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
-    "adapter_f16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
-    "adapter_f32.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
-    "adamw.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "adamw.cuh", API_H],
+    "adapter.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adapter.cuh", "adapter_launch.cuh", API_H],
+    "adapter_bf16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
+    "adapter_f16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
+    "adapter_f32.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
+    "adamw.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adamw.cuh", API_H],
 }
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",

@@ -467,10 +467,12 @@ int run_wgrad(condensa_ctx *ctx, const condensa_adapter_batch *b, const Rows &ro
 // ------------------------------------------------------------------ calls
 struct Ranges {
     std::vector<Interval> iv;
+    std::vector<RowRange> rows;
     void add(const void *p, long long bytes, bool out)
     {
         if (p && bytes > 0) iv.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, out});
     }
+    bool clash() { return rows_clash(iv, rows); }
 };
 
 // A matrix of `rows` x `width` values: checked, and its range noted.
@@ -481,7 +483,7 @@ int take_rows(condensa_ctx *ctx, const char *name, const void *p, long long ld, 
     if ((uintptr_t)p % e) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "%s is not aligned to its type", name);
     if (ld < width) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "%s: rows of %lld values lie %lld apart", name, width, ld);
     if (ld > (1ll << 40)) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "%s: row stride above 2^40", name);
-    r.add(p, ((rows - 1) * ld + width) * e, out);
+    r.rows.push_back({(uintptr_t)p, (uintptr_t)(width * e), (uintptr_t)(ld * e), (uintptr_t)rows, out});
     return CONDENSA_OK;
 }
 
@@ -501,7 +503,7 @@ int forward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, l
         r.add(ad.a, (long long)ad.rank * b->k * e, false);
         r.add(ad.b, (long long)ad.rank * b->n * e, false);
     }
-    if (ranges_clash(r.iv)) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "an output buffer overlaps another buffer of the call");
+    if (r.clash()) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "an output buffer overlaps another buffer of the call");
     if (rows.live == 0) return CONDENSA_OK;
     CU_TRY(ctx, cudaSetDevice(ctx->device));
     const RowCall call = row_call(x, y, h, ldx, ldy, ldh, false, e);
@@ -546,7 +548,7 @@ int backward(condensa_ctx *ctx, const condensa_adapter_batch *b, const void *x, 
         r.add(ad.grad_a, (long long)ad.rank * b->k * 4, true);
         r.add(ad.grad_b, (long long)ad.rank * b->n * 4, true);
     }
-    if (ranges_clash(r.iv)) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "an output buffer overlaps another buffer of the call");
+    if (r.clash()) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "an output buffer overlaps another buffer of the call");
     CU_TRY(ctx, cudaSetDevice(ctx->device));
     const bool row_kernel = rows.live && (dx || need_a);
     Packed pk;

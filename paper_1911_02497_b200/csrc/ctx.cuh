@@ -12,6 +12,7 @@
 
 #include "common.cuh"
 #include "op_workspace.h"
+#include "ranges.h"
 
 using cs::Ctl;
 
@@ -86,11 +87,6 @@ inline int fail(condensa_ctx *c, int code, const char *fmt, ...)
     } while (0)
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-struct Interval {
-    uintptr_t lo, hi;
-    bool out;
-};
 
 inline int stream_grid(condensa_ctx *ctx, long long n_items, int occ)
 {
@@ -172,20 +168,6 @@ struct PdlLaunch {
             return fail(ctx, CONDENSA_ERR_CUDA, "kernel launch: %s", cudaGetErrorString(e_)); \
         ctx->launches += 1;                                                                  \
     } while (0)
-
-// An output range may overlap nothing else of the call. Sorts `iv`.
-inline bool ranges_clash(std::vector<Interval> &iv)
-{
-    auto before = [](const Interval &a, const Interval &b) { return a.lo < b.lo; };
-    if (!std::is_sorted(iv.begin(), iv.end(), before)) std::sort(iv.begin(), iv.end(), before);
-    uintptr_t reach = 0, reach_out = 0;
-    for (const Interval &i : iv) {
-        if (i.lo < reach_out || (i.out && i.lo < reach)) return true;
-        reach = std::max(reach, i.hi);
-        if (i.out) reach_out = std::max(reach_out, i.hi);
-    }
-    return false;
-}
 
 // Room for `bytes` in the operators' workspace (op_workspace.h); `use` lives to the end of the call.
 inline int op_workspace(condensa_ctx *ctx, size_t bytes, cudaStream_t stream, OpWorkspaceUse &use)

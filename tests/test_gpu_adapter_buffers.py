@@ -1,0 +1,43 @@
+"""Where the adapters' matrices may lie: slices of one buffer, and sizes that no buffer has."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture()
+def ctx():
+    from paper_1911_02497_b200 import cstep
+    c = cstep.Context(0)
+    yield c
+    c.close()
+
+
+def test_column_slices_of_one_buffer(ctx):
+    """x and y, dy and dx side by side in the rows of one buffer, as a fused projection writes them."""
+    import torch
+    from paper_1911_02497_b200 import cstep
+    m, k, n, r = 70, 64, 128, 8
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(0)
+    draw = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    a, b, wide, back = draw(r, k), draw(n, r), draw(m, k + n + 16), draw(m, k + n)
+    ga, gb = [[torch.zeros(s, device="cuda") for _ in range(2)] for s in ((r, k), (n, r))]
+    tabs = [cstep.adapter_table([a], [b], [0.5], [ga[i]], [gb[i]]) for i in (0, 1)]
+    x, y, dy, dx = wide[:, :k].clone(), wide[:, k:k + n].clone(), back[:, :n].clone(), back[:, n:].clone()
+    hs = [torch.zeros(m, r, device="cuda") for _ in range(2)]
+    rest = wide[:, k + n:].clone()
+    ctx.adapter_forward(tabs[0], [m], [0], x, y, hs[0])
+    ctx.adapter_backward(tabs[0], [m], [0], x, dy, hs[0], dx)
+    ctx.adapter_forward(tabs[1], [m], [0], wide[:, :k], wide[:, k:k + n], hs[1])
+    ctx.adapter_backward(tabs[1], [m], [0], wide[:, :k], back[:, :n], hs[1], back[:, n:])
+    torch.cuda.synchronize()
+    assert torch.equal(wide[:, :k], x) and torch.equal(wide[:, k:k + n], y) and torch.equal(wide[:, k + n:], rest)
+    assert torch.equal(back[:, :n], dy) and torch.equal(back[:, n:], dx) and torch.equal(hs[0], hs[1])
+    assert torch.equal(ga[0], ga[1]) and torch.equal(gb[0], gb[1])
+    launches = ctx.launch_count()
+    with pytest.raises(cstep.CondensaError) as e:            # a column in common
+        ctx.adapter_forward(tabs[1], [m], [0], wide[:, :k], wide[:, k - 1:k - 1 + n], hs[1])
+    assert e.value.code == cstep.ERR_INVALID_ARG and ctx.launch_count() == launches
