@@ -482,7 +482,8 @@ int take_rows(condensa_ctx *ctx, const char *name, const void *p, long long ld, 
     if (!p) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "%s is NULL", name);
     if ((uintptr_t)p % e) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "%s is not aligned to its type", name);
     if (ld < width) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "%s: rows of %lld values lie %lld apart", name, width, ld);
-    if (ld > (1ll << 40)) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "%s: row stride above 2^40", name);
+    if (width == 0) return CONDENSA_OK;          // (h where no row has an adapter)
+    if (ld > (1ll << 40) || rows - 1 > (1ll << 56) / ld) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "%s: %lld rows %lld apart leave the address space", name, rows, ld);
     r.rows.push_back({(uintptr_t)p, (uintptr_t)(width * e), (uintptr_t)(ld * e), (uintptr_t)rows, out});
     return CONDENSA_OK;
 }

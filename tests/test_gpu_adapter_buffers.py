@@ -41,3 +41,33 @@ def test_column_slices_of_one_buffer(ctx):
     with pytest.raises(cstep.CondensaError) as e:            # a column in common
         ctx.adapter_forward(tabs[1], [m], [0], wide[:, :k], wide[:, k - 1:k - 1 + n], hs[1])
     assert e.value.code == cstep.ERR_INVALID_ARG and ctx.launch_count() == launches
+
+
+def test_rows_that_leave_the_address_space_are_refused(ctx):
+    """Rows times stride beyond 63 bits must not wrap around in the overlap check."""
+    import torch
+    from paper_1911_02497_b200 import cstep
+    a, b = torch.zeros(4, 64, device="cuda").half(), torch.zeros(32, 4, device="cuda").half()
+    tab, some = cstep.adapter_table([a], [b], [1.0]), torch.zeros(4096, device="cuda")
+    length, which = np.array([(1 << 31) - 1], dtype=np.int64), np.zeros(1, dtype=np.int32)
+    batch = cstep.AdapterBatch(tab.address, 1, 1, length.ctypes.data, which.ctypes.data, int(length[0]), 64, 32, tab.code, 0)
+    launches, p = ctx.launch_count(), some.data_ptr()
+    for ldx, ldy in ((1 << 40, 32), (64, 1 << 40), (1 << 33, 1 << 33), ((1 << 40) + 1, 32)):
+        rc = ctx._lib.condensa_adapter_forward(ctx._h, C.byref(batch), p, ldx, p + 8192, ldy, None, 0, None)
+        assert rc == cstep.ERR_TOO_LARGE
+    assert ctx.launch_count() == launches
+
+
+def test_h_of_a_batch_without_adapters(ctx):
+    """No row has an adapter: h has no column to keep, whatever stride it is given with."""
+    import torch
+    from paper_1911_02497_b200 import cstep
+    a, b = torch.zeros(4, 64, device="cuda").half(), torch.zeros(32, 4, device="cuda").half()
+    tab, some = cstep.adapter_table([a], [b], [1.0]), torch.zeros(4096, device="cuda")
+    length, which = np.array([3], dtype=np.int64), np.full(1, -1, dtype=np.int32)
+    batch = cstep.AdapterBatch(tab.address, 1, 1, length.ctypes.data, which.ctypes.data, 3, 64, 32, tab.code, 0)
+    p = some.data_ptr()
+    for ldh in (0, 1, 64):
+        assert ctx._lib.condensa_adapter_forward(ctx._h, C.byref(batch), p, 64, p + 4096, 32, p + 8192, ldh, None) == cstep.OK
+    torch.cuda.synchronize()
+    assert bool((some == 0).all())
