@@ -425,7 +425,7 @@ typedef struct {
     int32_t n_requests;
     const int64_t *request_rows;        /* HOST: rows of each request, >= 0; they follow one another */
     const int32_t *request_adapter;     /* HOST: index into adapters, or -1                       */
-    int64_t rows;                       /* of the batch: the sum of request_rows                  */
+    int64_t rows;                       /* of the batch: the sum of request_rows, at most 2^31 - 64 */
     int64_t k, n;                       /* widths of x and y, 1 .. 2^22                           */
     int32_t dtype;
     int32_t reserved;                   /* 0                                                      */

@@ -8,6 +8,7 @@
 using namespace cs;
 
 static_assert(CONDENSA_ADAPTER_MAX_RANK == AD_MAX_RANK, "largest rank");
+static_assert(AD_WG_ROWS <= 64, "rows of a tile, in the limit of a batch");
 
 namespace {
 
@@ -53,7 +54,8 @@ int read_batch(condensa_ctx *ctx, const condensa_adapter_batch *b, Rows &rows)
         const int a = b->request_adapter[q];
         if (n < 0) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "request %d: negative rows", q);
         if (a < -1 || a >= b->n_adapters) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "request %d: no adapter %d", q, a);
-        if (n > 0x7FFFFFFFll - rows.total) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "a batch has fewer than 2^31 rows");
+        // (a tile's rows are counted in 32 bits past the last one)
+        if (n > (1ll << 31) - 64 - rows.total) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "a batch has at most 2^31 - 64 rows");
         if (n > 0 && a >= 0) {
             rows.live += n;
             place[a] += 1;

@@ -71,3 +71,19 @@ def test_h_of_a_batch_without_adapters(ctx):
         assert ctx._lib.condensa_adapter_forward(ctx._h, C.byref(batch), p, 64, p + 4096, 32, p + 8192, ldh, None) == cstep.OK
     torch.cuda.synchronize()
     assert bool((some == 0).all())
+
+
+def test_the_longest_batch(ctx):
+    """2^31 - 64 rows are taken (and then miss their x); one more is refused for its length: tiles count past the last row."""
+    import torch
+    from paper_1911_02497_b200 import cstep
+    a, b = torch.zeros(1, 1, device="cuda").half(), torch.zeros(1, 1, device="cuda").half()
+    tab, which = cstep.adapter_table([a], [b], [1.0]), np.zeros(2, dtype=np.int32)
+    launches, most = ctx.launch_count(), (1 << 31) - 64
+    for rows, code in (([most, 0], cstep.ERR_INVALID_ARG), ([most - 1, 1], cstep.ERR_INVALID_ARG), ([most, 1], cstep.ERR_TOO_LARGE),
+                       ([(1 << 31) - 1, 0], cstep.ERR_TOO_LARGE), ([1, 1 << 62], cstep.ERR_TOO_LARGE)):
+        length = np.array(rows, dtype=np.int64)
+        batch = cstep.AdapterBatch(tab.address, 1, 2, length.ctypes.data, which.ctypes.data, int(sum(rows)), 1, 1, tab.code, 0)
+        assert ctx._lib.condensa_adapter_forward(ctx._h, C.byref(batch), None, 1, None, 1, None, 0, None) == code
+        assert ctx._lib.condensa_adapter_backward(ctx._h, C.byref(batch), None, 1, None, 1, None, 0, None, 0, 0, None) == code
+    assert ctx.launch_count() == launches
