@@ -444,6 +444,103 @@ CONDENSA_API int condensa_adapter_backward(condensa_ctx *ctx, const condensa_ada
                                            const float *h, int64_t ldh, void *dx, int64_t lddx,
                                            int accumulate, void *stream);
 
+/* ---- Matrices in 8 bits with scales, the product of a compressed projection with them, and the norm ahead of it.
+ *
+ * An 8-bit matrix holds E4M3 codes in row-major order and a scale byte s, 1 .. 254, that stands for 2^(s-127), for every
+ * group of CONDENSA_CODE_GROUP elements: the value of a code is E4M3(code) * 2^(s-127). There are two forms.
+ *   rows    (activations, gradients) a group is 128 columns of one row, counted from column 0 (the last may be shorter);
+ *           scales [rows][ceil(cols/128)]
+ *   blocks  (weights) a group is a block of 128 x 128, counted from row 0 and column 0;
+ *           scales [ceil(rows/128)][ceil(cols/128)]
+ * The encoders take the least s for which no finite magnitude of the group exceeds 448 * 2^(s-127), and s = 1 where that
+ * is less than 1; code = E4M3 of value * 2^(127-s), to nearest even (the product is exact or far below the least code). A value that is not
+ * finite becomes the code of NaN and has no part in its group's scale. Scales being powers of two, only the code rounds.
+ *
+ * codes: 16-byte aligned, rows `ld` bytes apart, a multiple of 16 (a single row may have any multiple that holds it); bytes past
+ * the columns are neither read nor written. scales: 4-byte aligned, rows `ld_scales` bytes apart, a multiple of 4; the same. */
+#define CONDENSA_CODE_GROUP 128
+
+typedef struct {
+    uint8_t *codes;         /* [rows][ld]                                                          */
+    uint8_t *scales;        /* [groups of rows][ld_scales]                                         */
+    int64_t ld, ld_scales;
+} condensa_coded;
+
+/* x [rows][cols] of CONDENSA_DTYPE_FP32, _FP16 or _BF16, rows `ldx` elements apart, into the row form. */
+CONDENSA_API int condensa_encode_rows(condensa_ctx *ctx, const void *x, int64_t ldx, int64_t rows, int64_t cols,
+                                      int dtype, const condensa_coded *out, void *stream);
+
+/* w [n][k] (theta of a C-step, say) into the block form. theta (NULL: not written): the values that the codes stand for, fp32, so that
+ * condensa_cstep_lagrange_update() can go by what the codes hold; it may be w itself (dtype fp32, same stride). */
+CONDENSA_API int condensa_encode_blocks(condensa_ctx *ctx, const void *w, int64_t ldw, int64_t n, int64_t k, int dtype,
+                                        const condensa_coded *out, float *theta, int64_t ld_theta, void *stream);
+
+/* Products with a projection w [n][k] in block form, the other operand in row form:
+ *   forward   y[i][j]  = sum over l of x[i][l] * w[j][l]       x [rows][k], y [rows][n]
+ *   backward  dx[i][l] = sum over j of dy[i][j] * w[j][l]      dy [rows][n], dx [rows][k]
+ * Both read the one copy of the codes. The projection is what a C-step left and is not trained: there is no gradient to w.
+ * y and dx are overwritten, of CONDENSA_DTYPE_FP16 or _BF16, rows `ld` elements apart. Products of codes and their scales are
+ * exact; sums are formed in fp32 by the matrix instruction, which cuts instead of rounding (up to 2^-23 of the largest partial sum for
+ * every 32 terms), and are rounded once to the result. fp32 results are not offered for that reason. Rows do not mix: a NaN in a row
+ * stays in that row of the result. The order of a sum depends on the shapes and the device only.
+ * n and k at most 2^22, rows at most 2^31 - 256. No workspace is used. Any alignment of the result is taken; rows that are 16- or
+ * 8-byte aligned are faster. */
+typedef struct {
+    condensa_coded code;    /* block form, read only                                               */
+    int64_t n, k;
+} condensa_projection;
+
+CONDENSA_API int condensa_projection_forward(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x,
+                                             int64_t rows, void *y, int64_t ldy, int dtype, void *stream);
+CONDENSA_API int condensa_projection_backward(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *dy,
+                                              int64_t rows, void *dx, int64_t lddx, int dtype, void *stream);
+
+/* Root-mean-square norm of rows, with the addition of a residual ahead of it and results in 16 or 32 bits, in 8 bits, or both.
+ *   forward   h = x + residual, rounded to dtype       r_i = 1 / sqrt(mean over j of h_ij^2 + eps)
+ *             y_ij = h_ij * r_i * gain_j
+ *   backward  t_ij = dy_ij * gain_j      q_i = mean over j of t_ij * h_ij * r_i
+ *             dx_ij = dh_ij + r_i * (t_ij - h_ij * r_i * q_i)        (the gradient of x and of the residual alike)
+ *             dgain_j = sum over i of dy_ij * h_ij * r_i
+ * x, residual, h, y, dy, dh and dx share `dtype` (CONDENSA_DTYPE_FP32, _FP16, _BF16), gain has `gain_dtype` (CONDENSA_DTYPE_FP32 or
+ * dtype). Everything is formed in fp32 (a sum of squares beyond its range in fp64) and rounded once for each result, codes included. The gradient of a result in 8 bits is that of
+ * the value ahead of the rounding. Sums over a row and over rows run in an order that depends on the shape and the device
+ * only. An infinity in a row makes its place NaN and the row's other results 0, a NaN the whole row NaN. */
+typedef struct {
+    const void *x;          /* [rows][ldx]                                                         */
+    const void *residual;   /* [rows][ld_residual]; NULL: none                                     */
+    const void *gain;       /* [cols]; NULL: ones                                                  */
+    void *h;                /* out: [rows][ldh]; NULL: not written. May be x or residual itself    */
+    void *y;                /* out: [rows][ldy]; NULL: not written. May be x or residual itself    */
+    condensa_coded code;    /* out: y in row form; codes NULL: not written                         */
+    float *rstd;            /* out: r, [rows]; NULL: not written                                   */
+    int64_t ldx, ld_residual, ldh, ldy;
+    int64_t rows, cols;     /* rows at most 2^31 - 256, cols 1 .. 2^22                             */
+    float eps;              /* > 0                                                                 */
+    int32_t dtype, gain_dtype;
+    int32_t reserved;       /* 0                                                                   */
+} condensa_norm;
+
+typedef struct {
+    const void *dy;         /* [rows][ld_dy]: gradient of y                                        */
+    const void *dh;         /* [rows][ld_dh]: gradient that reaches h otherwise; NULL: none        */
+    const void *h;          /* [rows][ldh]: what forward left in h (x where there was no residual) */
+    const void *gain;       /* [cols]; NULL: ones                                                  */
+    const float *rstd;      /* [rows]                                                              */
+    void *dx;               /* out: [rows][ld_dx]; NULL: not written. May be dy or dh itself       */
+    condensa_coded code;    /* out: dx in row form; codes NULL: not written                        */
+    float *dgain;           /* out: [cols]; NULL: not formed                                       */
+    int64_t ld_dy, ld_dh, ldh, ld_dx;
+    int64_t rows, cols;
+    int32_t dtype, gain_dtype;
+    int32_t accumulate;     /* 0: dgain is overwritten, otherwise added to                         */
+    int32_t reserved;       /* 0                                                                   */
+} condensa_norm_gradient;
+
+/* Outputs may overlap nothing else of the call but as said above ("itself": the same address and stride). forward uses no
+ * workspace; backward does where dgain is formed: a captured call must not run while another call of the context runs. */
+CONDENSA_API int condensa_norm_forward(condensa_ctx *ctx, const condensa_norm *norm, void *stream);
+CONDENSA_API int condensa_norm_backward(condensa_ctx *ctx, const condensa_norm_gradient *norm, void *stream);
+
 /* Operation selector for condensa_cstep_host(). */
 enum { CONDENSA_OP_PRUNE = 0, CONDENSA_OP_FILTER = 1, CONDENSA_OP_BLOCK = 2,
        CONDENSA_OP_QUANTIZE = 3, CONDENSA_OP_LAGRANGE = 4 };

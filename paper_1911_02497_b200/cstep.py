@@ -34,7 +34,9 @@ EXPORTS = ["condensa_create", "condensa_destroy", "condensa_cstep_prune", "conde
            "condensa_cstep_structure", "condensa_thin_flags", "condensa_thin_compact",
            "condensa_count_nonzero", "condensa_set_seed", "condensa_noalloc_status",
            "condensa_cstep_structured", "condensa_workspace_bytes", "condensa_thin_list",
-           "condensa_lstep_adamw", "condensa_grad_norm", "condensa_adapter_forward", "condensa_adapter_backward"]
+           "condensa_lstep_adamw", "condensa_grad_norm", "condensa_adapter_forward", "condensa_adapter_backward",
+           "condensa_encode_rows", "condensa_encode_blocks", "condensa_projection_forward", "condensa_projection_backward",
+           "condensa_norm_forward", "condensa_norm_backward"]
 
 
 class CondensaError(RuntimeError):
@@ -128,6 +130,34 @@ class AdapterBatch(C.Structure):
                 ("request_adapter", C.c_void_p), ("rows", C.c_int64), ("k", C.c_int64), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
+CODE_GROUP = 128                # columns (and, in blocks, rows) that share a scale of an 8-bit matrix
+
+
+class CodedMatrix(C.Structure):
+    """Mirror of ``condensa_coded``."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64), ("ld_scales", C.c_int64)]
+
+
+class Projection(C.Structure):
+    """Mirror of ``condensa_projection``."""
+    _fields_ = [("code", CodedMatrix), ("n", C.c_int64), ("k", C.c_int64)]
+
+
+class Norm(C.Structure):
+    """Mirror of ``condensa_norm``."""
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("gain", C.c_void_p), ("h", C.c_void_p), ("y", C.c_void_p), ("code", CodedMatrix),
+                ("rstd", C.c_void_p), ("ldx", C.c_int64), ("ld_residual", C.c_int64), ("ldh", C.c_int64), ("ldy", C.c_int64), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("eps", C.c_float), ("dtype", C.c_int32), ("gain_dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class NormGradient(C.Structure):
+    """Mirror of ``condensa_norm_gradient``."""
+    _fields_ = [("dy", C.c_void_p), ("dh", C.c_void_p), ("h", C.c_void_p), ("gain", C.c_void_p), ("rstd", C.c_void_p), ("dx", C.c_void_p),
+                ("code", CodedMatrix), ("dgain", C.c_void_p), ("ld_dy", C.c_int64), ("ld_dh", C.c_int64), ("ldh", C.c_int64), ("ld_dx", C.c_int64),
+                ("rows", C.c_int64), ("cols", C.c_int64), ("dtype", C.c_int32), ("gain_dtype", C.c_int32), ("accumulate", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 class KernelTime(C.Structure):
     """Mirror of ``condensa_kernel_time``."""
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int64), ("total_ms", C.c_double)]
@@ -172,6 +202,13 @@ def load():
     L.condensa_grad_norm.argtypes = [vp, vp, i32, f32, i32, f32, f32, vp, vp, vp]
     L.condensa_adapter_forward.argtypes = [vp, C.POINTER(AdapterBatch), vp, i64, vp, i64, vp, i64, vp]
     L.condensa_adapter_backward.argtypes = [vp, C.POINTER(AdapterBatch), vp, i64, vp, i64, vp, i64, vp, i64, i32, vp]
+    pc = C.POINTER(CodedMatrix)
+    L.condensa_encode_rows.argtypes = [vp, vp, i64, i64, i64, i32, pc, vp]
+    L.condensa_encode_blocks.argtypes = [vp, vp, i64, i64, i64, i32, pc, vp, i64, vp]
+    L.condensa_projection_forward.argtypes = [vp, C.POINTER(Projection), pc, i64, vp, i64, i32, vp]
+    L.condensa_projection_backward.argtypes = [vp, C.POINTER(Projection), pc, i64, vp, i64, i32, vp]
+    L.condensa_norm_forward.argtypes = [vp, C.POINTER(Norm), vp]
+    L.condensa_norm_backward.argtypes = [vp, C.POINTER(NormGradient), vp]
     L.condensa_launch_count.argtypes = [vp]
     L.condensa_launch_count.restype = C.c_int64
     L.condensa_last_error.argtypes = [vp]
@@ -385,6 +422,45 @@ def _kept_rows(h, rows: int, tab, batch, backward: bool):
     return h.data_ptr(), (h.stride(0) if rows > 1 else width)
 
 
+class Coded:
+    """An 8-bit matrix: E4M3 codes [rows, cols] and their scale bytes, as the encoders, the norm and the projection take it. Made by
+    :func:`coded_rows` or :func:`coded_blocks`; the buffers are kept alive."""
+
+    def __init__(self, codes, scales, high: int):
+        if codes.dim() != 2 or scales.dim() != 2:
+            raise ValueError("codes and scales must be matrices")
+        if str(codes.dtype) not in ("torch.float8_e4m3fn", "torch.uint8") or str(scales.dtype) not in ("torch.uint8", "torch.float8_e8m0fnu"):
+            raise TypeError("codes must be float8_e4m3fn or uint8, scales uint8 or float8_e8m0fnu")
+        self.rows, self.cols = (int(n) for n in codes.shape)
+        groups = -(-self.cols // CODE_GROUP)
+        want = (-(-self.rows // high), groups)
+        if tuple(scales.shape) != want:
+            raise ValueError("codes of shape %s need scales of shape %s" % (tuple(codes.shape), want))
+        if (self.cols > 1 and codes.stride(1) != 1) or (groups > 1 and scales.stride(1) != 1):
+            raise ValueError("the rows of codes and scales must be contiguous")
+        if codes.get_device() != scales.get_device():
+            raise ValueError("codes and scales must be on one device")
+        ld = codes.stride(0) if self.rows > 1 else -(-self.cols // 16) * 16
+        ld_scales = scales.stride(0) if want[0] > 1 else -(-groups // 4) * 4
+        if self.rows > 0 and (ld % 16 or codes.data_ptr() % 16 or ld_scales % 4 or scales.data_ptr() % 4):
+            raise ValueError("codes must be 16-byte aligned with rows a multiple of 16 bytes apart, scales 4-byte aligned with rows a multiple of 4 bytes apart")
+        self.codes, self.scales, self.high, self.device = codes, scales, high, codes.get_device()
+        self.struct = CodedMatrix(codes.data_ptr(), scales.data_ptr(), ld, ld_scales)
+        self.projection = Projection(self.struct, self.rows, self.cols) if high > 1 else None
+
+
+def coded_rows(codes, scales) -> Coded:
+    """Activations or gradients in 8 bits: ``codes`` [rows, cols] float8_e4m3fn or uint8 with rows a multiple of 16 bytes apart, ``scales``
+    [rows, ceil(cols / 128)] uint8 with rows a multiple of 4 bytes apart (slices of wider buffers: ``torch.empty(rows, -(-cols // 16) *
+    16)[:, :cols]``)."""
+    return Coded(codes, scales, 1)
+
+
+def coded_blocks(codes, scales) -> Coded:
+    """The weights of a projection in 8 bits: ``codes`` [n, k], ``scales`` [ceil(n / 128), ceil(k / 128)]; strides as in :func:`coded_rows`."""
+    return Coded(codes, scales, CODE_GROUP)
+
+
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         return None
@@ -437,7 +513,7 @@ class Context:
         rc = self._lib.condensa_create(C.byref(h), int(device), int(workspace_bytes))
         if rc != OK:
             raise CondensaError(rc, (self._lib.condensa_last_error(None) or b"").decode())
-        self._h = h
+        self._h, self.device = h, int(device)
 
     def close(self):
         if getattr(self, "_h", None):
@@ -559,6 +635,112 @@ class Context:
         ph, ldh = _kept_rows(h, m, tab, keep, True)
         self._check(self._lib.condensa_adapter_backward(self._h, C.byref(batch), px, ldx, pdy, lddy, ph, ldh, pdx, lddx,
                                                         1 if accumulate else 0, _stream_handle(stream)))
+
+    def _here(self, device: int, name: str):
+        if device != self.device:
+            raise ValueError("%s is on another device than the context" % name)
+
+    def _matrix(self, x, rows: int, cols: int, dtype, name: str):
+        """Address and row stride of an operand (None: 0, 0)."""
+        if x is None:
+            return None, 0
+        self._here(x.get_device(), name)
+        return _rows_of(x, rows, cols, dtype, name)
+
+    def _coded(self, code, rows: int, cols: int, high: int, name: str) -> Coded:
+        if not isinstance(code, Coded) or code.high != high:
+            raise TypeError("%s must be made by %s" % (name, "coded_rows" if high == 1 else "coded_blocks"))
+        if (code.rows, code.cols) != (rows, cols):
+            raise ValueError("%s has shape %s, not %s" % (name, (code.rows, code.cols), (rows, cols)))
+        self._here(code.device, name)
+        return code
+
+    def _vector(self, x, n: int, name: str):
+        """Address of a contiguous float32 vector (None: None)."""
+        if x is None:
+            return None
+        _dtype_code(x, (DTYPE_FP32,), name)
+        if tuple(x.shape) != (n,) or not _contiguous(x):
+            raise ValueError("%s must be contiguous and hold %d elements" % (name, n))
+        self._here(x.get_device(), name)
+        return x.data_ptr()
+
+    def _gain(self, gain, cols: int, dtype: int):
+        """Address and type of the gain of a norm."""
+        if gain is None:
+            return None, DTYPE_FP32
+        code = _dtype_code(gain, (DTYPE_FP32, dtype), "gain")
+        if tuple(gain.shape) != (cols,) or not _contiguous(gain):
+            raise ValueError("gain must be contiguous and hold %d elements" % cols)
+        self._here(gain.get_device(), "gain")
+        return gain.data_ptr(), code
+
+    def encode_rows(self, x, out: Coded, stream=None):
+        """``x`` [rows, cols] (float32, float16, bfloat16) into ``out``, a scale for every 128 columns of a row."""
+        rows, cols = x.shape
+        code = _dtype_code(x, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "x")
+        p, ld = self._matrix(x, rows, cols, x.dtype, "x")
+        out = self._coded(out, rows, cols, 1, "out")
+        self._check(self._lib.condensa_encode_rows(self._h, p, ld, rows, cols, code, C.byref(out.struct), _stream_handle(stream)))
+
+    def encode_blocks(self, w, out: Coded, theta=None, stream=None):
+        """``w`` [n, k] (float32, float16, bfloat16) into ``out``, a scale for every 128 x 128; ``theta`` (float32, may be ``w`` itself, or None)
+        receives the values that the codes stand for."""
+        n, k = w.shape
+        code = _dtype_code(w, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "w")
+        p, ld = self._matrix(w, n, k, w.dtype, "w")
+        if theta is not None:
+            _dtype_code(theta, (DTYPE_FP32,), "theta")
+        pt, ldt = self._matrix(theta, n, k, theta.dtype if theta is not None else None, "theta")
+        out = self._coded(out, n, k, CODE_GROUP, "out")
+        self._check(self._lib.condensa_encode_blocks(self._h, p, ld, n, k, code, C.byref(out.struct), pt, ldt, _stream_handle(stream)))
+
+    def _product(self, call, w: Coded, x: Coded, y, depth: int, width: int, names, stream):
+        w = self._coded(w, w.rows, w.cols, CODE_GROUP, "w")
+        rows = x.rows
+        x = self._coded(x, rows, depth, 1, names[0])
+        code = _dtype_code(y, (DTYPE_FP16, DTYPE_BF16), names[1])
+        p, ld = self._matrix(y, rows, width, y.dtype, names[1])
+        self._check(call(self._h, C.byref(w.projection), C.byref(x.struct), rows, p, ld, code, _stream_handle(stream)))
+
+    def projection_forward(self, w: Coded, x: Coded, y, stream=None):
+        """``y = x w^T``: ``w`` [n, k] by :func:`coded_blocks`, ``x`` [rows, k] by :func:`coded_rows`, ``y`` [rows, n] float16 or bfloat16."""
+        self._product(self._lib.condensa_projection_forward, w, x, y, w.cols, w.rows, ("x", "y"), stream)
+
+    def projection_backward(self, w: Coded, dy: Coded, dx, stream=None):
+        """``dx = dy w``, the gradient that reaches the rows: ``dy`` [rows, n] by :func:`coded_rows`, ``dx`` [rows, k] float16 or bfloat16."""
+        self._product(self._lib.condensa_projection_backward, w, dy, dx, w.rows, w.cols, ("dy", "dx"), stream)
+
+    def norm_forward(self, x, gain, eps=1e-5, residual=None, h=None, y=None, code: Optional[Coded] = None, rstd=None, stream=None):
+        """Root-mean-square norm of the rows of ``x + residual``: ``h`` receives the sum (it may be ``x`` or ``residual``), ``y`` the
+        normalised rows times ``gain`` (float32, or the type of ``x``; None: ones), ``code`` the same in 8 bits, ``rstd`` (float32) what
+        :meth:`norm_backward` needs. Any of the results may be None."""
+        rows, cols = x.shape
+        dtype = _dtype_code(x, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "x")
+        pg, gain_dtype = self._gain(gain, cols, dtype)
+        px, ldx = self._matrix(x, rows, cols, x.dtype, "x")
+        pr, ldr = self._matrix(residual, rows, cols, x.dtype, "residual")
+        ph, ldh = self._matrix(h, rows, cols, x.dtype, "h")
+        py, ldy = self._matrix(y, rows, cols, x.dtype, "y")
+        coded = self._coded(code, rows, cols, 1, "code").struct if code is not None else CodedMatrix()
+        n = Norm(px, pr, pg, ph, py, coded, self._vector(rstd, rows, "rstd"), ldx, ldr, ldh, ldy, rows, cols, eps, dtype, gain_dtype, 0)
+        self._check(self._lib.condensa_norm_forward(self._h, C.byref(n), _stream_handle(stream)))
+
+    def norm_backward(self, dy, h, gain, rstd, dh=None, dx=None, code: Optional[Coded] = None, dgain=None, accumulate=False, stream=None):
+        """Gradients of :meth:`norm_forward`: ``h`` is what it left there (``x`` without a residual), ``dh`` the gradient that reaches h
+        otherwise (None: none). ``dx`` receives the gradient of ``x`` and of the residual (it may be ``dy`` or ``dh``), ``code`` the same
+        in 8 bits, ``dgain`` (float32) that of the gain, added to with ``accumulate``."""
+        rows, cols = dy.shape
+        dtype = _dtype_code(dy, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "dy")
+        pg, gain_dtype = self._gain(gain, cols, dtype)
+        py, ldy = self._matrix(dy, rows, cols, dy.dtype, "dy")
+        pd, ldd = self._matrix(dh, rows, cols, dy.dtype, "dh")
+        ph, ldh = self._matrix(h, rows, cols, dy.dtype, "h")
+        px, ldx = self._matrix(dx, rows, cols, dy.dtype, "dx")
+        coded = self._coded(code, rows, cols, 1, "code").struct if code is not None else CodedMatrix()
+        n = NormGradient(py, pd, ph, pg, self._vector(rstd, rows, "rstd"), px, coded, self._vector(dgain, cols, "dgain"), ldy, ldd, ldh, ldx, rows, cols,
+                         dtype, gain_dtype, 1 if accumulate else 0, 0)
+        self._check(self._lib.condensa_norm_backward(self._h, C.byref(n), _stream_handle(stream)))
 
     def thin_flags(self, theta, d0, d1, inner, axis, keep, stream=None):
         self._check(self._lib.condensa_thin_flags(self._h, _addr(theta), int(d0), int(d1), int(inner), int(axis),
