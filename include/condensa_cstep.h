@@ -480,8 +480,8 @@ CONDENSA_API int condensa_encode_blocks(condensa_ctx *ctx, const void *w, int64_
  *   backward  dx[i][l] = sum over j of dy[i][j] * w[j][l]      dy [rows][n], dx [rows][k]
  * Both read the one copy of the codes. The projection is what a C-step left and is not trained: there is no gradient to w.
  * y and dx are overwritten, of CONDENSA_DTYPE_FP16 or _BF16, rows `ld` elements apart. Products of codes and their scales are
- * exact; sums are formed in fp32 by the matrix instruction, which cuts instead of rounding (up to 2^-23 of the largest partial sum for
- * every 32 terms), and are rounded once to the result. fp32 results are not offered for that reason. Rows do not mix: a NaN in a row
+ * exact; sums are formed in fp32 by the matrix instruction, 32 terms at a time, which cuts instead of rounding (measured: the terms and
+ * the sum so far at 2^-25 of the largest of them, the new sum at 2^-23 of itself), and are rounded once to the result. fp32 results are not offered for that reason. Rows do not mix: a NaN in a row
  * stays in that row of the result. The order of a sum depends on the shapes and the device only.
  * n and k at most 2^22, rows at most 2^31 - 256. No workspace is used. Any alignment of the result is taken; rows that are 16- or
  * 8-byte aligned are faster. */

@@ -645,6 +645,8 @@ class Context:
         if x is None:
             return None, 0
         self._here(x.get_device(), name)
+        if x.dim() != 2 or x.shape[1] != cols:
+            raise ValueError("%s must be a [%d, %d] matrix" % (name, rows, cols))
         return _rows_of(x, rows, cols, dtype, name)
 
     def _coded(self, code, rows: int, cols: int, high: int, name: str) -> Coded:
