@@ -13,9 +13,6 @@ typedef uint16_t u16;
 constexpr int GROUP = 128;              // columns (and, in blocks, rows) that share a scale
 constexpr int GROUP_LANES = GROUP / 8;  // threads of a group, eight columns each
 
-// An access of eight neighbouring values goes by 16 bytes, by 8, or value by value (V_EACH).
-enum { V_EACH = 0, V_8 = 8, V_16 = 16 };
-
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -30,24 +27,37 @@ struct alignas(16) Eight {
     T v[8];
     __device__ __forceinline__ float operator[](int i) const { return to_f32(v[i]); }
 };
-
-// Columns c .. c+7 of a row of `cols`; zero past the end.
+// Keeps the values as they are in registers: what has been made of them ahead of this is made anew behind it, not kept too.
 template <class T>
-__device__ __forceinline__ Eight<T> load8(const T *row, long long c, long long cols, int vec)
+__device__ __forceinline__ void hold(Eight<T> &e)
+{
+    u32 *w = reinterpret_cast<u32 *>(&e);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(e) / 4; ++i) asm volatile("" : "+r"(w[i]));
+}
+template <class T> struct Access;       // an access of four values
+template <> struct Access<float> { typedef uint4 Four; };
+template <> struct Access<__half> { typedef uint2 Four; };
+template <> struct Access<__nv_bfloat16> { typedef uint2 Four; };
+
+// Columns c .. c+7 of a row of `cols`; zero past the end. A says what the rows allow: 8 or 4 values at a time (alignment, and a
+// number of columns that is a multiple of it), or one. It is fixed when compiling: a choice at every access made three to
+// four times as many instructions, and kept the loads of a thread from leaving together (128 x 128 blocks of bf16: 87 us).
+template <int A, class T>
+__device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
 {
     Eight<T> e;
-    if (vec != V_EACH && c + 8 <= cols) {
-        if (vec == V_16) {
-            uint4 *d = reinterpret_cast<uint4 *>(&e);
-            const uint4 *s = reinterpret_cast<const uint4 *>(row + c);
+    if constexpr (A == 8) {
+        uint4 *d = reinterpret_cast<uint4 *>(&e);
+        const uint4 *s = reinterpret_cast<const uint4 *>(row + c);
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(e) / 16; ++i) d[i] = s[i];
-        } else {
-            uint2 *d = reinterpret_cast<uint2 *>(&e);
-            const uint2 *s = reinterpret_cast<const uint2 *>(row + c);
+        for (int i = 0; i < (int)sizeof(e) / 16; ++i) d[i] = c < cols ? s[i] : make_uint4(0, 0, 0, 0);
+    } else if constexpr (A == 4) {
+        typedef typename Access<T>::Four Four;
+        Four *d = reinterpret_cast<Four *>(&e);
+        const Four *s = reinterpret_cast<const Four *>(row + c);
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(e) / 8; ++i) d[i] = s[i];
-        }
+        for (int i = 0; i < 2; ++i) d[i] = c + 4 * i < cols ? s[i] : Four{};
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) e.v[i] = c + i < cols ? row[c + i] : from_f32<T>(0.0f);
@@ -55,21 +65,23 @@ __device__ __forceinline__ Eight<T> load8(const T *row, long long c, long long c
     return e;
 }
 
-template <class T>
-__device__ __forceinline__ void store8(T *row, long long c, long long cols, int vec, const Eight<T> &e)
+template <int A, class T>
+__device__ __forceinline__ void store8(T *row, int c, int cols, const Eight<T> &e)
 {
-    if (vec != V_EACH && c + 8 <= cols) {
-        if (vec == V_16) {
-            const uint4 *s = reinterpret_cast<const uint4 *>(&e);
-            uint4 *d = reinterpret_cast<uint4 *>(row + c);
+    if constexpr (A == 8) {
+        const uint4 *s = reinterpret_cast<const uint4 *>(&e);
+        uint4 *d = reinterpret_cast<uint4 *>(row + c);
+        if (c < cols) {
 #pragma unroll
             for (int i = 0; i < (int)sizeof(e) / 16; ++i) d[i] = s[i];
-        } else {
-            const uint2 *s = reinterpret_cast<const uint2 *>(&e);
-            uint2 *d = reinterpret_cast<uint2 *>(row + c);
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(e) / 8; ++i) d[i] = s[i];
         }
+    } else if constexpr (A == 4) {
+        typedef typename Access<T>::Four Four;
+        const Four *s = reinterpret_cast<const Four *>(&e);
+        Four *d = reinterpret_cast<Four *>(row + c);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (c + 4 * i < cols) d[i] = s[i];
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -77,54 +89,71 @@ __device__ __forceinline__ void store8(T *row, long long c, long long cols, int 
     }
 }
 
-// The scale of a group by the pattern of its largest magnitude, 1.m * 2^e: the quotient is at most 448 = 1.75 * 2^8.
-__device__ __forceinline__ u32 scale_of(u32 most)
+// The scale of a group by its largest magnitude 1.m * 2^e: the quotient is at most 448 = 1.75 * 2^8.
+__device__ __forceinline__ u32 scale_of(float most)
 {
-    const u32 e = most >> 23, up = (most & 0x7FFFFFu) > 0x600000u ? 1u : 0u;
-    return e > 8 ? e - 8 + up : 1u;
+    const u32 b = __float_as_uint(most), s = (b + 0x1FFFFFu) >> 23;     // (e, or e + 1 for m > 0x600000)
+    return s > 9 ? s - 8 : 1u;
 }
 __device__ __forceinline__ float scale_value(u32 s) { return __uint_as_float(s << 23); }            // 2^(s-127)
 __device__ __forceinline__ float scale_inverse(u32 s) { return __uint_as_float((254u - s) << 23); } // 2^(127-s); s is at most 247
 
-// Pattern of the largest magnitude of eight values; with `finite`, of those that are.
-__device__ __forceinline__ u32 most_of(const float (&v)[8], bool finite)
+// Largest magnitude; no number if one of them is none.
+__device__ __forceinline__ float most3(float a, float b, float c)
 {
-    u32 m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const u32 b = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-        m = max(m, finite && b >= 0x7F800000u ? 0u : b);
-    }
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
     return m;
 }
-// Largest of a group's 16 lanes. Every lane of the group is here.
-__device__ __forceinline__ u32 group_most(u32 m, u32 lanes)
+__device__ __forceinline__ float most2(float a, float b)
 {
-#pragma unroll
-    for (int d = GROUP_LANES / 2; d > 0; d >>= 1) m = max(m, __shfl_xor_sync(lanes, m, d));
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
     return m;
 }
+__device__ __forceinline__ float most_of(const float (&v)[8]) { return most3(most3(most3(v[0], v[1], v[2]), v[3], v[4]), most3(v[5], v[6], v[7]), 0.0f); }
+// ... of those that are finite
+__device__ __forceinline__ float most_finite(const float (&v)[8])
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fabsf(v[i]) <= 3.402823466e38f ? fmaxf(m, fabsf(v[i])) : m;
+    return m;
+}
+// Largest of a group's 16 lanes. Every lane of `lanes` is here.
+__device__ __forceinline__ float group_most(float m, u32 lanes)
+{
+#pragma unroll
+    for (int d = GROUP_LANES / 2; d > 0; d >>= 1) m = most2(m, __shfl_xor_sync(lanes, m, d));
+    return m;
+}
+__device__ __forceinline__ bool is_odd(float most) { return !(most <= 3.402823466e38f); }
 
-// Codes of eight values under 2^(127-s). (The conversion saturates infinities, so `odd` ones are taken out of its way.)
-__device__ __forceinline__ uint2 codes_of(const float (&v)[8], float inverse, bool odd)
+// Codes of eight values under 2^(127-s).
+__device__ __forceinline__ uint2 codes_of(const float (&v)[8], float inverse)
 {
     u16 q[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float x = v[2 * i] * inverse, y = v[2 * i + 1] * inverse;
-        if (odd) {
-            if (!(fabsf(v[2 * i]) <= 3.402823466e38f)) x = __uint_as_float(0x7FFFFFFFu);
-            if (!(fabsf(v[2 * i + 1]) <= 3.402823466e38f)) y = __uint_as_float(0x7FFFFFFFu);
-        }
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q[i]) : "f"(y), "f"(x));
-    }
+    for (int i = 0; i < 4; ++i)
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q[i]) : "f"(v[2 * i + 1] * inverse), "f"(v[2 * i] * inverse));
     return make_uint2((u32)q[0] | (u32)q[1] << 16, (u32)q[2] | (u32)q[3] << 16);
 }
-
-__device__ __forceinline__ void store_codes(u8 *row, long long c, long long cols, uint2 q)
+// (The conversion saturates infinities: they are made NaN ahead of it.)
+__device__ __forceinline__ void odd_to_nan(float (&v)[8])
 {
-    if (c + 8 <= cols) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (!(fabsf(v[i]) <= 3.402823466e38f)) v[i] = __uint_as_float(0x7FFFFFFFu);
+}
+
+// Rows of codes are 16-byte aligned whatever their width.
+template <int A>
+__device__ __forceinline__ void store_codes(u8 *row, int c, int cols, uint2 q)
+{
+    if (A == 8 || c + 8 <= cols) {
         *reinterpret_cast<uint2 *>(row + c) = q;
+    } else if (A == 4) {
+        *reinterpret_cast<u32 *>(row + c) = q.x;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -134,14 +163,17 @@ __device__ __forceinline__ void store_codes(u8 *row, long long c, long long cols
 
 // Columns c .. c+7 of a row (zero past its end), whose group the 16 lanes around this one hold, into codes and scale. All
 // lanes of the warp call it.
-__device__ __forceinline__ void encode8(const float (&v)[8], u8 *codes, u8 *scales, long long c, long long cols)
+template <int A>
+__device__ __forceinline__ void encode8(float (&v)[8], u8 *codes, u8 *scales, int c, int cols)
 {
-    u32 most = group_most(most_of(v, false), 0xFFFFFFFFu);
-    const bool odd = most >= 0x7F800000u;               // (the same for the group)
-    if (odd) most = group_most(most_of(v, true), 0xFFFFu << (threadIdx.x & 16));
+    float most = group_most(most_of(v), 0xFFFFFFFFu);
+    if (is_odd(most)) {                                 // (the same for the group)
+        most = group_most(most_finite(v), 0xFFFFu << (threadIdx.x & 16));
+        odd_to_nan(v);
+    }
     const u32 s = scale_of(most);
     if (c < cols) {
-        store_codes(codes, c, cols, codes_of(v, scale_inverse(s), odd));
+        store_codes<A>(codes, c, cols, codes_of(v, scale_inverse(s)));
         if (threadIdx.x % GROUP_LANES == 0) scales[c / GROUP] = (u8)s;
     }
 }

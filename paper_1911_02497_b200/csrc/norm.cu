@@ -2,8 +2,7 @@
 #include <cmath>
 #include <new>
 
-#include "norm.cuh"
-#include "op_args.h"
+#include "norm_launch.cuh"
 
 using namespace cs;
 
@@ -11,46 +10,7 @@ static_assert(CONDENSA_CODE_GROUP == GROUP, "columns that share a scale");
 
 namespace {
 
-// CTAs of a kernel that an SM holds.
-int resident_ctas(condensa_ctx *ctx, const void *f, int block, int &count)
-{
-    for (const condensa_ctx::ClusterFit &k : ctx->cluster_fit)
-        if (k.f == f && k.size == 0) {
-            count = k.count;
-            return CONDENSA_OK;
-        }
-    count = 0;
-    CU_TRY(ctx, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&count, f, block, 0));
-    if (count < 1) count = 1;
-    ctx->cluster_fit.push_back({f, 0, count});
-    return CONDENSA_OK;
-}
-
-constexpr int LONG_TPR = 512;           // threads of a row that is read twice
-
 // ------------------------------------------------------------------ forward
-template <class T, int TPR, int NV>
-int forward_as(condensa_ctx *ctx, const NormParams &P, cudaStream_t stream)
-{
-    constexpr int ROWS = RowThreads<TPR>::ROWS;
-    return op_launch(ctx, "k_norm_forward", k_norm_forward<T, TPR, NV>, dim3((unsigned)((P.rows + ROWS - 1) / ROWS)), RowThreads<TPR>::BLOCK, stream, P);
-}
-
-// The threads of a row: as many as hold it with one or two eights each.
-template <class T>
-int forward_of(condensa_ctx *ctx, const NormParams &P, cudaStream_t stream)
-{
-    const int eights = (P.cols + 7) / 8;
-    return eights <= 32   ? forward_as<T, 32, 1>(ctx, P, stream)
-         : eights <= 64   ? forward_as<T, 32, 2>(ctx, P, stream)
-         : eights <= 128  ? forward_as<T, 128, 1>(ctx, P, stream)
-         : eights <= 256  ? forward_as<T, 128, 2>(ctx, P, stream)
-         : eights <= 512  ? forward_as<T, 256, 2>(ctx, P, stream)
-         : eights <= 1024 ? forward_as<T, 512, 2>(ctx, P, stream)
-         : eights <= 2048 ? forward_as<T, 1024, 2>(ctx, P, stream)
-                          : op_launch(ctx, "k_norm_forward_long", k_norm_forward_long<T, LONG_TPR>, dim3((unsigned)P.rows), LONG_TPR, stream, P);
-}
-
 int forward(condensa_ctx *ctx, const condensa_norm *p, cudaStream_t stream)
 {
     if (!p) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "norm is NULL");
@@ -95,68 +55,18 @@ int forward(condensa_ctx *ctx, const condensa_norm *p, cudaStream_t stream)
     P.cols = (int)p->cols;
     P.eps = p->eps;
     P.gain_f32 = p->gain_dtype == CONDENSA_DTYPE_FP32;
-    P.vx = op_access(P.x, P.ldx, e);
-    P.vr = op_access(P.residual, P.ldr, e);
-    P.vh = op_access(P.h, P.ldh, e);
-    P.vy = op_access(P.y, P.ldy, e);
-    P.vg = op_access(P.gain, 0, ge);
-    return p->dtype == CONDENSA_DTYPE_BF16 ? forward_of<__nv_bfloat16>(ctx, P, stream)
-         : p->dtype == CONDENSA_DTYPE_FP16 ? forward_of<__half>(ctx, P, stream) : forward_of<float>(ctx, P, stream);
+    const int access = std::min({op_access(P.x, P.ldx, e, P.cols), op_access(P.residual, P.ldr, e, P.cols), op_access(P.h, P.ldh, e, P.cols),
+                                 op_access(P.y, P.ldy, e, P.cols), op_access(P.gain, 0, ge, P.cols)});
+    return p->dtype == CONDENSA_DTYPE_BF16 ? norm_forward_launch<__nv_bfloat16>(ctx, P, access, stream)
+         : p->dtype == CONDENSA_DTYPE_FP16 ? norm_forward_launch<__half>(ctx, P, access, stream) : norm_forward_launch<float>(ctx, P, access, stream);
 }
 
 // ------------------------------------------------------------------ backward
-// How a backward call is cut: CTAs, and the slots of sums for dgain that they leave.
-struct BackPlan {
-    int grid, slots;
-};
-
-template <class T, int TPR, int NV>
-int backward_as(condensa_ctx *ctx, NormBackParams &P, BackPlan &plan, bool run, cudaStream_t stream)
+int backward_type(condensa_ctx *ctx, int dtype, const NormBackParams &P, NormBackPlan &plan, int access, bool run, cudaStream_t stream)
 {
-    constexpr int ROWS = RowThreads<TPR>::ROWS, BLOCK = RowThreads<TPR>::BLOCK;
-    auto k = k_norm_backward<T, TPR, NV>;
-    if (run) return op_launch(ctx, "k_norm_backward", k, dim3((unsigned)plan.grid), BLOCK, stream, P);
-    int fit = 1;
-    const int rc = resident_ctas(ctx, (const void *)k, BLOCK, fit);
-    if (rc) return rc;
-    plan.grid = stream_grid(ctx, (P.rows + ROWS - 1) / ROWS, fit);
-    plan.slots = plan.grid * ROWS;
-    return CONDENSA_OK;
-}
-
-// The register file holds 64 values a thread of 1024, too few for fp32 operands.
-template <class T> int longest_back() { return sizeof(T) == 4 ? 1024 : 2048; }
-
-template <class T>
-int backward_of(condensa_ctx *ctx, NormBackParams &P, BackPlan &plan, bool run, cudaStream_t stream)
-{
-    const int eights = (P.cols + 7) / 8;
-    if (eights > longest_back<T>()) {
-        const unsigned strips = (unsigned)((eights + THREADS - 1) / THREADS);
-        if (!run) {
-            plan.grid = stream_grid(ctx, P.rows, std::max(1, 4 / (int)strips));
-            plan.slots = plan.grid;
-            return CONDENSA_OK;
-        }
-        int rc = CONDENSA_OK;
-        if (P.part) rc = op_launch(ctx, "k_norm_dgain_long", k_norm_dgain_long<T>, dim3(strips, (unsigned)plan.grid), THREADS, stream, P);
-        if (rc || (!P.dx && !P.codes)) return rc;
-        return op_launch(ctx, "k_norm_backward_long", k_norm_backward_long<T, LONG_TPR>, dim3((unsigned)P.rows), LONG_TPR, stream, P);
-    }
-    if constexpr (sizeof(T) == 2)
-        if (eights > 1024) return backward_as<T, 1024, 2>(ctx, P, plan, run, stream);
-    return eights <= 32  ? backward_as<T, 32, 1>(ctx, P, plan, run, stream)
-         : eights <= 64  ? backward_as<T, 32, 2>(ctx, P, plan, run, stream)
-         : eights <= 128 ? backward_as<T, 128, 1>(ctx, P, plan, run, stream)
-         : eights <= 256 ? backward_as<T, 128, 2>(ctx, P, plan, run, stream)
-         : eights <= 512 ? backward_as<T, 256, 2>(ctx, P, plan, run, stream)
-                         : backward_as<T, 512, 2>(ctx, P, plan, run, stream);
-}
-
-int backward_type(condensa_ctx *ctx, int dtype, NormBackParams &P, BackPlan &plan, bool run, cudaStream_t stream)
-{
-    return dtype == CONDENSA_DTYPE_BF16 ? backward_of<__nv_bfloat16>(ctx, P, plan, run, stream)
-         : dtype == CONDENSA_DTYPE_FP16 ? backward_of<__half>(ctx, P, plan, run, stream) : backward_of<float>(ctx, P, plan, run, stream);
+    return dtype == CONDENSA_DTYPE_BF16 ? norm_backward_launch<__nv_bfloat16>(ctx, P, plan, access, run, stream)
+         : dtype == CONDENSA_DTYPE_FP16 ? norm_backward_launch<__half>(ctx, P, plan, access, run, stream)
+                                        : norm_backward_launch<float>(ctx, P, plan, access, run, stream);
 }
 
 int backward(condensa_ctx *ctx, const condensa_norm_gradient *p, cudaStream_t stream)
@@ -205,22 +115,19 @@ int backward(condensa_ctx *ctx, const condensa_norm_gradient *p, cudaStream_t st
     P.rows = p->rows;
     P.cols = (int)p->cols;
     P.gain_f32 = p->gain_dtype == CONDENSA_DTYPE_FP32;
-    P.vy = op_access(P.dy, P.ldy, e);
-    P.vd = op_access(P.dh, P.ldd, e);
-    P.vh = op_access(P.h, P.ldh, e);
-    P.vx = op_access(P.dx, P.ldx, e);
-    P.vg = op_access(P.gain, 0, ge);
+    const int access = std::min({op_access(P.dy, P.ldy, e, P.cols), op_access(P.dh, P.ldd, e, P.cols), op_access(P.h, P.ldh, e, P.cols),
+                                 op_access(P.dx, P.ldx, e, P.cols), op_access(P.gain, 0, ge, P.cols)});
     P.ld_part = (P.cols + 7) / 8 * 8;
-    BackPlan plan = {0, 0};
+    NormBackPlan plan = {0, 0};
     OpWorkspaceUse use;
-    if (p->rows > 0 && (rc = backward_type(ctx, p->dtype, P, plan, false, stream)) != 0) return rc;
+    if (p->rows > 0 && (rc = backward_type(ctx, p->dtype, P, plan, access, false, stream)) != 0) return rc;
     if (p->dgain && plan.slots) {
         if ((rc = op_workspace(ctx, 256 + sizeof(float) * (size_t)plan.slots * (size_t)P.ld_part, stream, use)) != 0) return rc;
         P.part = (float *)(ctx->op.p + 256);
     }
-    if (p->rows > 0 && (rc = backward_type(ctx, p->dtype, P, plan, true, stream)) != 0) return rc;
+    if (p->rows > 0 && (rc = backward_type(ctx, p->dtype, P, plan, access, true, stream)) != 0) return rc;
     if (p->dgain) {
-        rc = op_launch(ctx, "k_norm_dgain", k_norm_dgain, dim3((unsigned)((P.cols + 31) / 32)), THREADS, stream, (const float *)P.part, P.ld_part, plan.slots,
+        rc = op_launch(ctx, "k_norm_dgain", k_norm_dgain, dim3((unsigned)((P.cols + 31) / 32)), DGAIN_WARPS * 32, stream, (const float *)P.part, P.ld_part, plan.slots,
                        p->dgain, P.cols, p->accumulate ? 1 : 0);
         if (rc) return rc;
     }
@@ -228,6 +135,23 @@ int backward(condensa_ctx *ctx, const condensa_norm_gradient *p, cudaStream_t st
 }
 
 // ------------------------------------------------------------------ encoders
+typedef void (*Encoder)(EncodeParams);
+template <class T> Encoder row_encoder_of(int access) { return access == 8 ? k_encode_rows<T, 8> : access == 4 ? k_encode_rows<T, 4> : k_encode_rows<T, 1>; }
+template <class T> Encoder block_encoder_of(int access) { return access == 8 ? k_encode_blocks<T, 8> : access == 4 ? k_encode_blocks<T, 4> : k_encode_blocks<T, 1>; }
+Encoder row_encoder(int dtype, int access)
+{
+    return dtype == CONDENSA_DTYPE_BF16 ? row_encoder_of<__nv_bfloat16>(access) : dtype == CONDENSA_DTYPE_FP16 ? row_encoder_of<__half>(access) : row_encoder_of<float>(access);
+}
+Encoder block_encoder(int dtype, int access)
+{
+    return dtype == CONDENSA_DTYPE_BF16 ? block_encoder_of<__nv_bfloat16>(access) : dtype == CONDENSA_DTYPE_FP16 ? block_encoder_of<__half>(access) : block_encoder_of<float>(access);
+}
+void set_groups(EncodeParams &P)
+{
+    P.groups = (u32)((P.cols + GROUP - 1) / GROUP);
+    P.reciprocal = P.groups == 1 ? 0xFFFFFFFFu : (u32)((1ull << 32) / P.groups);
+}
+
 int encode_rows(condensa_ctx *ctx, const void *x, long long ldx, long long rows, long long cols, int dtype, const condensa_coded *out, cudaStream_t stream)
 {
     if (!out) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "out is NULL");
@@ -245,13 +169,11 @@ int encode_rows(condensa_ctx *ctx, const void *x, long long ldx, long long rows,
     P.codes = out->codes; P.scales = out->scales; P.ldc = out->ld; P.lds = out->ld_scales;
     P.rows = rows;
     P.cols = (int)cols;
-    P.groups = (int)((cols + GROUP - 1) / GROUP);
-    P.vx = op_access(x, ldx, e);
+    set_groups(P);
     const long long per = THREADS / GROUP_LANES * ENC_UNITS, grid = (rows * P.groups + per - 1) / per;
     if (grid > 0x7FFFFFFFll) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "too many groups for one launch");
     CU_TRY(ctx, cudaSetDevice(ctx->device));
-    return op_launch(ctx, "k_encode_rows", dtype == CONDENSA_DTYPE_BF16 ? k_encode_rows<__nv_bfloat16> : dtype == CONDENSA_DTYPE_FP16 ? k_encode_rows<__half> : k_encode_rows<float>,
-                     dim3((unsigned)grid), THREADS, stream, P);
+    return op_launch(ctx, "k_encode_rows", row_encoder(dtype, op_access(x, ldx, e, cols)), dim3((unsigned)grid), THREADS, stream, P);
 }
 
 int encode_blocks(condensa_ctx *ctx, const void *w, long long ldw, long long n, long long k, int dtype, const condensa_coded *out, float *theta, long long ld_theta,
@@ -276,13 +198,10 @@ int encode_blocks(condensa_ctx *ctx, const void *w, long long ldw, long long n, 
     P.theta = theta; P.ld_theta = ld_theta;
     P.rows = n;
     P.cols = (int)k;
-    P.groups = (int)((k + GROUP - 1) / GROUP);
-    P.vx = op_access(w, ldw, e);
-    P.vt = op_access(theta, ld_theta, 4);
+    set_groups(P);
     CU_TRY(ctx, cudaSetDevice(ctx->device));
-    return op_launch(ctx, "k_encode_blocks",
-                     dtype == CONDENSA_DTYPE_BF16 ? k_encode_blocks<__nv_bfloat16> : dtype == CONDENSA_DTYPE_FP16 ? k_encode_blocks<__half> : k_encode_blocks<float>,
-                     dim3((unsigned)((n + GROUP - 1) / GROUP * P.groups)), THREADS, stream, P);
+    return op_launch(ctx, "k_encode_blocks", block_encoder(dtype, std::min(op_access(w, ldw, e, k), op_access(theta, ld_theta, 4, k))),
+                     dim3((unsigned)((n + GROUP - 1) / GROUP * P.groups)), ENC_BLOCK, stream, P);
 }
 
 }  // namespace

@@ -17,7 +17,6 @@ struct NormParams {
     long long ldx, ldr, ldh, ldy, ldc, lds;
     long long rows;
     int cols;
-    int vx, vr, vh, vy, vg;             // accesses that the rows allow
     int gain_f32;
     float eps;
 };
@@ -31,7 +30,6 @@ struct NormBackParams {
     long long ldy, ldd, ldh, ldx, ldc, lds, ld_part;
     long long rows;
     int cols;
-    int vy, vd, vh, vx, vg;
     int gain_f32;
 };
 
@@ -59,30 +57,30 @@ __device__ __forceinline__ F row_sum(F v, F *slots)
 __device__ __forceinline__ float rstd_of(float sum, int cols, float eps) { return 1.0f / sqrtf(sum / (float)cols + eps); }
 __device__ __forceinline__ float rstd_of(double sum, int cols, float eps) { return (float)(1.0 / sqrt(sum / cols + (double)eps)); }
 
-template <class T>
-__device__ __forceinline__ void load_gain(const void *gain, int f32, int vec, long long c, int cols, float (&g)[8])
+template <class T, int A>
+__device__ __forceinline__ void load_gain(const void *gain, int f32, int c, int cols, float (&g)[8])
 {
     if (!gain) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = 1.0f;
     } else if (f32) {
-        const Eight<float> e = load8((const float *)gain, c, cols, vec);
+        const Eight<float> e = load8<A>((const float *)gain, c, cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = e[i];
     } else {
-        const Eight<T> e = load8((const T *)gain, c, cols, vec);
+        const Eight<T> e = load8<A>((const T *)gain, c, cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = e[i];
     }
 }
 
 // h of columns c .. c+7: x, or the rounded sum of x and the residual.
-template <class T>
-__device__ __forceinline__ Eight<T> load_h(const NormParams &P, long long row, long long c)
+template <class T, int A>
+__device__ __forceinline__ Eight<T> load_h(const NormParams &P, long long row, int c)
 {
-    Eight<T> h = load8((const T *)P.x + row * P.ldx, c, P.cols, P.vx);
+    Eight<T> h = load8<A>((const T *)P.x + row * P.ldx, c, P.cols);
     if (P.residual) {
-        const Eight<T> r = load8((const T *)P.residual + row * P.ldr, c, P.cols, P.vr);
+        const Eight<T> r = load8<A>((const T *)P.residual + row * P.ldr, c, P.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h.v[i] = from_f32<T>(h[i] + r[i]);
     }
@@ -90,25 +88,25 @@ __device__ __forceinline__ Eight<T> load_h(const NormParams &P, long long row, l
 }
 
 // What follows from eight values of h.
-template <class T>
-__device__ __forceinline__ void norm_out(const NormParams &P, long long row, long long c, const Eight<T> &h, float rstd)
+template <class T, int A>
+__device__ __forceinline__ void norm_out(const NormParams &P, long long row, int c, const Eight<T> &h, float rstd)
 {
     float g[8], y[8];
-    load_gain<T>(P.gain, P.gain_f32, P.vg, c, P.cols, g);
+    load_gain<T, A>(P.gain, P.gain_f32, c, P.cols, g);
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = h[i] * rstd * g[i];
     if (P.y) {
         Eight<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o.v[i] = from_f32<T>(y[i]);
-        store8((T *)P.y + row * P.ldy, c, P.cols, P.vy, o);
+        store8<A>((T *)P.y + row * P.ldy, c, P.cols, o);
     }
     if (P.codes) {
         if (c + 8 > P.cols) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = c + i < P.cols ? y[i] : 0.0f;        // (a row that is no number)
         }
-        encode8(y, P.codes + row * P.ldc, P.scales + row * P.lds, c, P.cols);
+        encode8<A>(y, P.codes + row * P.ldc, P.scales + row * P.lds, c, P.cols);
     }
 }
 
@@ -116,7 +114,7 @@ template <int TPR> struct RowThreads {
     static constexpr int BLOCK = TPR < 128 ? 128 : TPR, ROWS = BLOCK / TPR;
 };
 
-template <class T, int TPR, int NV>
+template <class T, int A, int TPR, int NV>
 __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const __grid_constant__ NormParams P)
 {
     __shared__ float slots[32];
@@ -129,10 +127,10 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
     Eight<T> h[NV];
     float sum = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) h[v] = load_h<T>(P, row, (long long)(v * TPR + t) * 8);
+    for (int v = 0; v < NV; ++v) h[v] = load_h<T, A>(P, row, (v * TPR + t) * 8);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        if (P.h) store8((T *)P.h + row * P.ldh, (long long)(v * TPR + t) * 8, P.cols, P.vh, h[v]);
+        if (P.h) store8<A>((T *)P.h + row * P.ldh, (v * TPR + t) * 8, P.cols, h[v]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fmaf(h[v][i], h[v][i], sum);
     }
@@ -149,11 +147,14 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
     if (t == 0 && P.rstd) P.rstd[row] = rstd;
     if (!P.y && !P.codes) return;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) norm_out<T>(P, row, (long long)(v * TPR + t) * 8, h[v], rstd);
+    for (int v = 0; v < NV; ++v) {
+        hold(h[v]);
+        norm_out<T, A>(P, row, (v * TPR + t) * 8, h[v], rstd);
+    }
 }
 
 // Rows that are longer than the threads' registers: read twice, the second time mostly from L2.
-template <class T, int TPR>
+template <class T, int A, int TPR>
 __global__ void __launch_bounds__(TPR) k_norm_forward_long(const __grid_constant__ NormParams P)
 {
     __shared__ double slots[32];
@@ -161,9 +162,9 @@ __global__ void __launch_bounds__(TPR) k_norm_forward_long(const __grid_constant
     pdl_launch_dependents();
     const long long row = blockIdx.x;
     double sum = 0.0;
-    for (long long c = threadIdx.x * 8; c < P.cols; c += TPR * 8) {
-        const Eight<T> h = load_h<T>(P, row, c);
-        if (P.h) store8((T *)P.h + row * P.ldh, c, P.cols, P.vh, h);
+    for (int c = threadIdx.x * 8; c < P.cols; c += TPR * 8) {
+        const Eight<T> h = load_h<T, A>(P, row, c);
+        if (P.h) store8<A>((T *)P.h + row * P.ldh, c, P.cols, h);
         double part = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) part += (double)h[i] * h[i];
@@ -172,18 +173,18 @@ __global__ void __launch_bounds__(TPR) k_norm_forward_long(const __grid_constant
     const float rstd = rstd_of(row_sum<TPR>(sum, slots), P.cols, P.eps);
     if (threadIdx.x == 0 && P.rstd) P.rstd[row] = rstd;
     if (!P.y && !P.codes) return;
-    for (long long c0 = 0; c0 < P.cols; c0 += TPR * 8) {            // (all lanes stay for the shuffles)
-        const long long c = c0 + threadIdx.x * 8;
+    for (int c0 = 0; c0 < P.cols; c0 += TPR * 8) {            // (all lanes stay for the shuffles)
+        const int c = c0 + threadIdx.x * 8;
         // what this thread wrote to h, or x and the residual again where there is no h
-        const Eight<T> h = P.h ? load8((const T *)P.h + row * P.ldh, c, P.cols, P.vh) : load_h<T>(P, row, c);
-        norm_out<T>(P, row, c, h, rstd);
+        const Eight<T> h = P.h ? load8<A>((const T *)P.h + row * P.ldh, c, P.cols) : load_h<T, A>(P, row, c);
+        norm_out<T, A>(P, row, c, h, rstd);
     }
 }
 
 // ------------------------------------------------------------------ backward
 // dx of columns c .. c+7; q: the mean that is taken out.
-template <class T>
-__device__ __forceinline__ void norm_back_out(const NormBackParams &P, long long row, long long c, const Eight<T> &dy, const Eight<T> &h,
+template <class T, int A>
+__device__ __forceinline__ void norm_back_out(const NormBackParams &P, long long row, int c, const Eight<T> &dy, const Eight<T> &h,
                                               const Eight<T> &dh, const float (&g)[8], float rstd, float q)
 {
     float d[8];
@@ -196,21 +197,26 @@ __device__ __forceinline__ void norm_back_out(const NormBackParams &P, long long
         Eight<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o.v[i] = from_f32<T>(d[i]);
-        store8((T *)P.dx + row * P.ldx, c, P.cols, P.vx, o);
+        store8<A>((T *)P.dx + row * P.ldx, c, P.cols, o);
     }
     if (P.codes) {
         if (c + 8 > P.cols) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = c + i < P.cols ? d[i] : 0.0f;
         }
-        encode8(d, P.codes + row * P.ldc, P.scales + row * P.lds, c, P.cols);
+        encode8<A>(d, P.codes + row * P.ldc, P.scales + row * P.lds, c, P.cols);
     }
 }
 
+// CTAs that an SM shall hold: 768 threads (80 registers each) keep memory busy; fp32 operands take more registers.
+template <class T, int TPR> struct BackCtas {
+    static constexpr int THREADS_SM = sizeof(T) == 4 ? 512 : 768, B = RowThreads<TPR>::BLOCK, N = THREADS_SM / B > 0 ? THREADS_SM / B : 1;
+};
+
 // A CTA takes every gridDim-th row (group of rows), so that a thread's sums for dgain stay in its registers; they leave
 // once, as one of the slots that k_norm_dgain adds up.
-template <class T, int TPR, int NV>
-__global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_backward(const __grid_constant__ NormBackParams P)
+template <class T, int A, int TPR, int NV>
+__global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackCtas<T, TPR>::N) k_norm_backward(const __grid_constant__ NormBackParams P)
 {
     constexpr int ROWS = RowThreads<TPR>::ROWS;
     __shared__ float slots[2][32];
@@ -221,22 +227,22 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_backward(const 
     float g[NV][8], acc[NV][8] = {};
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-        if (KEEP) load_gain<T>(P.gain, P.gain_f32, P.vg, (long long)(v * TPR + t) * 8, P.cols, g[v]);
+        if (KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
     int turn = 0;
     for (long long row = (long long)blockIdx.x * ROWS + sub; row < P.rows; row += (long long)gridDim.x * ROWS, turn ^= 1) {
         Eight<T> dy[NV], h[NV], dh[NV];
         const float rstd = P.rstd[row];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const long long c = (long long)(v * TPR + t) * 8;
-            dy[v] = load8((const T *)P.dy + row * P.ldy, c, P.cols, P.vy);
-            h[v] = load8((const T *)P.h + row * P.ldh, c, P.cols, P.vh);
-            if (P.dh) dh[v] = load8((const T *)P.dh + row * P.ldd, c, P.cols, P.vd);
+            const int c = (v * TPR + t) * 8;
+            dy[v] = load8<A>((const T *)P.dy + row * P.ldy, c, P.cols);
+            h[v] = load8<A>((const T *)P.h + row * P.ldh, c, P.cols);
+            if (P.dh) dh[v] = load8<A>((const T *)P.dh + row * P.ldd, c, P.cols);
         }
         float sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if (!KEEP) load_gain<T>(P.gain, P.gain_f32, P.vg, (long long)(v * TPR + t) * 8, P.cols, g[v]);
+            if (!KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float p = dy[v][i] * (h[v][i] * rstd);
@@ -248,15 +254,17 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_backward(const 
         const float q = row_sum<TPR>(sum, slots[turn]) / (float)P.cols;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            if (!KEEP) load_gain<T>(P.gain, P.gain_f32, P.vg, (long long)(v * TPR + t) * 8, P.cols, g[v]);
-            norm_back_out<T>(P, row, (long long)(v * TPR + t) * 8, dy[v], h[v], dh[v], g[v], rstd, q);
+            if (!KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
+            hold(dy[v]);
+            hold(h[v]);
+            norm_back_out<T, A>(P, row, (v * TPR + t) * 8, dy[v], h[v], dh[v], g[v], rstd, q);
         }
     }
     if (!P.part) return;
     float *part = P.part + ((long long)blockIdx.x * ROWS + sub) * P.ld_part;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const long long c = (long long)(v * TPR + t) * 8;
+        const int c = (v * TPR + t) * 8;
         if (c >= P.ld_part) continue;                   // (ld_part is a multiple of 8)
         *reinterpret_cast<float4 *>(part + c) = make_float4(acc[v][0], acc[v][1], acc[v][2], acc[v][3]);
         *reinterpret_cast<float4 *>(part + c + 4) = make_float4(acc[v][4], acc[v][5], acc[v][6], acc[v][7]);
@@ -264,7 +272,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_backward(const 
 }
 
 // Longer rows: dx by a CTA per row that reads it twice ...
-template <class T, int TPR>
+template <class T, int A, int TPR>
 __global__ void __launch_bounds__(TPR) k_norm_backward_long(const __grid_constant__ NormBackParams P)
 {
     __shared__ float slots[32];
@@ -274,37 +282,37 @@ __global__ void __launch_bounds__(TPR) k_norm_backward_long(const __grid_constan
     const T *dyr = (const T *)P.dy + row * P.ldy, *hr = (const T *)P.h + row * P.ldh;
     const float rstd = P.rstd[row];
     float sum = 0.0f, g[8];
-    for (long long c = threadIdx.x * 8; c < P.cols; c += TPR * 8) {
-        const Eight<T> dy = load8(dyr, c, P.cols, P.vy), h = load8(hr, c, P.cols, P.vh);
-        load_gain<T>(P.gain, P.gain_f32, P.vg, c, P.cols, g);
+    for (int c = threadIdx.x * 8; c < P.cols; c += TPR * 8) {
+        const Eight<T> dy = load8<A>(dyr, c, P.cols), h = load8<A>(hr, c, P.cols);
+        load_gain<T, A>(P.gain, P.gain_f32, c, P.cols, g);
         float part = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) part = fmaf(dy[i] * (h[i] * rstd), g[i], part);
         sum += part;
     }
     const float q = row_sum<TPR>(sum, slots) / (float)P.cols;
-    for (long long c0 = 0; c0 < P.cols; c0 += TPR * 8) {
-        const long long c = c0 + threadIdx.x * 8;
-        const Eight<T> dy = load8(dyr, c, P.cols, P.vy), h = load8(hr, c, P.cols, P.vh);
+    for (int c0 = 0; c0 < P.cols; c0 += TPR * 8) {
+        const int c = c0 + threadIdx.x * 8;
+        const Eight<T> dy = load8<A>(dyr, c, P.cols), h = load8<A>(hr, c, P.cols);
         Eight<T> dh;
-        if (P.dh) dh = load8((const T *)P.dh + row * P.ldd, c, P.cols, P.vd);
-        load_gain<T>(P.gain, P.gain_f32, P.vg, c, P.cols, g);
-        norm_back_out<T>(P, row, c, dy, h, dh, g, rstd, q);
+        if (P.dh) dh = load8<A>((const T *)P.dh + row * P.ldd, c, P.cols);
+        load_gain<T, A>(P.gain, P.gain_f32, c, P.cols, g);
+        norm_back_out<T, A>(P, row, c, dy, h, dh, g, rstd, q);
     }
 }
 
 // ... and the sums for dgain by strips of THREADS * 8 columns, ahead of it (dx may be dy itself): a CTA takes every
 // gridDim.y-th row.
-template <class T>
+template <class T, int A>
 __global__ void __launch_bounds__(THREADS) k_norm_dgain_long(const __grid_constant__ NormBackParams P)
 {
     pdl_wait();
     pdl_launch_dependents();
-    const long long c = ((long long)blockIdx.x * THREADS + threadIdx.x) * 8;
+    const int c = (int)(blockIdx.x * THREADS + threadIdx.x) * 8;
     if (c >= P.ld_part) return;
     float acc[8] = {};
     for (long long row = blockIdx.y; row < P.rows; row += gridDim.y) {
-        const Eight<T> dy = load8((const T *)P.dy + row * P.ldy, c, P.cols, P.vy), h = load8((const T *)P.h + row * P.ldh, c, P.cols, P.vh);
+        const Eight<T> dy = load8<A>((const T *)P.dy + row * P.ldy, c, P.cols), h = load8<A>((const T *)P.h + row * P.ldh, c, P.cols);
         const float rstd = P.rstd[row];
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] += dy[i] * (h[i] * rstd);
@@ -314,24 +322,24 @@ __global__ void __launch_bounds__(THREADS) k_norm_dgain_long(const __grid_consta
     *reinterpret_cast<float4 *>(part + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
 }
 
-// dgain = (dgain +) the sum of the slots, in their order by eighths. A CTA takes 32 columns, a warp every eighth slot.
-__global__ void __launch_bounds__(THREADS) k_norm_dgain(const float *part, long long ld, int slots, float *dgain, int cols, int accumulate)
+// dgain = (dgain +) the sum of the slots: a CTA takes 32 columns, a warp every 32nd slot, the warps' sums are added in order.
+constexpr int DGAIN_WARPS = 32;
+static __global__ void __launch_bounds__(DGAIN_WARPS * 32) k_norm_dgain(const float *part, long long ld, int slots, float *dgain, int cols, int accumulate)
 {
-    __shared__ float s[WARPS][32];
+    __shared__ float s[DGAIN_WARPS][33];
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long c = (long long)blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + lane;
     float sum = 0.0f;
     if (c < cols) {
 #pragma unroll 8
-        for (int i = warp; i < slots; i += WARPS) sum += part[i * ld + c];
+        for (int i = warp; i < slots; i += DGAIN_WARPS) sum += part[i * ld + c];
     }
     s[warp][lane] = sum;
     __syncthreads();
     if (warp == 0 && c < cols) {
 #pragma unroll
-        for (int i = 1; i < WARPS; ++i) sum += s[i][lane];
+        for (int i = 1; i < DGAIN_WARPS; ++i) sum += s[i][lane];
         dgain[c] = accumulate ? dgain[c] + sum : sum;
     }
 }
@@ -344,77 +352,121 @@ struct EncodeParams {
     long long ldx, ldc, lds, ld_theta;
     long long rows;
     int cols;
-    int groups;                         // of a row
-    int vx, vt;
+    u32 groups, reciprocal;             // of a row; floor(2^32 / groups), at most 2^32 - 1
 };
 
 constexpr int ENC_UNITS = 4;            // groups of a half-warp, all of whose loads leave together
 
-// Rows: nothing is shared between groups, so half-warps take them one after the other, whatever rows they lie in.
+// Largest magnitude of eight values as they lie in memory; no number if one of them is none. Patterns of 16-bit values
+// are compared two at a time.
+__device__ __forceinline__ float most_raw(const Eight<float> &e)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e.v[i];
+    return most_of(v);
+}
 template <class T>
+__device__ __forceinline__ float most_raw(const Eight<T> &e)
+{
+    const uint4 w = *reinterpret_cast<const uint4 *>(&e);
+    constexpr u32 M = 0x7FFF7FFFu;
+    const u32 m = __vimax3_s16x2(__vimax3_s16x2(w.x & M, w.y & M, w.z & M), w.w & M, 0);
+    const u16 top = (u16)max(m & 0xFFFFu, m >> 16);
+    return to_f32(*reinterpret_cast<const T *>(&top));
+}
+
+// Rows: nothing is shared between groups, so half-warps take them one after the other, whatever rows they lie in.
+template <class T, int A>
 __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__ EncodeParams P)
 {
     pdl_wait();
     pdl_launch_dependents();
     constexpr int HALVES = THREADS / GROUP_LANES;
     const int half = threadIdx.x / GROUP_LANES, lane = threadIdx.x % GROUP_LANES;
-    const u64 units = (u64)P.rows * (u32)P.groups, first = (u64)blockIdx.x * (HALVES * ENC_UNITS);
-    long long row[ENC_UNITS];
+    const u64 units = (u64)P.rows * P.groups, first = (u64)blockIdx.x * (HALVES * ENC_UNITS) + half;
+    u64 row[ENC_UNITS];
     int c[ENC_UNITS];
     Eight<T> e[ENC_UNITS];
 #pragma unroll
     for (int i = 0; i < ENC_UNITS; ++i) {
-        const u64 u = first + i * HALVES + half;
-        const u64 r = units >> 32 ? u / (u32)P.groups : (u64)((u32)u / (u32)P.groups);
-        const bool live = u < units;
-        row[i] = live ? (long long)r : 0;
-        c[i] = live ? (int)(u - r * (u32)P.groups) * GROUP + lane * 8 : P.cols;        // (P.cols: nothing to read or write)
-        e[i] = load8((const T *)P.x + row[i] * P.ldx, c[i], P.cols, P.vx);
+        const u64 u = first + i * HALVES;
+        u32 g;
+        if (units >> 32) {
+            row[i] = u / P.groups;
+            g = (u32)(u - row[i] * P.groups);
+        } else {                        // (the estimate by the reciprocal is the quotient or one less)
+            u32 r = __umulhi((u32)u, P.reciprocal);
+            g = (u32)u - r * P.groups;
+            if (g >= P.groups) {
+                g -= P.groups;
+                r += 1;
+            }
+            row[i] = r;
+        }
+        c[i] = u < units ? (int)g * GROUP + lane * 8 : P.cols;           // (P.cols: nothing to read or write)
+        e[i] = load8<A>((const T *)P.x + row[i] * P.ldx, c[i], P.cols);
     }
 #pragma unroll
     for (int i = 0; i < ENC_UNITS; ++i) {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = e[i][j];
-        encode8(v, P.codes + row[i] * P.ldc, P.scales + row[i] * P.lds, c[i], P.cols);
+        float most = group_most(most_raw(e[i]), 0xFFFFFFFFu);
+        if (is_odd(most)) {
+            most = group_most(most_finite(v), 0xFFFFu << (threadIdx.x & 16));
+            odd_to_nan(v);
+        }
+        const u32 s = scale_of(most);
+        if (c[i] < P.cols) {
+            store_codes<A>(P.codes + row[i] * P.ldc, c[i], P.cols, codes_of(v, scale_inverse(s)));
+            if (lane == 0) P.scales[row[i] * P.lds + c[i] / GROUP] = (u8)s;
+        }
     }
 }
 
-// Blocks of 128 x 128: a CTA each, sixteen rows at a time.
-template <class T>
-__global__ void __launch_bounds__(THREADS) k_encode_blocks(const __grid_constant__ EncodeParams P)
+// Blocks of 128 x 128: a CTA each, thirty-two rows at a time.
+constexpr int ENC_BLOCK = 512;
+template <class T, int A>
+__global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_constant__ EncodeParams P)
 {
-    __shared__ u32 s_most[2][WARPS];
+    constexpr int STEP = ENC_BLOCK / GROUP_LANES, N = GROUP / STEP, W = ENC_BLOCK / 32;
+    __shared__ float s_most[2][W];
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int STEP = THREADS / GROUP_LANES, N = GROUP / STEP;
-    const long long bj = blockIdx.x % P.groups, bi = blockIdx.x / P.groups;
-    const long long c = bj * GROUP + threadIdx.x % GROUP_LANES * 8, r0 = bi * GROUP + threadIdx.x / GROUP_LANES;
+    const u32 bi = blockIdx.x / P.groups, bj = blockIdx.x - bi * P.groups;
+    const int c = (int)bj * GROUP + threadIdx.x % GROUP_LANES * 8;
+    const long long r0 = (long long)bi * GROUP + threadIdx.x / GROUP_LANES;
     Eight<T> e[N];
-    u32 most = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const long long r = r0 + i * STEP;
-        e[i] = load8((const T *)P.x + min(r, P.rows - 1) * P.ldx, r < P.rows ? c : (long long)P.cols, P.cols, P.vx);
+        e[i] = load8<A>((const T *)P.x + r * P.ldx, r < P.rows ? c : P.cols, P.cols);
     }
-    bool odd = false;
+    float most = 0.0f;
 #pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {              // a second time only where something is not finite
-        most = 0;
+    for (int i = 0; i < N; ++i) most = most2(most, most_raw(e[i]));
+    auto join = [&](float *slot) {      // over the CTA
+        most = group_most(most, 0xFFFFFFFFu);
+        most = most2(most, __shfl_xor_sync(0xFFFFFFFFu, most, 16));
+        if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = most;
+        __syncthreads();
+        const float x = slot[threadIdx.x % W];
+        most = group_most(x, 0xFFFFFFFFu);
+    };
+    static_assert(W == GROUP_LANES, "the warps' maxima are one per lane of a group");
+    join(s_most[0]);
+    const bool odd = is_odd(most);      // (the same for the CTA)
+    if (odd) {
+        most = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = e[i][j];
-            most = max(most, most_of(v, pass == 1));
+            most = fmaxf(most, most_finite(v));
         }
-        most = __reduce_max_sync(0xFFFFFFFFu, most);
-        if ((threadIdx.x & 31) == 0) s_most[pass][threadIdx.x >> 5] = most;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) most = max(most, s_most[pass][w]);
-        if (most < 0x7F800000u) break;                  // (the same for the CTA)
-        odd = true;
+        join(s_most[1]);
     }
     const u32 s = scale_of(most);
     const float inverse = scale_inverse(s), scale = scale_value(s);
@@ -426,8 +478,9 @@ __global__ void __launch_bounds__(THREADS) k_encode_blocks(const __grid_constant
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = e[i][j];
-        const uint2 q = codes_of(v, inverse, odd);
-        store_codes(P.codes + r * P.ldc, c, P.cols, q);
+        if (odd) odd_to_nan(v);
+        const uint2 q = codes_of(v, inverse);
+        store_codes<A>(P.codes + r * P.ldc, c, P.cols, q);
         if (P.theta) {
             Eight<float> o;
 #pragma unroll
@@ -438,7 +491,7 @@ __global__ void __launch_bounds__(THREADS) k_encode_blocks(const __grid_constant
                 o.v[2 * j] = f.x * scale;
                 o.v[2 * j + 1] = f.y * scale;
             }
-            store8(P.theta + r * P.ld_theta, c, P.cols, P.vt, o);
+            store8<A>(P.theta + r * P.ld_theta, c, P.cols, o);
         }
     }
 }

@@ -49,11 +49,12 @@ struct OpArgs {
     }
 };
 
-// Access by eights that rows of `e`-byte values allow: 16 bytes, 8, or value by value.
-inline int op_access(const void *p, long long ld, int e)
+// Values of `e` bytes that an access to rows `ld` apart may take at once: 8, 4 or 1 (rows of `cols`).
+inline int op_access(const void *p, long long ld, int e, long long cols)
 {
+    if (!p) return 8;
     const uintptr_t bits = (uintptr_t)p | (uintptr_t)(ld * e);
-    return bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : 0;
+    return bits % 16 == 0 && cols % 8 == 0 ? 8 : bits % (4 * e) == 0 && cols % 4 == 0 ? 4 : 1;
 }
 
 // A launch that may start while the kernel ahead of it ends: every kernel launched so waits for that one before it reads or

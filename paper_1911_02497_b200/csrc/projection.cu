@@ -74,7 +74,7 @@ int run(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x
     P.width = (int)width;
     P.groups = (int)((depth + GROUP - 1) / GROUP);
     P.blocks = (int)((width + PJ_WIDE - 1) / PJ_WIDE);
-    P.vec = op_access(y, ldy, 2);
+    P.access = op_access(y, ldy, 2, width);
     // equal tiles of rows
     const long long tiles = (rows + PJ_MAX_TILE - 1) / PJ_MAX_TILE;
     P.tile = (int)(((rows + tiles - 1) / tiles + 15) / 16 * 16);

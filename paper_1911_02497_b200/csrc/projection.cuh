@@ -35,7 +35,7 @@ struct ProjectionParams {
     int blocks;                         // of 128 output columns
     int tile;                           // rows of a tile, a multiple of 16
     int stages, ring;                   // ring: bytes of the stages, or of the sums that lie there in the end
-    int vec;
+    int access;                         // values of a row of the result that may be written at once
     u32 columns;                        // of tensor memory
 };
 
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(128) k_projection(const __grid_constant__ Proj
     }
     if (parts > 1) cluster.sync();
     const int r0 = P.tile * part / parts, r1 = P.tile * (part + 1) / parts;
-    const long long col = (long long)block * PJ_WIDE + tid % 16 * 8;
+    const int col = block * PJ_WIDE + tid % 16 * 8;
     for (int r = r0 + tid / 16; r < r1; r += 8) {
         if (row0 + r >= P.rows) break;
         float v[8] = {};
@@ -288,7 +288,10 @@ __global__ void __launch_bounds__(128) k_projection(const __grid_constant__ Proj
         Eight<T> e;
 #pragma unroll
         for (int i = 0; i < 8; ++i) e.v[i] = from_f32<T>(v[i]);
-        store8((T *)P.out + (row0 + r) * P.ldo, col, P.width, P.vec, e);
+        T *out = (T *)P.out + (row0 + r) * P.ldo;
+        if (P.access == 8) store8<8>(out, col, P.width, e);
+        else if (P.access == 4) store8<4>(out, col, P.width, e);
+        else store8<1>(out, col, P.width, e);
     }
     if (parts > 1) cluster.sync();      // (nobody leaves while its sums are read)
 }
