@@ -43,7 +43,116 @@ int code_map(condensa_ctx *ctx, CUtensorMap &map, const condensa_coded &c, long 
 
 typedef void (*Kernel)(ProjectionParams);
 
-constexpr int PJ_SMEM_MOST = 227 * 1024, PJ_SMEM_HALF = 113 * 1024, PJ_MAX_PARTS = 8;
+constexpr int PJ_SMEM_MOST = 227 * 1024, PJ_SMEM_HALF = 113 * 1024, PJ_MAX_PARTS = 8, PP_MAX_PARTS = 4;
+
+// How a product is cut.
+struct Shape {
+    bool pair;              // pairs of CTAs, or single ones
+    int tile, parts;        // rows of a tile; CTAs (pairs) that share its depth
+    long long clusters;     // CTAs (pairs) launched: one per tile and part, or as many as the device holds at once
+};
+
+struct Variant {
+    Kernel f;
+    int wide, threads, fixed, stages;       // output columns of a tile; shared memory beside the ring; most stages
+    bool sums;                              // the ring holds a tile's sums in the end
+};
+
+template <class T, bool TRANS>
+Variant variant_of(const Shape &s)
+{
+    if (!s.pair) return {k_projection<T, TRANS>, PJ_WIDE, 128, PJ_PAD + PJ_SLOTS * PJ_SCALES, PJ_STAGES, true};
+    const int fixed = PJ_PAD + PJ_SLOTS * PP_SCALES + PP_OUT;
+    if (s.parts > 1) return {k_projection_pair<T, TRANS, true>, 2 * PJ_WIDE, PP_THREADS, fixed, PP_STAGES, true};
+    return {k_projection_pair<T, TRANS, false>, 2 * PJ_WIDE, PP_THREADS, fixed, PP_STAGES, false};
+}
+
+Variant variant_of(int dtype, bool trans, const Shape &s)
+{
+    return dtype == CONDENSA_DTYPE_BF16 ? (trans ? variant_of<__nv_bfloat16, true>(s) : variant_of<__nv_bfloat16, false>(s))
+                                        : (trans ? variant_of<__half, true>(s) : variant_of<__half, false>(s));
+}
+
+int allow_smem(condensa_ctx *ctx, Kernel k)
+{
+    for (const void *f : ctx->op_smem_set)
+        if (f == (const void *)k) return CONDENSA_OK;
+    CU_TRY(ctx, cudaFuncSetAttribute((const void *)k, cudaFuncAttributeMaxDynamicSharedMemorySize, PJ_SMEM_MOST - 1024));
+    ctx->op_smem_set.push_back((const void *)k);
+    return CONDENSA_OK;
+}
+
+// Clusters of `n` CTAs, one on an SM, that the device holds at once.
+int resident_clusters(condensa_ctx *ctx, const Variant &v, int n, int &count)
+{
+    for (const condensa_ctx::ClusterFit &f : ctx->cluster_fit)
+        if (f.f == (const void *)v.f && f.size == n) {
+            count = f.count;
+            return CONDENSA_OK;
+        }
+    const int rc = allow_smem(ctx, v.f);
+    if (rc) return rc;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)n);
+    cfg.blockDim = dim3((unsigned)v.threads);
+    cfg.dynamicSmemBytes = (size_t)(PJ_SMEM_MOST - 1024);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)n;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    count = 0;
+    CU_TRY(ctx, cudaOccupancyMaxActiveClusters(&count, (const void *)v.f, &cfg));
+    if (count < 1) return fail(ctx, CONDENSA_ERR_INTERNAL, "no cluster of %d CTAs fits the device", n);
+    ctx->cluster_fit.push_back({(const void *)v.f, n, count});
+    return CONDENSA_OK;
+}
+
+// The cut that a simple account in cycles makes cheapest. A group of the depth costs a CTA what the tensor core needs (2 per row of
+// the tile) or what its codes need on their way from L2, whichever is more; then there are the rounds of tiles, and something fixed.
+int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups, int dtype, bool trans, Shape &best)
+{
+    const int quads = (groups + PJ_QUAD - 1) / PJ_QUAD;
+    const double L2 = 56.0;             // bytes a cycle for an SM
+    double least = 0.0;
+    auto offer = [&](const Shape &s, double t) {
+        if (least == 0.0 || t < 0.999 * least) {
+            least = t;
+            best = s;
+        }
+    };
+    {   // single CTAs: equal tiles of up to 128 rows
+        const long long n = (rows + PJ_MAX_TILE - 1) / PJ_MAX_TILE;
+        const int tile = (int)(((rows + n - 1) / n + 15) / 16 * 16);
+        const long long tiles = n * ((width + PJ_WIDE - 1) / PJ_WIDE);
+        const double group = std::max(2.0 * tile, (PJ_A + 128.0 * tile) / L2);
+        for (int parts = 1; parts <= std::min(PJ_MAX_PARTS, quads); ++parts) {
+            const long long ctas = tiles * parts;
+            if (parts > 1 && ctas > ctx->num_sms) break;
+            const double depth = (double)((quads + parts - 1) / parts * PJ_QUAD), rounds = (double)((ctas + ctx->num_sms - 1) / ctx->num_sms);
+            offer({false, tile, parts, ctas}, rounds * (depth * group + 800.0) + 1500.0 + (parts > 1 ? 600.0 : 0.0));
+        }
+    }
+    if (rows > 64) {
+        for (int tile = 64; tile <= PP_TILE; tile += 32) {
+            const long long tiles = (rows + tile - 1) / tile * ((width + 2 * PJ_WIDE - 1) / (2 * PJ_WIDE));
+            const double group = std::max(2.0 * tile, (PJ_A + 64.0 * tile) / L2);
+            for (int parts = 1; parts <= std::min(PP_MAX_PARTS, quads); ++parts) {
+                Shape s = {true, tile, parts, tiles * parts};
+                int fit = 0;
+                const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), 2 * parts, fit);
+                if (rc) return rc;
+                if (parts > 1 && tiles > fit) break;
+                if (parts == 1) s.clusters = std::min(tiles, (long long)fit);
+                const double depth = (double)((quads + parts - 1) / parts * PJ_QUAD), rounds = (double)((tiles + fit - 1) / fit);
+                offer(s, rounds * (depth * group + 300.0) + 3500.0 + (parts > 1 ? 2000.0 : 0.0));
+            }
+        }
+    }
+    return CONDENSA_OK;
+}
 
 int run(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x, long long rows, void *y, long long ldy, int dtype, bool trans,
         cudaStream_t stream)
@@ -73,45 +182,37 @@ int run(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x
     P.rows = rows;
     P.width = (int)width;
     P.groups = (int)((depth + GROUP - 1) / GROUP);
-    P.blocks = (int)((width + PJ_WIDE - 1) / PJ_WIDE);
     P.access = op_access(y, ldy, 2, width);
-    // equal tiles of rows
-    const long long tiles = (rows + PJ_MAX_TILE - 1) / PJ_MAX_TILE;
-    P.tile = (int)(((rows + tiles - 1) / tiles + 15) / 16 * 16);
     const int quads = (P.groups + PJ_QUAD - 1) / PJ_QUAD;
-    long long ctas = tiles * P.blocks;
-    int parts = 1;
-    while (parts < PJ_MAX_PARTS && parts < quads && ctas * (parts + 1) <= ctx->num_sms) ++parts;
-    ctas *= parts;
-    if (ctas > 0x7FFFFFFFll) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "too many tiles for one launch");
-    const int stage = PJ_A + P.tile * GROUP, fixed = PJ_PAD + PJ_SLOTS * PJ_SCALES + 1024;
-    const int room = (ctas > ctx->num_sms ? PJ_SMEM_HALF : PJ_SMEM_MOST) - fixed;
-    const int deepest = (quads + parts - 1) / parts * PJ_QUAD;
-    P.stages = std::min(std::min(PJ_STAGES, deepest), room / stage);
-    P.ring = std::max(P.stages * stage, P.tile * PJ_WIDE * 4);
+    Shape shape;
+    if ((rc = choose_shape(ctx, rows, width, P.groups, dtype, trans, shape)) != 0) return rc;
+    const Variant v = variant_of(dtype, trans, shape);
+    const int high = shape.pair ? shape.tile / 2 : shape.tile, stage = PJ_A + high * GROUP, deepest = (quads + shape.parts - 1) / shape.parts * PJ_QUAD;
+    P.tile = shape.tile;
+    P.blocks = (int)((width + v.wide - 1) / v.wide);
+    const long long tiles = (rows + P.tile - 1) / P.tile * P.blocks, ctas = std::min(tiles * shape.parts, shape.clusters) * (shape.pair ? 2 : 1);
+    if (tiles * shape.parts > 0x3FFFFFFFll) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "too many tiles for one launch");
+    P.tiles = (int)tiles;
+    // as many stages as there is room for (a CTA by itself shares its SM where there are more of them than SMs)
+    const int fixed = v.fixed + 1024, room = (!shape.pair && ctas > ctx->num_sms ? PJ_SMEM_HALF : PJ_SMEM_MOST) - fixed;
+    P.stages = std::min(std::min(v.stages, deepest), room / stage);
+    P.ring = std::max(P.stages * stage, v.sums ? P.tile * PJ_WIDE * 4 : 0);
     P.columns = 32;
     while (P.columns < (u32)P.tile + 16) P.columns *= 2;
     if ((rc = code_map(ctx, P.w, w->code, w->n, w->k, PJ_WIDE)) != 0) return rc;
-    if ((rc = code_map(ctx, P.x, *x, rows, depth, P.tile)) != 0) return rc;
-    const Kernel k = dtype == CONDENSA_DTYPE_BF16 ? (trans ? k_projection<__nv_bfloat16, true> : k_projection<__nv_bfloat16, false>)
-                                                  : (trans ? k_projection<__half, true> : k_projection<__half, false>);
-    bool known = false;
-    for (const void *f : ctx->op_smem_set) known = known || f == (const void *)k;
-    if (!known) {
-        CU_TRY(ctx, cudaFuncSetAttribute((const void *)k, cudaFuncAttributeMaxDynamicSharedMemorySize, PJ_SMEM_MOST - 1024));
-        ctx->op_smem_set.push_back((const void *)k);
-    }
-    PdlLaunch l(ctx, 1, 128, (size_t)(PJ_PAD + P.ring + PJ_SLOTS * PJ_SCALES), stream);
+    if ((rc = code_map(ctx, P.x, *x, rows, depth, high)) != 0) return rc;
+    if ((rc = allow_smem(ctx, v.f)) != 0) return rc;
+    PdlLaunch l(ctx, 1, v.threads, (size_t)(v.fixed + P.ring), stream);
     l.cfg.gridDim = dim3((unsigned)ctas);
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)parts;
+    at[0].val.clusterDim.x = (unsigned)(shape.parts * (shape.pair ? 2 : 1));
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     at[1] = l.attr;
     l.cfg.attrs = at;
     l.cfg.numAttrs += 1;
     const int pa_ = prof_begin(ctx, trans ? "k_projection_back" : "k_projection", stream);
-    CU_TRY(ctx, cudaLaunchKernelEx(&l.cfg, k, P));
+    CU_TRY(ctx, cudaLaunchKernelEx(&l.cfg, v.f, P));
     ctx->launches += 1;
     prof_end(ctx, pa_, stream);
     return CONDENSA_OK;

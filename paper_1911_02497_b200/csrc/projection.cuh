@@ -18,7 +18,10 @@ namespace cs {
 constexpr int PJ_WIDE = 128;            // output columns of a tile
 constexpr int PJ_QUAD = 4;              // groups of the depth whose scales share a word
 constexpr int PJ_STAGES = 12;           // most stages of the ring
-constexpr int PJ_SLOTS = 4;             // quads of scales in shared memory
+// Two warps bring the scales, two quads at a time and in turn: a warp's loads for its next two are on their way while it waits for
+// room. (The fence ahead of the tensor core's copy waits for all of a thread's loads, so one warp that loaded ahead of its
+// fences took 1.4 us for each quad, more than its products: 2.2 PFLOP/s.)
+constexpr int PJ_BATCH = 2, PJ_SLOTS = 2 * PJ_BATCH;    // quads
 constexpr int PJ_A = GROUP * PJ_WIDE;   // bytes of a stage's weights
 constexpr int PJ_SCALES = 1024;         // bytes of a quad's scales: weights, rows
 constexpr int PJ_PAD = 1024;            // swizzle patterns start at multiples of 1024 bytes
@@ -32,7 +35,8 @@ struct ProjectionParams {
     void *out;
     long long rows;
     int width, groups;                  // output columns, groups of the depth
-    int blocks;                         // of 128 output columns
+    int blocks;                         // of 128 output columns; of pairs: of 256
+    int tiles;                          // pairs: tiles in all
     int tile;                           // rows of a tile, a multiple of 16
     int stages, ring;                   // ring: bytes of the stages, or of the sums that lie there in the end
     int access;                         // values of a row of the result that may be written at once
@@ -40,6 +44,14 @@ struct ProjectionParams {
 };
 
 __device__ __forceinline__ u32 smem_u32(const void *p) { return (u32)__cvta_generic_to_shared(p); }
+// One lane of a warp whose lanes are all here. The compiler knows the region behind it for a single thread's, which a comparison of the
+// lane's number does not tell it: products alone, 128 rows, went from 230 to 160 ns for a group of the depth.
+__device__ __forceinline__ bool elect_one()
+{
+    u32 p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 __device__ __forceinline__ void mbar_init(u32 bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void mbar_expect(u32 bar, u32 bytes) { asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory"); }
 __device__ __forceinline__ void mbar_arrive(u32 bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
@@ -87,53 +99,126 @@ __device__ __forceinline__ void tmem_ld(u32 addr, float (&v)[16])
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
                    "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]) : "r"(addr));
 }
-__device__ __forceinline__ void tmem_ld_wait(float (&v)[16])
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait(float (&v)[N])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 16; ++i) asm volatile("" : "+f"(v[i]));          // (no use of the values may move ahead of the wait)
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));          // (no use of the values may move ahead of the wait)
 }
 
-// The scale bytes of a quad: of 128 output columns' weights, the same for all of them ...
-__device__ __forceinline__ u32 weight_scales(const ProjectionParams &P, int quad, long long block)
-{
-    u32 word = 0;
+// The scale bytes of a quad on their way to shared memory: those of 128 output columns' weights, the same for all of them, and
+// those of the rows `lane`, `lane` + 32, ... of a tile. Nothing here is looked at before it is stored, so that the loads of several
+// quads are under way at once (with a use behind each load a quad took 1.5 us, more than its products: 2.2 PFLOP/s).
+template <int N>
+struct QuadScales {
+    u32 w[PJ_QUAD], x[N];
+
+    __device__ __forceinline__ void fetch(const ProjectionParams &P, int quad, long long block, long long row)
+    {
+        const u8 *s = P.w_scales + min(block, (long long)(P.width - 1) / GROUP) * P.w_wide;
+        const int g = quad * PJ_QUAD;
 #pragma unroll
-    for (int b = 0; b < PJ_QUAD; ++b) {
-        const int g = quad * PJ_QUAD + b;
-        if (g < P.groups) word |= (u32)P.w_scales[g * P.w_depth + block * P.w_wide] << (8 * b);
+        for (int b = 0; b < PJ_QUAD; ++b) w[b] = s[min(g + b, P.groups - 1) * P.w_depth];       // (past the last group: anything, it is not used)
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+            if (c * 32 < P.tile) {
+                const long long r = min(row + c * 32, P.rows - 1);      // (past the last row: the same)
+                const u8 *at = P.x_scales + r * P.ld_xs + g;
+                if (g + PJ_QUAD <= P.groups || r + 1 < P.rows) {
+                    x[c] = *reinterpret_cast<const u32 *>(at);          // a row's last word lies within its stride ...
+                } else {                                                // ... but for the last row, which may end with its groups
+                    x[c] = 0;
+                    for (int b = 0; g + b < P.groups; ++b) x[c] |= (u32)at[b] << (8 * b);
+                }
+            } else {
+                x[c] = 0;
+            }
     }
-    return word;
-}
-// ... and of a row (past the last one: anything, its sums are not used).
-__device__ __forceinline__ u32 row_scales(const ProjectionParams &P, int quad, long long row)
-{
-    if (row >= P.rows) return 0;
-    const u8 *s = P.x_scales + row * P.ld_xs + quad * PJ_QUAD;
-    if (quad * PJ_QUAD + PJ_QUAD <= P.groups) return *reinterpret_cast<const u32 *>(s);
-    u32 word = 0;
+    // 512 bytes for the weights, 512 for each 128 rows: 32 lanes of four words
+    __device__ __forceinline__ void store(char *to, int lane) const
+    {
+        const u32 a = w[0] | w[1] << 8 | w[2] << 16 | w[3] << 24;
+        uint4 *d = reinterpret_cast<uint4 *>(to) + lane;
+        d[0] = make_uint4(a, a, a, a);
 #pragma unroll
-    for (int b = 0; b < PJ_QUAD - 1; ++b)
-        if (quad * PJ_QUAD + b < P.groups) word |= (u32)s[b] << (8 * b);
-    return word;
+        for (int i = 0; i < (N + 3) / 4; ++i) d[32 * (i + 1)] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], 4 * i + 3 < N ? x[4 * i + 3 < N ? 4 * i + 3 : 0] : 0u);
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void store_result(const ProjectionParams &P, long long row, int col, const Eight<T> &e)
+{
+    T *out = (T *)P.out + row * P.ldo;
+    if (P.access == 8) store8<8>(out, col, P.width, e);
+    else if (P.access == 4) store8<4>(out, col, P.width, e);
+    else store8<1>(out, col, P.width, e);
+}
+
+// Sums of rows r0 .. r1 - 1 of a tile over `parts` CTAs of the cluster (every `step`th from `first` on), in their order, into the result.
+// The loads of all parts, and of two rows, leave together: one after the other they took 10 us for four parts.
+template <class T, int THREADS_>
+__device__ __forceinline__ void add_parts(const ProjectionParams &P, cooperative_groups::cluster_group &cluster, float *sums, int parts, int first, int step, bool fine,
+                                          long long row0, int r0, int r1, int col0)
+{
+    constexpr int AHEAD = 4, ROWS = THREADS_ / 16;
+    const int c = threadIdx.x % 16 * 8;
+    r1 = (int)min((long long)r1, P.rows - row0);
+    for (int r = r0 + (int)threadIdx.x / 16; r < r1; r += 2 * ROWS) {
+        float v[2][8];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = fine ? 0.0f : __uint_as_float(0x7FFFFFFFu);
+        for (int p = 0; p < parts; p += AHEAD) {
+            float4 x[AHEAD][2][2];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                if (p + j < parts) {
+                    const float *at = (parts > 1 ? cluster.map_shared_rank(sums, first + (p + j) * step) : sums) + c;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        if (r + k * ROWS < r1) {
+                            x[j][k][0] = *reinterpret_cast<const float4 *>(at + (r + k * ROWS) * PJ_WIDE);
+                            x[j][k][1] = *reinterpret_cast<const float4 *>(at + (r + k * ROWS) * PJ_WIDE + 4);
+                        }
+                }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                if (p + j < parts)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        v[k][0] += x[j][k][0].x; v[k][1] += x[j][k][0].y; v[k][2] += x[j][k][0].z; v[k][3] += x[j][k][0].w;
+                        v[k][4] += x[j][k][1].x; v[k][5] += x[j][k][1].y; v[k][6] += x[j][k][1].z; v[k][7] += x[j][k][1].w;
+                    }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (r + k * ROWS < r1) {
+                Eight<T> e;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e.v[i] = from_f32<T>(v[k][i]);
+                store_result<T>(P, row0 + r + k * ROWS, col0 + c, e);
+            }
+    }
 }
 
 // A cluster of CTAs takes a tile: its CTAs share the depth by quads, each leaves its sums in its own shared memory, and
 // each adds up a part of the tile's rows over all of them, in their order, by distributed shared memory.
-// Four warps: copies, products, scales, tensor memory; then all take the sums.
+// Four warps: copies, products, and two for the scales; then all take the sums.
 template <class T, bool TRANS>
-__global__ void __launch_bounds__(128) k_projection(const __grid_constant__ ProjectionParams P)
+__global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ ProjectionParams P)
 {
     extern __shared__ char pj_raw[];
-    __shared__ u64 bars[2 * PJ_STAGES + 2 * PJ_SLOTS + 1];
+    __shared__ u64 bars[2 * PJ_STAGES + 4 + 1];
     __shared__ u32 s_tmem;
     __shared__ int s_fail;
     char *ring = pj_raw + ((PJ_PAD - (smem_u32(pj_raw) & (PJ_PAD - 1))) & (PJ_PAD - 1));
     char *scales = ring + P.ring;
     const u32 ring_u = smem_u32(ring), scales_u = smem_u32(scales);
-    const u32 full = smem_u32(bars), empty = full + 8 * PJ_STAGES, sc_full = empty + 8 * PJ_STAGES, sc_empty = sc_full + 8 * PJ_SLOTS,
-              done = sc_empty + 8 * PJ_SLOTS;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const u32 full = smem_u32(bars), empty = full + 8 * PJ_STAGES, sc_full = empty + 8 * PJ_STAGES, sc_empty = sc_full + 16,
+              done = sc_empty + 16;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -151,7 +236,7 @@ __global__ void __launch_bounds__(128) k_projection(const __grid_constant__ Proj
             mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
-        for (int s = 0; s < PJ_SLOTS; ++s) {
+        for (int s = 0; s < 2; ++s) {
             mbar_init(sc_full + 8 * s, 1);
             mbar_init(sc_empty + 8 * s, 1);
         }
@@ -171,7 +256,7 @@ __global__ void __launch_bounds__(128) k_projection(const __grid_constant__ Proj
     pdl_launch_dependents();
 
     if (warp == 0) {                    // ---- copies
-        if (lane == 0) {
+        if (elect_one()) {
             int stage = 0;
             u32 turn = 0;
             for (int g = g0; g < g1; ++g) {
@@ -191,18 +276,20 @@ __global__ void __launch_bounds__(128) k_projection(const __grid_constant__ Proj
             }
         }
     } else if (warp == 1) {             // ---- products
-        if (lane == 0) {
+        if (elect_one()) {
             const u32 idesc = umma_idesc(TRANS, PJ_WIDE, P.tile);
             const u32 sa = tmem + (u32)P.tile;
             int stage = 0;
             u32 turn = 0;
             bool fine = true;
             for (int q = q0; q < q1 && fine; ++q) {
-                const int slot = (q - q0) % PJ_SLOTS;
-                const u32 to = sa + (u32)((q - q0) & 1) * 8;
-                fine = mbar_wait(sc_full + 8 * slot, (u32)((q - q0) / PJ_SLOTS) & 1);
-                if (!fine) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const int i = q - q0, slot = i % PJ_SLOTS, batch = i / PJ_BATCH;
+                const u32 to = sa + (u32)(i & 1) * 8;
+                if (i % PJ_BATCH == 0) {
+                    fine = mbar_wait(sc_full + 8 * (batch & 1), (u32)(batch / 2) & 1);
+                    if (!fine) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                }
                 scales_to_tmem(to, umma_desc(scales_u + (u32)slot * PJ_SCALES, 128, 0));
                 scales_to_tmem(to + 4, umma_desc(scales_u + (u32)slot * PJ_SCALES + 512, 128, 0));
                 for (int g = q * PJ_QUAD; g < min((q + 1) * PJ_QUAD, g1); ++g) {
@@ -221,32 +308,33 @@ __global__ void __launch_bounds__(128) k_projection(const __grid_constant__ Proj
                         turn ^= 1;
                     }
                 }
-                if (fine) umma_commit(sc_empty + 8 * slot);
+                if (fine && i % PJ_BATCH == PJ_BATCH - 1) umma_commit(sc_empty + 8 * (batch & 1));
             }
             if (!fine) s_fail = 1;
             umma_commit(done);
         }
-    } else if (warp == 2) {             // ---- scales
-        u32 wa = 0, wx[4];
+    } else {                            // ---- scales
+        const int side = warp - 2;
+        QuadScales<4> next[PJ_BATCH];
         auto fetch = [&](int q) {
-            wa = weight_scales(P, q, block);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) wx[c] = c * 32 < P.tile ? row_scales(P, q, row0 + c * 32 + lane) : 0u;
+            for (int j = 0; j < PJ_BATCH; ++j)
+                if (q + j < q1) next[j].fetch(P, q + j, block, row0 + lane);
         };
-        if (q0 < q1) fetch(q0);
-        for (int q = q0; q < q1; ++q) {
-            const int i = q - q0, slot = i % PJ_SLOTS;
-            if (i >= PJ_SLOTS && !mbar_wait(sc_empty + 8 * slot, (u32)(i / PJ_SLOTS - 1) & 1)) {
+        int q = q0 + side * PJ_BATCH;
+        fetch(q);
+        for (u32 turn = 0; q < q1; q += PJ_SLOTS, turn ^= 1) {
+            if (q >= q0 + PJ_SLOTS && !mbar_wait(sc_empty + 8 * side, turn ^ 1)) {
                 s_fail = 1;
                 break;
             }
-            uint4 *to = reinterpret_cast<uint4 *>(scales + slot * PJ_SCALES) + lane;
-            to[0] = make_uint4(wa, wa, wa, wa);
-            to[32] = make_uint4(wx[0], wx[1], wx[2], wx[3]);
+#pragma unroll
+            for (int j = 0; j < PJ_BATCH; ++j)
+                if (q + j < q1) next[j].store(scales + (side * PJ_BATCH + j) * PJ_SCALES, lane);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(sc_full + 8 * slot);
-            if (q + 1 < q1) fetch(q + 1);
+            if (lane == 0) mbar_arrive(sc_full + 8 * side);
+            fetch(q + PJ_SLOTS);
         }
     }
     __syncwarp();
@@ -274,26 +362,319 @@ __global__ void __launch_bounds__(128) k_projection(const __grid_constant__ Proj
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(P.columns) : "memory");
     }
     if (parts > 1) cluster.sync();
-    const int r0 = P.tile * part / parts, r1 = P.tile * (part + 1) / parts;
-    const int col = block * PJ_WIDE + tid % 16 * 8;
-    for (int r = r0 + tid / 16; r < r1; r += 8) {
-        if (row0 + r >= P.rows) break;
-        float v[8] = {};
-        for (int p = 0; p < parts; ++p) {
-            const float4 *s = reinterpret_cast<const float4 *>((parts > 1 ? cluster.map_shared_rank(sums, p) : sums) + r * PJ_WIDE + tid % 16 * 8);
-            const float4 x = s[0], y = s[1];
-            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-            v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-        }
-        Eight<T> e;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e.v[i] = from_f32<T>(v[i]);
-        T *out = (T *)P.out + (row0 + r) * P.ldo;
-        if (P.access == 8) store8<8>(out, col, P.width, e);
-        else if (P.access == 4) store8<4>(out, col, P.width, e);
-        else store8<1>(out, col, P.width, e);
-    }
+    add_parts<T, 128>(P, cluster, sums, parts, 0, 1, true, row0, P.tile * part / parts, P.tile * (part + 1) / parts, block * PJ_WIDE);
     if (parts > 1) cluster.sync();      // (nobody leaves while its sums are read)
+}
+
+// ------------------------------------------------------------------ many rows: pairs of CTAs
+// Two CTAs of a cluster form one product of 256 output columns (tcgen05 cta_group::2): each brings its own 128 columns of
+// weights and half of the rows, and keeps its 128 columns' sums; per byte that an SM takes from L2 this is up to 1.7 times the work
+// of a CTA by itself. The first CTA of the pair issues the products. Persistent: two accumulators in tensor memory take
+// turns, so that four warps write out a tile while the next one is multiplied. SPLIT: the pairs of a cluster share one
+// tile's depth instead, as in the kernel above.
+constexpr int PP_THREADS = 256;
+constexpr int PP_TILE = 224;            // most rows of a tile: two accumulators and the scales fill tensor memory
+constexpr int PP_STAGES = 8;
+constexpr int PP_SCALES = 1536;         // bytes of a quad's scales: weights, rows
+constexpr int PP_COLUMNS = 512;
+constexpr int PP_OUT = 4 * 2048;        // where the four warps turn their sums around
+
+__device__ __forceinline__ u32 peer_address(u32 addr, u32 rank)
+{
+    u32 r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+// An arrival at a barrier of any CTA of the cluster, and the wait that sees what came before it.
+__device__ __forceinline__ void mbar_arrive_at(u32 cluster_addr) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_addr) : "memory"); }
+__device__ __forceinline__ bool mbar_wait_cluster(u32 bar, u32 ph)
+{
+    for (int i = 0; i < (1 << 20); ++i) {
+        u32 done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(ph), "r"(1000u) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+// A box into this CTA's shared memory, counted at a barrier of either CTA of the pair.
+__device__ __forceinline__ void tma_load_pair(u32 dst, const CUtensorMap *map, int x, int y, u32 bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void umma_scaled_pair(u32 d, u64 a, u64 b, u32 idesc, u32 scale_a, u32 scale_b, u32 add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\ttcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(add) : "memory");
+}
+// Each CTA's scales, from its own shared memory into its own tensor memory.
+__device__ __forceinline__ void scales_to_tmem_pair(u32 tmem, u64 desc)
+{
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(tmem), "l"(desc) : "memory");
+}
+// Arrives at the barrier of this address in both CTAs once the products so far are done.
+__device__ __forceinline__ void umma_commit_pair(u32 bar, u32 ranks)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((u16)ranks) : "memory");
+}
+__device__ __forceinline__ void tmem_ld(u32 addr, float (&v)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+                   "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
+                   "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+                   "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]) : "r"(addr));
+}
+__device__ __forceinline__ u32 pack2(float lo, float hi, __half) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const u32 *>(&h); }
+__device__ __forceinline__ u32 pack2(float lo, float hi, __nv_bfloat16) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const u32 *>(&h); }
+
+// Sums of 32 rows x 32 output columns, a column per lane, into the result: neighbouring rows go as pairs through the
+// warp's 2 KB of shared memory and come back as eight neighbouring columns of a row.
+template <class T>
+__device__ __forceinline__ void write_block(const ProjectionParams &P, const float (&v)[32], u32 *turn, long long row0, int col0, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) turn[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int i = r * 8 + lane / 4, n8 = lane % 4 * 8, first = (i & 1) * 4;      // (odd pairs read their halves the other way round: no bank conflicts)
+        uint4 w[2];
+        w[0] = *reinterpret_cast<const uint4 *>(turn + i * 32 + n8 + first);
+        w[1] = *reinterpret_cast<const uint4 *>(turn + i * 32 + n8 + (4 - first));
+        const uint4 a = first ? w[1] : w[0], b = first ? w[0] : w[1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u32 sel = h ? 0x7632u : 0x5410u;
+            Eight<T> e;
+            *reinterpret_cast<uint4 *>(&e) = make_uint4(__byte_perm(a.x, a.y, sel), __byte_perm(a.z, a.w, sel), __byte_perm(b.x, b.y, sel), __byte_perm(b.z, b.w, sel));
+            if (row0 + 2 * i + h < P.rows) store_result<T>(P, row0 + 2 * i + h, col0 + n8, e);
+        }
+    }
+    __syncwarp();
+}
+
+template <class T, bool TRANS, bool SPLIT>
+__global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_constant__ ProjectionParams P)
+{
+    extern __shared__ char pj_raw[];
+    __shared__ u64 bars[2 * PP_STAGES + 4 + 4];
+    __shared__ u32 s_tmem;
+    __shared__ int s_fail;
+    char *ring = pj_raw + ((PJ_PAD - (smem_u32(pj_raw) & (PJ_PAD - 1))) & (PJ_PAD - 1));
+    char *scales = ring + P.ring, *turn_room = scales + PJ_SLOTS * PP_SCALES;
+    const u32 ring_u = smem_u32(ring), scales_u = smem_u32(scales);
+    const u32 full = smem_u32(bars), empty = full + 8 * PP_STAGES, sc_full = empty + 8 * PP_STAGES, sc_empty = sc_full + 16,
+              acc_full = sc_empty + 16, acc_empty = acc_full + 16;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    const u32 rank = cluster.block_rank(), side = rank & 1, leader = rank & ~1u, both = 3u << leader;
+    const int parts = SPLIT ? (int)cluster.num_blocks() / 2 : 1, part = SPLIT ? (int)rank / 2 : 0;
+    const u32 tiles = (u32)P.tiles, first = SPLIT ? blockIdx.x / (2 * parts) : blockIdx.x / 2, stride = SPLIT ? tiles : gridDim.x / 2;
+    const int quads = (P.groups + PJ_QUAD - 1) / PJ_QUAD, q0 = (int)((long long)quads * part / parts), q1 = (int)((long long)quads * (part + 1) / parts);
+    const int g0 = q0 * PJ_QUAD, g1 = min(q1 * PJ_QUAD, P.groups);
+    const int half = P.tile / 2, stage_bytes = PJ_A + half * GROUP;
+
+    if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&P.w) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&P.x) : "memory");
+        for (int s = 0; s < PP_STAGES; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(sc_full + 8 * s, 2);
+            mbar_init(sc_empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(acc_full + 8 * s, 1);
+            mbar_init(acc_empty + 8 * s, 8);
+        }
+        s_fail = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&s_tmem)), "r"(PP_COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster.sync();                     // (the barriers of both CTAs are there)
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const u32 tmem = s_tmem;
+    pdl_wait();
+    pdl_launch_dependents();
+
+    if (warp == 0) {                    // ---- copies, in both CTAs; counted at the leader's barriers
+        if (elect_one()) {
+            const u32 full_at = peer_address(full, leader);
+            int stage = 0, issued = 0;
+            u32 turn = 0;
+            bool fine = true;
+            for (u32 t = first; t < tiles && fine; t += stride) {
+                const int col = (int)(t % (u32)P.blocks * 2 + side) * PJ_WIDE, row = (int)(t / (u32)P.blocks) * P.tile + (int)side * half;
+                for (int g = g0; g < g1; ++g) {
+                    if (issued >= P.stages) fine = mbar_wait(empty + 8 * stage, turn ^ 1);
+                    if (!fine) break;
+                    ++issued;
+                    const u32 dst = ring_u + (u32)stage * (u32)stage_bytes, bar = full_at + 8 * stage;
+                    if (side == 0) mbar_expect(full + 8 * stage, 2 * (u32)stage_bytes);
+                    if (TRANS) tma_load_pair(dst, &P.w, col, g * GROUP, bar);
+                    else tma_load_pair(dst, &P.w, g * GROUP, col, bar);
+                    tma_load_pair(dst + PJ_A, &P.x, g * GROUP, row, bar);
+                    if (++stage == P.stages) {
+                        stage = 0;
+                        turn ^= 1;
+                    }
+                }
+            }
+            if (!fine) {                // a wait ran out: the results are no numbers, but no copy lands in what comes next
+                s_fail = 1;
+                for (int i = max(0, issued - P.stages); i < issued; ++i)
+                    mbar_wait(side == 0 ? full + 8 * (i % P.stages) : empty + 8 * (i % P.stages), (u32)(i / P.stages) & 1);
+            }
+        }
+    } else if (warp == 1) {             // ---- products, issued by the leader
+        if (side == 0 && elect_one()) {
+            const u32 idesc = umma_idesc(TRANS, 2 * PJ_WIDE, P.tile), sa = tmem + 2 * (u32)P.tile;
+            int stage = 0, quad = 0, done = 0;
+            u32 turn = 0;
+            bool fine = true;
+            for (u32 t = first; t < tiles && fine; t += stride, ++done) {
+                const u32 buf = (u32)done & 1, d = tmem + buf * (u32)P.tile;
+                if (done >= 2) fine = mbar_wait_cluster(acc_empty + 8 * buf, (u32)(done / 2 - 1) & 1);
+                if (!fine) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int q = q0; q < q1 && fine; ++q, ++quad) {
+                    const u32 to = sa + (u32)(quad & 1) * 12, src = scales_u + (u32)(quad % PJ_SLOTS) * PP_SCALES, batch = (u32)quad / PJ_BATCH;
+                    if (quad % PJ_BATCH == 0) {
+                        fine = mbar_wait_cluster(sc_full + 8 * (batch & 1), batch / 2 & 1);
+                        if (!fine) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    }
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) scales_to_tmem_pair(to + 4 * i, umma_desc(src + 512 * i, 128, 0));
+                    for (int g = q * PJ_QUAD; g < min((q + 1) * PJ_QUAD, g1); ++g) {
+                        fine = mbar_wait_cluster(full + 8 * stage, turn);
+                        if (!fine) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const u32 at = ring_u + (u32)stage * (u32)stage_bytes;
+                        const u64 a = umma_desc(at, 1024, 2), b = umma_desc(at + PJ_A, 1024, 2);
+                        const u32 id = umma_idesc_at(idesc, (u32)(g % PJ_QUAD));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            umma_scaled_pair(d, a + (TRANS ? k * (32 * GROUP / 16) : k * 2), b + k * 2, id, to, to + 4, g > g0 || k > 0);
+                        umma_commit_pair(empty + 8 * stage, both);
+                        if (++stage == P.stages) {
+                            stage = 0;
+                            turn ^= 1;
+                        }
+                    }
+                    if (fine && quad % PJ_BATCH == PJ_BATCH - 1) umma_commit_pair(sc_empty + 8 * (batch & 1), both);
+                }
+                if (fine) umma_commit_pair(acc_full + 8 * buf, both);
+            }
+            if (!fine) s_fail = 1;
+        }
+    } else if (warp < 4) {              // ---- scales: each CTA's weights, and all rows'
+        const int turns = warp - 2;
+        const u32 full_at = peer_address(sc_full + 8 * turns, leader);
+        QuadScales<7> next[PJ_BATCH];
+        u32 t = first;                  // the quad that is fetched next
+        int q = q0;
+        auto skip = [&]() {
+            if (++q == q1) {
+                q = q0;
+                t = tiles - t > stride ? t + stride : tiles;
+            }
+        };
+        auto fetch = [&]() {
+#pragma unroll
+            for (int j = 0; j < PJ_BATCH; ++j)
+                if (t < tiles) {
+                    next[j].fetch(P, q, (long long)(t % (u32)P.blocks * 2 + side), (long long)(t / (u32)P.blocks) * P.tile + lane);
+                    skip();
+                }
+        };
+        auto pass = [&]() {             // (the other warp's)
+            for (int j = 0; j < PJ_BATCH; ++j)
+                if (t < tiles) skip();
+        };
+        const long long all = first < tiles ? (long long)((tiles - first + stride - 1) / stride) * (q1 - q0) : 0;
+        if (turns) pass();
+        fetch();
+        u32 phase = 0;
+        for (long long i = turns * PJ_BATCH; i < all; i += PJ_SLOTS, phase ^= 1) {
+            if (i >= PJ_SLOTS && !mbar_wait(sc_empty + 8 * turns, phase ^ 1)) {
+                s_fail = 1;
+                break;
+            }
+#pragma unroll
+            for (int j = 0; j < PJ_BATCH; ++j)
+                if (i + j < all) next[j].store(scales + (turns * PJ_BATCH + j) * PP_SCALES, lane);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(full_at);
+            pass();
+            fetch();
+        }
+    } else if (warp >= 4) {             // ---- results
+        const u32 empty_at = peer_address(acc_empty, leader);
+        const int w = warp - 4;
+        u32 *turn = reinterpret_cast<u32 *>(turn_room + w * 2048);
+        bool fine = true;
+        int done = 0;
+        for (u32 t = first; t < tiles; t += stride, ++done) {
+            const u32 buf = (u32)done & 1;
+            fine = fine && mbar_wait(acc_full + 8 * buf, (u32)(done / 2) & 1);
+            __syncwarp();
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const u32 at = tmem + ((u32)w << 21) + buf * (u32)P.tile;
+            const long long row0 = (long long)(t / (u32)P.blocks) * P.tile;
+            const int col0 = (int)(t % (u32)P.blocks * 2 + side) * PJ_WIDE + w * 32;
+#pragma unroll 1
+            for (int c = 0; c < P.tile; c += 32) {
+                float v[32];
+                tmem_ld(at + (u32)c, v);
+                tmem_ld_wait(v);
+                if (c + 32 >= P.tile) {                 // the sums are in registers: the accumulator is free
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_at(empty_at + 8 * buf);
+                }
+                if (!fine) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FFFFFFFu);
+                }
+                if constexpr (SPLIT) {
+                    float *sums = reinterpret_cast<float *>(ring);          // [row][128 output columns]
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sums[(c + i) * PJ_WIDE + w * 32 + lane] = v[i];
+                } else {
+                    if (row0 + c < P.rows) write_block<T>(P, v, turn, row0 + c, col0, lane);
+                }
+            }
+        }
+        if (!fine) s_fail = 1;
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster.sync();                     // (both CTAs are through with their tensor memory and each other's barriers)
+    if (warp == 3) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(PP_COLUMNS) : "memory");
+    }
+    if constexpr (SPLIT) {
+        int fail = 0;                   // (of any CTA of the cluster)
+        for (int p = 0; p < 2 * parts; ++p) fail |= *cluster.map_shared_rank(&s_fail, p);
+        add_parts<T, PP_THREADS>(P, cluster, reinterpret_cast<float *>(ring), parts, (int)side, 2, !fail, (long long)(first / (u32)P.blocks) * P.tile,
+                                 P.tile * part / parts, P.tile * (part + 1) / parts, (int)(first % (u32)P.blocks * 2 + side) * PJ_WIDE);
+        cluster.sync();                 // (nobody leaves while its sums are read)
+    }
 }
 
 }  // namespace cs
