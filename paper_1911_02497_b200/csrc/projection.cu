@@ -110,45 +110,61 @@ int resident_clusters(condensa_ctx *ctx, const Variant &v, int n, int &count)
     return CONDENSA_OK;
 }
 
-// The cut that a simple account in cycles makes cheapest. A group of the depth costs a CTA what the tensor core needs (2 per row of
-// the tile) or what its codes need on their way from L2, whichever is more; then there are the rounds of tiles, and something fixed.
+// The cut that a simple account in microseconds makes cheapest; its figures are measured (the start and end of a launch are left out but for
+// what differs). A group of the depth costs a CTA by itself 150 ns and 0.6 for each row of the tile, one of a pair 130 and 1.05, and all
+// their codes pass L2 at 13 MB/us. Codes come from memory at 70 KB/us for an SM and at no more than 4.5 MB/us in so short a time.
+// A row of sums takes a single CTA 26 ns to write, a pair 4 ns; sums over a cluster cost 0.7 us and its barriers, more for wider tiles.
+// Examples (us): 1 row 1500 -> 6000: (single, tile 16, 1 part) 5.4, 3 parts 6.0. 128 rows 4096^2: (single, 32, 1) 10.4, (64, 1) 10.9,
+// (128, 1) 13.2, (128, 4) 13.0, pairs (64, 1) 11.8. 512 rows: pairs (128, 1) 13.6, single (128, 1) 14.1, pairs (96, 1) 17.7.
+// 2048 rows: pairs (160, 1) 30.7, (224, 1) 33.0, single (128, 1) 39.3.
 int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups, int dtype, bool trans, Shape &best)
 {
     const int quads = (groups + PJ_QUAD - 1) / PJ_QUAD;
-    const double L2 = 56.0;             // bytes a cycle for an SM
+    const double sms = ctx->num_sms, codes = (double)groups * GROUP * (double)(width + rows);
     double least = 0.0;
-    auto offer = [&](const Shape &s, double t) {
-        if (least == 0.0 || t < 0.999 * least) {
+    auto offer = [&](const Shape &s, long long ctas, double rounds, double group, double bytes, double more) {
+        const double depth = (double)((quads + s.parts - 1) / s.parts * PJ_QUAD), busy = std::min((double)ctas, sms);
+        const double t = std::max(rounds * depth * std::max(group, bytes * busy / 13e6), codes / std::min(4.5e6, 70e3 * busy)) + more;
+        if (least == 0.0 || t < 0.99 * least) {
             least = t;
             best = s;
         }
     };
-    {   // single CTAs: equal tiles of up to 128 rows
-        const long long n = (rows + PJ_MAX_TILE - 1) / PJ_MAX_TILE;
-        const int tile = (int)(((rows + n - 1) / n + 15) / 16 * 16);
-        const long long tiles = n * ((width + PJ_WIDE - 1) / PJ_WIDE);
-        const double group = std::max(2.0 * tile, (PJ_A + 128.0 * tile) / L2);
+    const auto cut = [&](long long n, int step) { return (int)(((rows + n - 1) / n + step - 1) / step * step); };      // rows of n equal tiles
+    int before = 0;
+    for (long long n = (rows + PJ_MAX_TILE - 1) / PJ_MAX_TILE; n <= (rows + 15) / 16 && n <= 64; ++n) {
+        const int tile = cut(n, 16);
+        if (tile == before) continue;
+        before = tile;
+        const long long tiles = (rows + tile - 1) / tile * ((width + PJ_WIDE - 1) / PJ_WIDE);
         for (int parts = 1; parts <= std::min(PJ_MAX_PARTS, quads); ++parts) {
+            const Shape s = {false, tile, parts, tiles * parts};
             const long long ctas = tiles * parts;
-            if (parts > 1 && ctas > ctx->num_sms) break;
-            const double depth = (double)((quads + parts - 1) / parts * PJ_QUAD), rounds = (double)((ctas + ctx->num_sms - 1) / ctx->num_sms);
-            offer({false, tile, parts, ctas}, rounds * (depth * group + 800.0) + 1500.0 + (parts > 1 ? 600.0 : 0.0));
+            double rounds = (double)((ctas + ctx->num_sms - 1) / ctx->num_sms);
+            if (parts > 1) {
+                int fit = 0;
+                const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), parts, fit);
+                if (rc) return rc;
+                if (tiles > fit) break;
+            }
+            offer(s, ctas, rounds, 0.15 + 0.0006 * tile, PJ_A + (double)GROUP * tile, 0.026 * tile * rounds + (parts > 1 ? 0.7 + 0.3 * parts + 0.006 * tile : 0.0));
         }
     }
-    if (rows > 64) {
-        for (int tile = 64; tile <= PP_TILE; tile += 32) {
-            const long long tiles = (rows + tile - 1) / tile * ((width + 2 * PJ_WIDE - 1) / (2 * PJ_WIDE));
-            const double group = std::max(2.0 * tile, (PJ_A + 64.0 * tile) / L2);
-            for (int parts = 1; parts <= std::min(PP_MAX_PARTS, quads); ++parts) {
-                Shape s = {true, tile, parts, tiles * parts};
-                int fit = 0;
-                const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), 2 * parts, fit);
-                if (rc) return rc;
-                if (parts > 1 && tiles > fit) break;
-                if (parts == 1) s.clusters = std::min(tiles, (long long)fit);
-                const double depth = (double)((quads + parts - 1) / parts * PJ_QUAD), rounds = (double)((tiles + fit - 1) / fit);
-                offer(s, rounds * (depth * group + 300.0) + 3500.0 + (parts > 1 ? 2000.0 : 0.0));
-            }
+    before = 0;
+    for (long long n = (rows + PP_TILE - 1) / PP_TILE; rows > 64 && n <= (rows + 63) / 64 && (before == 0 || before > 64); ++n) {
+        const int tile = cut(n, 32);
+        if (tile == before) continue;
+        before = tile;
+        const long long tiles = (rows + tile - 1) / tile * ((width + 2 * PJ_WIDE - 1) / (2 * PJ_WIDE));
+        for (int parts = 1; parts <= std::min(PP_MAX_PARTS, quads); ++parts) {
+            Shape s = {true, tile, parts, tiles * parts};
+            int fit = 0;
+            const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), 2 * parts, fit);
+            if (rc) return rc;
+            if (parts > 1 && tiles > fit) break;
+            if (parts == 1) s.clusters = std::min(tiles, (long long)fit);
+            const double rounds = (double)((tiles + fit - 1) / fit);
+            offer(s, 2 * s.clusters, rounds, 0.13 + 0.00105 * tile, PJ_A + 0.5 * GROUP * tile, 1.5 + 0.004 * tile * rounds + (parts > 1 ? 2.0 + 0.01 * tile + 0.5 * parts : 0.0));
         }
     }
     return CONDENSA_OK;

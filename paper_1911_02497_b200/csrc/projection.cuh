@@ -370,14 +370,15 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
 // Two CTAs of a cluster form one product of 256 output columns (tcgen05 cta_group::2): each brings its own 128 columns of
 // weights and half of the rows, and keeps its 128 columns' sums; per byte that an SM takes from L2 this is up to 1.7 times the work
 // of a CTA by itself. The first CTA of the pair issues the products. Persistent: two accumulators in tensor memory take
-// turns, so that four warps write out a tile while the next one is multiplied. SPLIT: the pairs of a cluster share one
+// turns, so that a tile is written out while the next one is multiplied. SPLIT: the pairs of a cluster share one
 // tile's depth instead, as in the kernel above.
-constexpr int PP_THREADS = 256;
+constexpr int PP_OUT_WARPS = 8;         // warps that write results: two for each 32 lanes of tensor memory, in turn
+constexpr int PP_THREADS = 128 + 32 * PP_OUT_WARPS;
 constexpr int PP_TILE = 224;            // most rows of a tile: two accumulators and the scales fill tensor memory
 constexpr int PP_STAGES = 8;
 constexpr int PP_SCALES = 1536;         // bytes of a quad's scales: weights, rows
 constexpr int PP_COLUMNS = 512;
-constexpr int PP_OUT = 4 * 2048;        // where the four warps turn their sums around
+constexpr int PP_OUT = PP_OUT_WARPS * 2048;     // where they turn their sums around
 
 __device__ __forceinline__ u32 peer_address(u32 addr, u32 rank)
 {
@@ -431,26 +432,26 @@ __device__ __forceinline__ u32 pack2(float lo, float hi, __half) { const __half2
 __device__ __forceinline__ u32 pack2(float lo, float hi, __nv_bfloat16) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const u32 *>(&h); }
 
 // Sums of 32 rows x 32 output columns, a column per lane, into the result: neighbouring rows go as pairs through the
-// warp's 2 KB of shared memory and come back as eight neighbouring columns of a row.
-template <class T>
-__device__ __forceinline__ void write_block(const ProjectionParams &P, const float (&v)[32], u32 *turn, long long row0, int col0, int lane)
+// warp's 2 KB of shared memory and come back as eight neighbouring columns of a row. `out`: row 0, column 0; `rows` of them are wanted.
+template <int A, class T>
+__device__ __forceinline__ void write_block(const float (&v)[32], u32 *turn, T *out, long long ldo, int rows, int col0, int width, int lane)
 {
 #pragma unroll
     for (int i = 0; i < 16; ++i) turn[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
     __syncwarp();
+    const int i0 = lane / 4, n8 = lane % 4 * 8, first = (i0 & 1) * 4;      // (odd pairs read their halves the other way round: no bank conflicts)
+    T *row = out + (long long)(2 * i0) * ldo;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int i = r * 8 + lane / 4, n8 = lane % 4 * 8, first = (i & 1) * 4;      // (odd pairs read their halves the other way round: no bank conflicts)
-        uint4 w[2];
-        w[0] = *reinterpret_cast<const uint4 *>(turn + i * 32 + n8 + first);
-        w[1] = *reinterpret_cast<const uint4 *>(turn + i * 32 + n8 + (4 - first));
-        const uint4 a = first ? w[1] : w[0], b = first ? w[0] : w[1];
+    for (int r = 0; r < 2; ++r, row += 16 * ldo) {
+        const u32 *at = turn + (r * 8 + i0) * 32 + n8;
+        const uint4 x = *reinterpret_cast<const uint4 *>(at + first), y = *reinterpret_cast<const uint4 *>(at + (4 - first));
+        const uint4 a = first ? y : x, b = first ? x : y;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const u32 sel = h ? 0x7632u : 0x5410u;
             Eight<T> e;
             *reinterpret_cast<uint4 *>(&e) = make_uint4(__byte_perm(a.x, a.y, sel), __byte_perm(a.z, a.w, sel), __byte_perm(b.x, b.y, sel), __byte_perm(b.z, b.w, sel));
-            if (row0 + 2 * i + h < P.rows) store_result<T>(P, row0 + 2 * i + h, col0 + n8, e);
+            if (16 * r + 2 * i0 + h < rows) store8<A>(row + h * ldo, col0 + n8, width, e);
         }
     }
     __syncwarp();
@@ -491,7 +492,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(acc_full + 8 * s, 1);
-            mbar_init(acc_empty + 8 * s, 8);
+            mbar_init(acc_empty + 8 * s, 2 * PP_OUT_WARPS);
         }
         s_fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -623,8 +624,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
         }
     } else if (warp >= 4) {             // ---- results
         const u32 empty_at = peer_address(acc_empty, leader);
-        const int w = warp - 4;
-        u32 *turn = reinterpret_cast<u32 *>(turn_room + w * 2048);
+        const int w = warp & 3, turns = (warp - 4) / 4;
+        u32 *turn = reinterpret_cast<u32 *>(turn_room + (warp - 4) * 2048);
         bool fine = true;
         int done = 0;
         for (u32 t = first; t < tiles; t += stride, ++done) {
@@ -635,16 +636,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
             const u32 at = tmem + ((u32)w << 21) + buf * (u32)P.tile;
             const long long row0 = (long long)(t / (u32)P.blocks) * P.tile;
             const int col0 = (int)(t % (u32)P.blocks * 2 + side) * PJ_WIDE + w * 32;
+            const int rows = (int)min(P.rows - row0, (long long)P.tile);
 #pragma unroll 1
-            for (int c = 0; c < P.tile; c += 32) {
+            for (int c = turns * 32; c < P.tile; c += PP_OUT_WARPS / 4 * 32) {
                 float v[32];
                 tmem_ld(at + (u32)c, v);
                 tmem_ld_wait(v);
-                if (c + 32 >= P.tile) {                 // the sums are in registers: the accumulator is free
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_at(empty_at + 8 * buf);
-                }
                 if (!fine) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(0x7FFFFFFFu);
@@ -653,10 +650,16 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
                     float *sums = reinterpret_cast<float *>(ring);          // [row][128 output columns]
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sums[(c + i) * PJ_WIDE + w * 32 + lane] = v[i];
-                } else {
-                    if (row0 + c < P.rows) write_block<T>(P, v, turn, row0 + c, col0, lane);
+                } else if (c < rows) {
+                    T *out = (T *)P.out + (row0 + c) * P.ldo;
+                    if (P.access == 8) write_block<8>(v, turn, out, P.ldo, rows - c, col0, P.width, lane);
+                    else if (P.access == 4) write_block<4>(v, turn, out, P.ldo, rows - c, col0, P.width, lane);
+                    else write_block<1>(v, turn, out, P.ldo, rows - c, col0, P.width, lane);
                 }
             }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(empty_at + 8 * buf);          // (its sums are in registers or written)
         }
         if (!fine) s_fail = 1;
     }
