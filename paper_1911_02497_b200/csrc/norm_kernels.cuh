@@ -6,17 +6,18 @@ using namespace cs;
 
 namespace {
 
-// CTAs of a kernel that an SM holds.
-int resident_ctas(condensa_ctx *ctx, const void *f, int block, int &count)
+// CTAs of a kernel that an SM holds; allows it its shared memory.
+int resident_ctas(condensa_ctx *ctx, const void *f, int block, int smem, int &count)
 {
     for (const condensa_ctx::ClusterFit &k : ctx->cluster_fit)
         if (k.f == f && k.size == 0) {
             count = k.count;
             return CONDENSA_OK;
         }
+    if (smem > 48 * 1024) CU_TRY(ctx, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     count = 0;
-    CU_TRY(ctx, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&count, f, block, 0));
-    if (count < 1) count = 1;
+    CU_TRY(ctx, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&count, f, block, (size_t)smem));
+    if (count < 1) return fail(ctx, CONDENSA_ERR_INTERNAL, "a kernel of the norm does not fit an SM");
     ctx->cluster_fit.push_back({f, 0, count});
     return CONDENSA_OK;
 }
@@ -56,9 +57,10 @@ int backward_as(condensa_ctx *ctx, const NormBackParams &P, NormBackPlan &plan, 
 {
     constexpr int ROWS = RowThreads<TPR>::ROWS, BLOCK = RowThreads<TPR>::BLOCK;
     auto k = k_norm_backward<T, A, TPR, NV>;
-    if (run) return op_launch(ctx, "k_norm_backward", k, dim3((unsigned)plan.grid), BLOCK, stream, P);
+    constexpr int SMEM = BackRing<T, A, TPR, NV>::SMEM;
+    if (run) return op_launch_smem(ctx, "k_norm_backward", k, dim3((unsigned)plan.grid), BLOCK, SMEM, stream, P);
     int fit = 1;
-    const int rc = resident_ctas(ctx, (const void *)k, BLOCK, fit);
+    const int rc = resident_ctas(ctx, (const void *)k, BLOCK, SMEM, fit);
     if (rc) return rc;
     plan.grid = stream_grid(ctx, (P.rows + ROWS - 1) / ROWS, fit);
     plan.slots = plan.grid * ROWS;
@@ -69,7 +71,7 @@ template <class T, int A>
 int backward_of(condensa_ctx *ctx, const NormBackParams &P, NormBackPlan &plan, bool run, cudaStream_t stream)
 {
     const int eights = (P.cols + 7) / 8;
-    // a thread of 1024 has 64 registers, too few for fp32 operands
+    // (fp32 operands of longer rows leave no room for two stages)
     if (eights > (sizeof(T) == 4 ? 1024 : 2048)) {
         const unsigned strips = (unsigned)((eights + THREADS - 1) / THREADS);
         if (!run) {

@@ -60,13 +60,18 @@ inline int op_access(const void *p, long long ld, int e, long long cols)
 // A launch that may start while the kernel ahead of it ends: every kernel launched so waits for that one before it reads or
 // writes anything.
 template <class... A>
-inline int op_launch(condensa_ctx *ctx, const char *name, void (*k)(A...), dim3 grid, int block, cudaStream_t stream, A... args)
+inline int op_launch_smem(condensa_ctx *ctx, const char *name, void (*k)(A...), dim3 grid, int block, size_t smem, cudaStream_t stream, A... args)
 {
-    PdlLaunch l(ctx, 1, block, 0, stream);
+    PdlLaunch l(ctx, 1, block, smem, stream);
     l.cfg.gridDim = grid;
     const int pa_ = prof_begin(ctx, name, stream);
     CU_TRY(ctx, cudaLaunchKernelEx(&l.cfg, k, args...));
     ctx->launches += 1;
     prof_end(ctx, pa_, stream);
     return CONDENSA_OK;
+}
+template <class... A>
+inline int op_launch(condensa_ctx *ctx, const char *name, void (*k)(A...), dim3 grid, int block, cudaStream_t stream, A... args)
+{
+    return op_launch_smem(ctx, name, k, grid, block, 0, stream, args...);
 }
