@@ -40,9 +40,39 @@ template <> struct Access<float> { typedef uint4 Four; };
 template <> struct Access<__half> { typedef uint2 Four; };
 template <> struct Access<__nv_bfloat16> { typedef uint2 Four; };
 
+// Moves words so that they begin `by` values further on. `by` is the same for all threads of a row, so nothing here diverges.
+__device__ __forceinline__ void shift_words(u32 (&w)[8], int by)           // 16-bit values: by 0 .. 7
+{
+    if (by & 4) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (by & 2) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    if (by & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+}
+__device__ __forceinline__ void shift_words(u32 (&w)[12], int by)          // 32-bit values: by 0 .. 3
+{
+    if (by & 2) {
+#pragma unroll
+        for (int i = 0; i < 10; ++i) w[i] = w[i + 2];
+    }
+    if (by & 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = w[i + 1];
+    }
+}
+
 // Columns c .. c+7 of a row of `cols`; zero past the end. A says what the rows allow: 8 or 4 values at a time (alignment, and a
 // number of columns that is a multiple of it), or one. It is fixed when compiling: a choice at every access made three to
 // four times as many instructions, and kept the loads of a thread from leaving together (128 x 128 blocks of bf16: 87 us).
+// Rows that begin anywhere (A = 1) are read by the aligned 16 bytes that hold the values, where those lie within the row, and
+// shifted; value by value the norm of 8000 x 2047 in bf16 took 79 us, not 22 as of 8000 x 2048.
 template <int A, class T>
 __device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
 {
@@ -59,8 +89,21 @@ __device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
 #pragma unroll
         for (int i = 0; i < 2; ++i) d[i] = c + 4 * i < cols ? s[i] : Four{};
     } else {
+        constexpr int V = 16 / (int)sizeof(T), N = (int)sizeof(e) / 16 + 1;        // values of 16 bytes; such pieces that hold the eight
+        const int by = (int)(reinterpret_cast<uintptr_t>(row + c) % 16 / sizeof(T)), c0 = c - by;
+        if (c0 >= 0 && c0 + (by ? N : N - 1) * V <= cols) {
+            alignas(16) u32 w[4 * N];
+            const uint4 *s = reinterpret_cast<const uint4 *>(row + c0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e.v[i] = c + i < cols ? row[c + i] : from_f32<T>(0.0f);
+            for (int i = 0; i < N; ++i) *reinterpret_cast<uint4 *>(w + 4 * i) = i < N - 1 || by ? s[i] : make_uint4(0, 0, 0, 0);
+            shift_words(w, by);
+            u32 *d = reinterpret_cast<u32 *>(&e);
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(e) / 4; ++i) d[i] = w[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e.v[i] = c + i < cols ? row[c + i] : from_f32<T>(0.0f);
+        }
     }
     return e;
 }
@@ -88,6 +131,29 @@ __device__ __forceinline__ void store8(T *row, int c, int cols, const Eight<T> &
             if (c + i < cols) row[c + i] = e.v[i];
     }
 }
+
+// The same by a whole warp whose lanes hold eights that follow one another in a row. Where rows begin anywhere, the values go through
+// the warp's `turn` (32 eights) and out 32 neighbours at a time, not with 16 bytes between the lanes of an access.
+template <int A, class T>
+__device__ __forceinline__ void store8_warp(T *row, int c, int cols, const Eight<T> &e, Eight<T> *turn)
+{
+    if constexpr (A != 1) {
+        store8<A>(row, c, cols, e);
+    } else {
+        const int lane = threadIdx.x & 31, first = c - lane * 8;
+        __syncwarp();
+        turn[lane] = e;
+        __syncwarp();
+        const T *s = reinterpret_cast<const T *>(turn);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (first + i * 32 + lane < cols) row[first + i * 32 + lane] = s[i * 32 + lane];
+    }
+}
+// Room for the turns of a CTA's warps.
+template <int A, class T, int BLOCK> struct Turns {
+    static constexpr int N = A == 1 ? BLOCK : 1;
+};
 
 // The scale of a group by its largest magnitude 1.m * 2^e: the quotient is at most 448 = 1.75 * 2^8.
 __device__ __forceinline__ u32 scale_of(float most)

@@ -89,7 +89,7 @@ __device__ __forceinline__ Eight<T> load_h(const NormParams &P, long long row, i
 
 // What follows from eight values of h.
 template <class T, int A>
-__device__ __forceinline__ void norm_out(const NormParams &P, long long row, int c, const Eight<T> &h, float rstd)
+__device__ __forceinline__ void norm_out(const NormParams &P, long long row, int c, const Eight<T> &h, float rstd, Eight<T> *turn)
 {
     float g[8], y[8];
     load_gain<T, A>(P.gain, P.gain_f32, c, P.cols, g);
@@ -99,7 +99,7 @@ __device__ __forceinline__ void norm_out(const NormParams &P, long long row, int
         Eight<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o.v[i] = from_f32<T>(y[i]);
-        store8<A>((T *)P.y + row * P.ldy, c, P.cols, o);
+        store8_warp<A>((T *)P.y + row * P.ldy, c, P.cols, o, turn);
     }
     if (P.codes) {
         if (c + 8 > P.cols) {
@@ -119,6 +119,8 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
 {
     __shared__ float slots[32];
     __shared__ double wide[32];
+    __shared__ Eight<T> s_turns[Turns<A, T, RowThreads<TPR>::BLOCK>::N];
+    Eight<T> *turn = s_turns + (A == 1 ? threadIdx.x / 32 * 32 : 0);
     pdl_wait();
     pdl_launch_dependents();
     const long long row = (long long)blockIdx.x * RowThreads<TPR>::ROWS + threadIdx.x / TPR;
@@ -130,7 +132,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
     for (int v = 0; v < NV; ++v) h[v] = load_h<T, A>(P, row, (v * TPR + t) * 8);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        if (P.h) store8<A>((T *)P.h + row * P.ldh, (v * TPR + t) * 8, P.cols, h[v]);
+        if (P.h) store8_warp<A>((T *)P.h + row * P.ldh, (v * TPR + t) * 8, P.cols, h[v], turn);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fmaf(h[v][i], h[v][i], sum);
     }
@@ -149,7 +151,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         hold(h[v]);
-        norm_out<T, A>(P, row, (v * TPR + t) * 8, h[v], rstd);
+        norm_out<T, A>(P, row, (v * TPR + t) * 8, h[v], rstd, turn);
     }
 }
 
@@ -158,13 +160,16 @@ template <class T, int A, int TPR>
 __global__ void __launch_bounds__(TPR) k_norm_forward_long(const __grid_constant__ NormParams P)
 {
     __shared__ double slots[32];
+    __shared__ Eight<T> s_turns[Turns<A, T, TPR>::N];
+    Eight<T> *turn = s_turns + (A == 1 ? threadIdx.x / 32 * 32 : 0);
     pdl_wait();
     pdl_launch_dependents();
     const long long row = blockIdx.x;
     double sum = 0.0;
-    for (int c = threadIdx.x * 8; c < P.cols; c += TPR * 8) {
+    for (int c0 = 0; c0 < P.cols; c0 += TPR * 8) {                  // (all lanes stay for the shuffles)
+        const int c = c0 + threadIdx.x * 8;
         const Eight<T> h = load_h<T, A>(P, row, c);
-        if (P.h) store8<A>((T *)P.h + row * P.ldh, c, P.cols, h);
+        if (P.h) store8_warp<A>((T *)P.h + row * P.ldh, c, P.cols, h, turn);
         double part = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) part += (double)h[i] * h[i];
@@ -173,11 +178,11 @@ __global__ void __launch_bounds__(TPR) k_norm_forward_long(const __grid_constant
     const float rstd = rstd_of(row_sum<TPR>(sum, slots), P.cols, P.eps);
     if (threadIdx.x == 0 && P.rstd) P.rstd[row] = rstd;
     if (!P.y && !P.codes) return;
-    for (int c0 = 0; c0 < P.cols; c0 += TPR * 8) {            // (all lanes stay for the shuffles)
+    for (int c0 = 0; c0 < P.cols; c0 += TPR * 8) {
         const int c = c0 + threadIdx.x * 8;
         // what this thread wrote to h, or x and the residual again where there is no h
         const Eight<T> h = P.h ? load8<A>((const T *)P.h + row * P.ldh, c, P.cols) : load_h<T, A>(P, row, c);
-        norm_out<T, A>(P, row, c, h, rstd);
+        norm_out<T, A>(P, row, c, h, rstd, turn);
     }
 }
 
@@ -185,7 +190,7 @@ __global__ void __launch_bounds__(TPR) k_norm_forward_long(const __grid_constant
 // dx of columns c .. c+7; q: the mean that is taken out.
 template <class T, int A>
 __device__ __forceinline__ void norm_back_out(const NormBackParams &P, long long row, int c, const Eight<T> &dy, const Eight<T> &h,
-                                              const Eight<T> &dh, const float (&g)[8], float rstd, float q)
+                                              const Eight<T> &dh, const float (&g)[8], float rstd, float q, Eight<T> *turn)
 {
     float d[8];
 #pragma unroll
@@ -197,7 +202,7 @@ __device__ __forceinline__ void norm_back_out(const NormBackParams &P, long long
         Eight<T> o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o.v[i] = from_f32<T>(d[i]);
-        store8<A>((T *)P.dx + row * P.ldx, c, P.cols, o);
+        store8_warp<A>((T *)P.dx + row * P.ldx, c, P.cols, o, turn);
     }
     if (P.codes) {
         if (c + 8 > P.cols) {
@@ -217,7 +222,7 @@ template <class T, int A, int TPR, int NV> struct BackRing {
     static constexpr int ROW = 3 * NV * BLOCK * EIGHT;                 // bytes of a stage: dy, h, dh
     static constexpr int STAGES = A == 1 ? 0 : 3 * ROW <= 75 * 1024 ? 3 : 2;
     static constexpr int SMEM = STAGES * ROW;
-    static constexpr int FIT = SMEM ? 226 * 1024 / (SMEM + 1024) : 8, WANT = 768 / BLOCK > 0 ? 768 / BLOCK : 1;
+    static constexpr int FIT = SMEM ? 226 * 1024 / (SMEM + 1024) : 8, THREADS_SM = A == 1 ? 512 : 768, WANT = THREADS_SM / BLOCK > 0 ? THREADS_SM / BLOCK : 1;
     static constexpr int CTAS = FIT < WANT ? FIT : WANT;               // of an SM
     static_assert(SMEM <= 226 * 1024 && CTAS >= 1, "shared memory");
 };
@@ -249,6 +254,8 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
     constexpr int ROWS = RowThreads<TPR>::ROWS, BLOCK = R::BLOCK, S = R::STAGES;
     extern __shared__ __align__(16) char nb_ring[];
     __shared__ float slots[2][32];
+    __shared__ Eight<T> s_turns[Turns<A, T, BLOCK>::N];
+    Eight<T> *turn = s_turns + (A == 1 ? threadIdx.x / 32 * 32 : 0);
     pdl_wait();
     pdl_launch_dependents();
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -280,8 +287,8 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
         rstd_next = rstd_at(first);
         if (S == 3) rstd_last = rstd_at(first + step);
     }
-    int turn = 0, stage = 0;
-    for (long long row = first; row < P.rows; row += step, turn ^= 1) {
+    int phase = 0, stage = 0;
+    for (long long row = first; row < P.rows; row += step, phase ^= 1) {
         Eight<T> e[A == 1 ? NV : 1][3];
         auto take = [&](int o, int v) {
             if constexpr (S > 0) return *reinterpret_cast<const Eight<T> *>(place(stage, o, v));
@@ -316,7 +323,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
             }
         }
         if (P.dx || P.codes) {                          // (the same for all)
-            const float q = row_sum<TPR>(sum, slots[turn]) / (float)P.cols;
+            const float q = row_sum<TPR>(sum, slots[phase]) / (float)P.cols;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 if (!KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
@@ -324,7 +331,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
                 if (P.dh) dh = take(2, v);
                 hold(dy);
                 hold(h);
-                norm_back_out<T, A>(P, row, (v * TPR + t) * 8, dy, h, dh, g[v], rstd, q);
+                norm_back_out<T, A>(P, row, (v * TPR + t) * 8, dy, h, dh, g[v], rstd, q, turn);
             }
         }
         if (S > 0) stage = stage + 1 == S ? 0 : stage + 1;
@@ -345,6 +352,8 @@ template <class T, int A, int TPR>
 __global__ void __launch_bounds__(TPR) k_norm_backward_long(const __grid_constant__ NormBackParams P)
 {
     __shared__ float slots[32];
+    __shared__ Eight<T> s_turns[Turns<A, T, TPR>::N];
+    Eight<T> *turn = s_turns + (A == 1 ? threadIdx.x / 32 * 32 : 0);
     pdl_wait();
     pdl_launch_dependents();
     const long long row = blockIdx.x;
@@ -366,7 +375,7 @@ __global__ void __launch_bounds__(TPR) k_norm_backward_long(const __grid_constan
         Eight<T> dh;
         if (P.dh) dh = load8<A>((const T *)P.dh + row * P.ldd, c, P.cols);
         load_gain<T, A>(P.gain, P.gain_f32, c, P.cols, g);
-        norm_back_out<T, A>(P, row, c, dy, h, dh, g, rstd, q);
+        norm_back_out<T, A>(P, row, c, dy, h, dh, g, rstd, q, turn);
     }
 }
 
@@ -501,6 +510,7 @@ __global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_consta
 {
     constexpr int STEP = ENC_BLOCK / GROUP_LANES, N = GROUP / STEP, W = ENC_BLOCK / 32;
     __shared__ float s_most[2][W];
+    __shared__ Eight<float> s_turns[Turns<A, float, ENC_BLOCK>::N];
     pdl_wait();
     pdl_launch_dependents();
     const u32 bi = blockIdx.x / P.groups, bj = blockIdx.x - bi * P.groups;
@@ -540,27 +550,41 @@ __global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_consta
     const u32 s = scale_of(most);
     const float inverse = scale_inverse(s), scale = scale_value(s);
     if (threadIdx.x == 0) P.scales[bi * P.lds + bj] = (u8)s;
+    const int lane = threadIdx.x % GROUP_LANES;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const long long r = r0 + i * STEP;
-        if (r >= P.rows || c >= P.cols) continue;
+        if (A != 1 && (r >= P.rows || c >= P.cols)) continue;
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = e[i][j];
         if (odd) odd_to_nan(v);
         const uint2 q = codes_of(v, inverse);
-        store_codes<A>(P.codes + r * P.ldc, c, P.cols, q);
-        if (P.theta) {
-            Eight<float> o;
+        const bool there = A != 1 || (r < P.rows && c < P.cols);
+        if (there) store_codes<A>(P.codes + r * P.ldc, c, P.cols, q);
+        if (!P.theta) continue;
+        Eight<float> o;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u32 h2;
-                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((u16)((j < 2 ? q.x : q.y) >> (16 * (j & 1)))));
-                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
-                o.v[2 * j] = f.x * scale;
-                o.v[2 * j + 1] = f.y * scale;
+        for (int j = 0; j < 4; ++j) {
+            u32 h2;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((u16)((j < 2 ? q.x : q.y) >> (16 * (j & 1)))));
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+            o.v[2 * j] = f.x * scale;
+            o.v[2 * j + 1] = f.y * scale;
+        }
+        float *row = P.theta + r * P.ld_theta;
+        if constexpr (A != 1) {
+            if (there) store8<A>(row, c, P.cols, o);
+        } else {                        // through shared memory and out 16 neighbours at a time (whole warps are here)
+            float *turn = reinterpret_cast<float *>(s_turns + threadIdx.x / GROUP_LANES * GROUP_LANES);
+            __syncwarp();
+            reinterpret_cast<Eight<float> *>(turn)[lane] = o;
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = (int)bj * GROUP + j * GROUP_LANES + lane;
+                if (r < P.rows && at < P.cols) row[at] = turn[j * GROUP_LANES + lane];
             }
-            store8<A>(P.theta + r * P.ld_theta, c, P.cols, o);
         }
     }
 }

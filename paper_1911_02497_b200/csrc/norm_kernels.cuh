@@ -31,25 +31,20 @@ int forward_as(condensa_ctx *ctx, const NormParams &P, cudaStream_t stream)
     return op_launch(ctx, "k_norm_forward", k_norm_forward<T, A, TPR, NV>, dim3((unsigned)((P.rows + ROWS - 1) / ROWS)), RowThreads<TPR>::BLOCK, stream, P);
 }
 
-// The threads of a row: as many as hold it with one or two eights each. (Fewer kernels for rows that allow no wide access.)
+// The threads of a row: as many as hold it with one or two eights each.
 template <class T, int A>
 int forward_of(condensa_ctx *ctx, const NormParams &P, cudaStream_t stream)
 {
     const int eights = (P.cols + 7) / 8;
     if (eights > 2048)
         return op_launch(ctx, "k_norm_forward_long", k_norm_forward_long<T, A, LONG_TPR>, dim3((unsigned)P.rows), LONG_TPR, stream, P);
-    if constexpr (A == 1) {
-        return eights <= 64 ? forward_as<T, A, 32, 2>(ctx, P, stream) : eights <= 512 ? forward_as<T, A, 256, 2>(ctx, P, stream)
-                                                                                     : forward_as<T, A, 1024, 2>(ctx, P, stream);
-    } else {
-        return eights <= 32   ? forward_as<T, A, 32, 1>(ctx, P, stream)
-             : eights <= 64   ? forward_as<T, A, 32, 2>(ctx, P, stream)
-             : eights <= 128  ? forward_as<T, A, 128, 1>(ctx, P, stream)
-             : eights <= 256  ? forward_as<T, A, 128, 2>(ctx, P, stream)
-             : eights <= 512  ? forward_as<T, A, 256, 2>(ctx, P, stream)
-             : eights <= 1024 ? forward_as<T, A, 512, 2>(ctx, P, stream)
-                              : forward_as<T, A, 1024, 2>(ctx, P, stream);
-    }
+    return eights <= 32   ? forward_as<T, A, 32, 1>(ctx, P, stream)
+         : eights <= 64   ? forward_as<T, A, 32, 2>(ctx, P, stream)
+         : eights <= 128  ? forward_as<T, A, 128, 1>(ctx, P, stream)
+         : eights <= 256  ? forward_as<T, A, 128, 2>(ctx, P, stream)
+         : eights <= 512  ? forward_as<T, A, 256, 2>(ctx, P, stream)
+         : eights <= 1024 ? forward_as<T, A, 512, 2>(ctx, P, stream)
+                          : forward_as<T, A, 1024, 2>(ctx, P, stream);
 }
 
 template <class T, int A, int TPR, int NV>
@@ -86,17 +81,12 @@ int backward_of(condensa_ctx *ctx, const NormBackParams &P, NormBackPlan &plan, 
     }
     if constexpr (sizeof(T) == 2)
         if (eights > 1024) return backward_as<T, A, 1024, 2>(ctx, P, plan, run, stream);
-    if constexpr (A == 1) {
-        return eights <= 64 ? backward_as<T, A, 32, 2>(ctx, P, plan, run, stream) : eights <= 512 ? backward_as<T, A, 256, 2>(ctx, P, plan, run, stream)
-                                                                                                 : backward_as<T, A, 512, 2>(ctx, P, plan, run, stream);
-    } else {
-        return eights <= 32  ? backward_as<T, A, 32, 1>(ctx, P, plan, run, stream)
-             : eights <= 64  ? backward_as<T, A, 32, 2>(ctx, P, plan, run, stream)
-             : eights <= 128 ? backward_as<T, A, 128, 1>(ctx, P, plan, run, stream)
-             : eights <= 256 ? backward_as<T, A, 128, 2>(ctx, P, plan, run, stream)
-             : eights <= 512 ? backward_as<T, A, 256, 2>(ctx, P, plan, run, stream)
-                             : backward_as<T, A, 512, 2>(ctx, P, plan, run, stream);
-    }
+    return eights <= 32  ? backward_as<T, A, 32, 1>(ctx, P, plan, run, stream)
+         : eights <= 64  ? backward_as<T, A, 32, 2>(ctx, P, plan, run, stream)
+         : eights <= 128 ? backward_as<T, A, 128, 1>(ctx, P, plan, run, stream)
+         : eights <= 256 ? backward_as<T, A, 128, 2>(ctx, P, plan, run, stream)
+         : eights <= 512 ? backward_as<T, A, 256, 2>(ctx, P, plan, run, stream)
+                         : backward_as<T, A, 512, 2>(ctx, P, plan, run, stream);
 }
 
 }  // namespace

@@ -144,13 +144,13 @@ struct QuadScales {
     }
 };
 
+// (of rows that allow four values at once, at least)
 template <class T>
 __device__ __forceinline__ void store_result(const ProjectionParams &P, long long row, int col, const Eight<T> &e)
 {
     T *out = (T *)P.out + row * P.ldo;
     if (P.access == 8) store8<8>(out, col, P.width, e);
-    else if (P.access == 4) store8<4>(out, col, P.width, e);
-    else store8<1>(out, col, P.width, e);
+    else store8<4>(out, col, P.width, e);
 }
 
 // Sums of rows r0 .. r1 - 1 of a tile over `parts` CTAs of the cluster (every `step`th from `first` on), in their order, into the result.
@@ -162,6 +162,27 @@ __device__ __forceinline__ void add_parts(const ProjectionParams &P, cooperative
     constexpr int AHEAD = 4, ROWS = THREADS_ / 16;
     const int c = threadIdx.x % 16 * 8;
     r1 = (int)min((long long)r1, P.rows - row0);
+    if (P.access == 1) {                // results column by column, so that neighbouring lanes write neighbours
+        constexpr int N = 4, STEP = THREADS_ / PJ_WIDE;
+        const int column = threadIdx.x % PJ_WIDE;
+        for (int r = r0 + (int)threadIdx.x / PJ_WIDE; r < r1; r += N * STEP) {
+            float v[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = fine ? 0.0f : __uint_as_float(0x7FFFFFFFu);
+            for (int p = 0; p < parts; ++p) {
+                const float *at = (parts > 1 ? cluster.map_shared_rank(sums, first + p * step) : sums) + column;
+                float x[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k] = at[min(r + k * STEP, r1 - 1) * PJ_WIDE];
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] += x[k];
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (r + k * STEP < r1 && col0 + column < P.width) ((T *)P.out)[(row0 + r + k * STEP) * P.ldo + col0 + column] = from_f32<T>(v[k]);
+        }
+        return;
+    }
     for (int r = r0 + (int)threadIdx.x / 16; r < r1; r += 2 * ROWS) {
         float v[2][8];
 #pragma unroll
@@ -426,6 +447,13 @@ __device__ __forceinline__ u32 pack2(float lo, float hi, __nv_bfloat16) { const 
 template <int A, class T>
 __device__ __forceinline__ void write_block(const float (&v)[32], u32 *turn, T *out, long long ldo, int rows, int col0, int width, int lane)
 {
+    if constexpr (A == 1) {             // (neighbouring columns are neighbouring lanes' already)
+        if (col0 + lane < width)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < rows) out[i * ldo + col0 + lane] = from_f32<T>(v[i]);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) turn[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
     __syncwarp();
