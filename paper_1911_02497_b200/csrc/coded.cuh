@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace cs {
@@ -27,6 +29,45 @@ struct alignas(16) Eight {
     T v[8];
     __device__ __forceinline__ float operator[](int i) const { return to_f32(v[i]); }
 };
+// Eight values as fp32, and eight fp32 values rounded, two at a time.
+template <class T>
+__device__ __forceinline__ void widen(const Eight<T> &e, float (&v)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e[i];
+    } else {
+        const u32 *w = reinterpret_cast<const u32 *>(&e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(w + i));
+                v[2 * i] = f.x;
+                v[2 * i + 1] = f.y;
+            }
+        }
+    }
+}
+__device__ __forceinline__ u32 pack2(float lo, float hi, __half) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const u32 *>(&h); }
+__device__ __forceinline__ u32 pack2(float lo, float hi, __nv_bfloat16) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const u32 *>(&h); }
+template <class T>
+__device__ __forceinline__ Eight<T> rounded(const float (&v)[8])
+{
+    Eight<T> e;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = v[i];
+    } else {
+        u32 *w = reinterpret_cast<u32 *>(&e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], T());
+    }
+    return e;
+}
+
 // Keeps the values as they are in registers: what has been made of them ahead of this is made anew behind it, not kept too.
 template <class T>
 __device__ __forceinline__ void hold(Eight<T> &e)
@@ -240,7 +281,7 @@ __device__ __forceinline__ void encode8(float (&v)[8], u8 *codes, u8 *scales, in
     const u32 s = scale_of(most);
     if (c < cols) {
         store_codes<A>(codes, c, cols, codes_of(v, scale_inverse(s)));
-        if (threadIdx.x % GROUP_LANES == 0) scales[c / GROUP] = (u8)s;
+        if (threadIdx.x % GROUP_LANES == 0) scales[(u32)c / GROUP] = (u8)s;
     }
 }
 

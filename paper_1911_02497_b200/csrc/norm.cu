@@ -53,6 +53,7 @@ int forward(condensa_ctx *ctx, const condensa_norm *p, cudaStream_t stream)
     }
     P.rows = p->rows;
     P.cols = (int)p->cols;
+    P.inv_cols = 1.0f / (float)p->cols;
     P.eps = p->eps;
     P.gain_f32 = p->gain_dtype == CONDENSA_DTYPE_FP32;
     const int access = std::min({op_access(P.x, P.ldx, e, P.cols), op_access(P.residual, P.ldr, e, P.cols), op_access(P.h, P.ldh, e, P.cols),
@@ -114,6 +115,7 @@ int backward(condensa_ctx *ctx, const condensa_norm_gradient *p, cudaStream_t st
     }
     P.rows = p->rows;
     P.cols = (int)p->cols;
+    P.inv_cols = 1.0f / (float)p->cols;
     P.gain_f32 = p->gain_dtype == CONDENSA_DTYPE_FP32;
     const int access = std::min({op_access(P.dy, P.ldy, e, P.cols), op_access(P.dh, P.ldd, e, P.cols), op_access(P.h, P.ldh, e, P.cols),
                                  op_access(P.dx, P.ldx, e, P.cols), op_access(P.gain, 0, ge, P.cols)});

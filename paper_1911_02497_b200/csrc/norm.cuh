@@ -17,6 +17,7 @@ struct NormParams {
     long long ldx, ldr, ldh, ldy, ldc, lds;
     long long rows;
     int cols;
+    float inv_cols;                     // 1 / cols
     int gain_f32;
     float eps;
 };
@@ -30,6 +31,7 @@ struct NormBackParams {
     long long ldy, ldd, ldh, ldx, ldc, lds, ld_part;
     long long rows;
     int cols;
+    float inv_cols;
     int gain_f32;
 };
 
@@ -54,7 +56,12 @@ __device__ __forceinline__ F row_sum(F v, F *slots)
     return lanes_sum(lane < TPR / 32 ? slots[lane] : (F)0, 32);
 }
 
-__device__ __forceinline__ float rstd_of(float sum, int cols, float eps) { return 1.0f / sqrtf(sum / (float)cols + eps); }
+// (the root's approximation, and one Newton step: every thread of a row does this, and quotients and roots in full were a tenth of the kernel)
+__device__ __forceinline__ float rstd_of(float sum, float inv_cols, float eps)
+{
+    const float x = fmaf(sum, inv_cols, eps), r = rsqrtf(x);
+    return fmaf(r * 0.5f, fmaf(-x * r, r, 1.0f), r);
+}
 __device__ __forceinline__ float rstd_of(double sum, int cols, float eps) { return (float)(1.0 / sqrt(sum / cols + (double)eps)); }
 
 template <class T, int A>
@@ -64,13 +71,9 @@ __device__ __forceinline__ void load_gain(const void *gain, int f32, int c, int 
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = 1.0f;
     } else if (f32) {
-        const Eight<float> e = load8<A>((const float *)gain, c, cols);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = e[i];
+        widen(load8<A>((const float *)gain, c, cols), g);
     } else {
-        const Eight<T> e = load8<A>((const T *)gain, c, cols);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = e[i];
+        widen(load8<A>((const T *)gain, c, cols), g);
     }
 }
 
@@ -81,8 +84,12 @@ __device__ __forceinline__ Eight<T> load_h(const NormParams &P, long long row, i
     Eight<T> h = load8<A>((const T *)P.x + row * P.ldx, c, P.cols);
     if (P.residual) {
         const Eight<T> r = load8<A>((const T *)P.residual + row * P.ldr, c, P.cols);
+        float a[8], b[8];
+        widen(h, a);
+        widen(r, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h.v[i] = from_f32<T>(h[i] + r[i]);
+        for (int i = 0; i < 8; ++i) a[i] += b[i];
+        h = rounded<T>(a);
     }
     return h;
 }
@@ -93,14 +100,10 @@ __device__ __forceinline__ void norm_out(const NormParams &P, long long row, int
 {
     float g[8], y[8];
     load_gain<T, A>(P.gain, P.gain_f32, c, P.cols, g);
+    widen(h, y);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = h[i] * rstd * g[i];
-    if (P.y) {
-        Eight<T> o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o.v[i] = from_f32<T>(y[i]);
-        store8_warp<A>((T *)P.y + row * P.ldy, c, P.cols, o, turn);
-    }
+    for (int i = 0; i < 8; ++i) y[i] = y[i] * rstd * g[i];
+    if (P.y) store8_warp<A>((T *)P.y + row * P.ldy, c, P.cols, rounded<T>(y), turn);
     if (P.codes) {
         if (c + 8 > P.cols) {
 #pragma unroll
@@ -123,9 +126,10 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
     Eight<T> *turn = s_turns + (A == 1 ? threadIdx.x / 32 * 32 : 0);
     pdl_wait();
     pdl_launch_dependents();
-    const long long row = (long long)blockIdx.x * RowThreads<TPR>::ROWS + threadIdx.x / TPR;
+    constexpr int ROWS = RowThreads<TPR>::ROWS;
+    const long long row = ROWS == 1 ? blockIdx.x : (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
     if (row >= P.rows) return;                          // (whole rows of threads: no barrier misses them)
-    const int t = threadIdx.x % TPR;
+    const int t = ROWS == 1 ? threadIdx.x : threadIdx.x % TPR;
     Eight<T> h[NV];
     float sum = 0.0f;
 #pragma unroll
@@ -133,11 +137,13 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         if (P.h) store8_warp<A>((T *)P.h + row * P.ldh, (v * TPR + t) * 8, P.cols, h[v], turn);
+        float f[8];
+        widen(h[v], f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(h[v][i], h[v][i], sum);
+        for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
     }
     sum = row_sum<TPR>(sum, slots);
-    float rstd = rstd_of(sum, P.cols, P.eps);
+    float rstd = rstd_of(sum, P.inv_cols, P.eps);
     if (!(sum <= 3.4e38f)) {                            // beyond fp32, or not a number (the same for the row)
         double d = 0.0;
 #pragma unroll
@@ -192,18 +198,16 @@ template <class T, int A>
 __device__ __forceinline__ void norm_back_out(const NormBackParams &P, long long row, int c, const Eight<T> &dy, const Eight<T> &h,
                                               const Eight<T> &dh, const float (&g)[8], float rstd, float q, Eight<T> *turn)
 {
-    float d[8];
+    float d[8], u[8], s[8];
+    widen(dy, d);
+    widen(h, u);
+    if (P.dh) widen(dh, s);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        d[i] = rstd * fmaf(-(h[i] * rstd), q, dy[i] * g[i]);
-        if (P.dh) d[i] += dh[i];
+        d[i] = rstd * fmaf(-(u[i] * rstd), q, d[i] * g[i]);
+        if (P.dh) d[i] += s[i];
     }
-    if (P.dx) {
-        Eight<T> o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o.v[i] = from_f32<T>(d[i]);
-        store8_warp<A>((T *)P.dx + row * P.ldx, c, P.cols, o, turn);
-    }
+    if (P.dx) store8_warp<A>((T *)P.dx + row * P.ldx, c, P.cols, rounded<T>(d), turn);
     if (P.codes) {
         if (c + 8 > P.cols) {
 #pragma unroll
@@ -258,7 +262,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
     Eight<T> *turn = s_turns + (A == 1 ? threadIdx.x / 32 * 32 : 0);
     pdl_wait();
     pdl_launch_dependents();
-    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const int t = ROWS == 1 ? threadIdx.x : threadIdx.x % TPR, sub = ROWS == 1 ? 0 : threadIdx.x / TPR;
     constexpr bool KEEP = TPR < 1024;                   // (a thread of 1024 has 64 registers: the gain is read again, from L1)
     float g[NV][8], acc[NV][8] = {};
 #pragma unroll
@@ -314,7 +318,9 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if (!KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
-            const Eight<T> dy = take(0, v), h = take(1, v);
+            float dy[8], h[8];
+            widen(take(0, v), dy);
+            widen(take(1, v), h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float p = dy[i] * (h[i] * rstd);
@@ -323,7 +329,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
             }
         }
         if (P.dx || P.codes) {                          // (the same for all)
-            const float q = row_sum<TPR>(sum, slots[phase]) / (float)P.cols;
+            const float q = row_sum<TPR>(sum, slots[phase]) * P.inv_cols;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 if (!KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
@@ -368,7 +374,7 @@ __global__ void __launch_bounds__(TPR) k_norm_backward_long(const __grid_constan
         for (int i = 0; i < 8; ++i) part = fmaf(dy[i] * (h[i] * rstd), g[i], part);
         sum += part;
     }
-    const float q = row_sum<TPR>(sum, slots) / (float)P.cols;
+    const float q = row_sum<TPR>(sum, slots) * P.inv_cols;
     for (int c0 = 0; c0 < P.cols; c0 += TPR * 8) {
         const int c = c0 + threadIdx.x * 8;
         const Eight<T> dy = load8<A>(dyr, c, P.cols), h = load8<A>(hr, c, P.cols);
@@ -488,8 +494,7 @@ __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__
 #pragma unroll
     for (int i = 0; i < ENC_UNITS; ++i) {
         float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = e[i][j];
+        widen(e[i], v);
         float most = group_most(most_raw(e[i]), 0xFFFFFFFFu);
         if (is_odd(most)) {
             most = group_most(most_finite(v), 0xFFFFu << (threadIdx.x & 16));
@@ -541,8 +546,7 @@ __global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_consta
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = e[i][j];
+            widen(e[i], v);
             most = fmaxf(most, most_finite(v));
         }
         join(s_most[1]);
@@ -556,8 +560,7 @@ __global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_consta
         const long long r = r0 + i * STEP;
         if (A != 1 && (r >= P.rows || c >= P.cols)) continue;
         float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = e[i][j];
+        widen(e[i], v);
         if (odd) odd_to_nan(v);
         const uint2 q = codes_of(v, inverse);
         const bool there = A != 1 || (r < P.rows && c < P.cols);

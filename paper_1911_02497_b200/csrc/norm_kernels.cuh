@@ -14,7 +14,7 @@ int resident_ctas(condensa_ctx *ctx, const void *f, int block, int smem, int &co
             count = k.count;
             return CONDENSA_OK;
         }
-    if (smem > 48 * 1024) CU_TRY(ctx, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    if (smem) CU_TRY(ctx, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     count = 0;
     CU_TRY(ctx, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&count, f, block, (size_t)smem));
     if (count < 1) return fail(ctx, CONDENSA_ERR_INTERNAL, "a kernel of the norm does not fit an SM");

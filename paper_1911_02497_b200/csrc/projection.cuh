@@ -214,10 +214,7 @@ __device__ __forceinline__ void add_parts(const ProjectionParams &P, cooperative
 #pragma unroll
         for (int k = 0; k < 2; ++k)
             if (r + k * ROWS < r1) {
-                Eight<T> e;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e.v[i] = from_f32<T>(v[k][i]);
-                store_result<T>(P, row0 + r + k * ROWS, col0 + c, e);
+                store_result<T>(P, row0 + r + k * ROWS, col0 + c, rounded<T>(v[k]));
             }
     }
 }
@@ -439,9 +436,6 @@ __device__ __forceinline__ void tmem_ld(u32 addr, float (&v)[32])
                    "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
                    "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]) : "r"(addr));
 }
-__device__ __forceinline__ u32 pack2(float lo, float hi, __half) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const u32 *>(&h); }
-__device__ __forceinline__ u32 pack2(float lo, float hi, __nv_bfloat16) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const u32 *>(&h); }
-
 // Sums of 32 rows x 32 output columns, a column per lane, into the result: neighbouring rows go as pairs through the
 // warp's 2 KB of shared memory and come back as eight neighbouring columns of a row. `out`: row 0, column 0; `rows` of them are wanted.
 template <int A, class T>
