@@ -449,6 +449,10 @@ class Coded:
         self.projection = Projection(self.struct, self.rows, self.cols) if high > 1 else None
 
 
+_REAL = (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16)
+_NO_CODE = CodedMatrix()
+
+
 def coded_rows(codes, scales) -> Coded:
     """Activations or gradients in 8 bits: ``codes`` [rows, cols] float8_e4m3fn or uint8 with rows a multiple of 16 bytes apart, ``scales``
     [rows, ceil(cols / 128)] uint8 with rows a multiple of 4 bytes apart (slices of wider buffers: ``torch.empty(rows, -(-cols // 16) *
@@ -640,14 +644,17 @@ class Context:
         if device != self.device:
             raise ValueError("%s is on another device than the context" % name)
 
-    def _matrix(self, x, rows: int, cols: int, dtype, name: str):
-        """Address and row stride of an operand (None: 0, 0)."""
-        if x is None:
-            return None, 0
-        self._here(x.get_device(), name)
-        if x.dim() != 2 or x.shape[1] != cols:
-            raise ValueError("%s must be a [%d, %d] matrix" % (name, rows, cols))
-        return _rows_of(x, rows, cols, dtype, name)
+    def _matrix(self, x, shape, dtype, name: str):
+        """Address and row stride of an operand of this shape and type."""
+        if x.get_device() != self.device:
+            self._here(x.get_device(), name)
+        if x.shape != shape or x.dtype != dtype:
+            raise ValueError("%s must be a [%d, %d] matrix of %s" % ((name,) + tuple(shape) + (dtype,)))
+        ld, step = x.stride()
+        rows, cols = shape
+        if step != 1 and cols > 1:
+            raise ValueError("the rows of %s must be contiguous" % name)
+        return x.data_ptr(), (ld if rows > 1 else max(cols, ld))
 
     def _coded(self, code, rows: int, cols: int, high: int, name: str) -> Coded:
         if not isinstance(code, Coded) or code.high != high:
@@ -679,21 +686,22 @@ class Context:
 
     def encode_rows(self, x, out: Coded, stream=None):
         """``x`` [rows, cols] (float32, float16, bfloat16) into ``out``, a scale for every 128 columns of a row."""
-        rows, cols = x.shape
-        code = _dtype_code(x, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "x")
-        p, ld = self._matrix(x, rows, cols, x.dtype, "x")
+        rows, cols = shape = x.shape
+        code = _dtype_code(x, _REAL, "x")
+        p, ld = self._matrix(x, shape, x.dtype, "x")
         out = self._coded(out, rows, cols, 1, "out")
         self._check(self._lib.condensa_encode_rows(self._h, p, ld, rows, cols, code, C.byref(out.struct), _stream_handle(stream)))
 
     def encode_blocks(self, w, out: Coded, theta=None, stream=None):
         """``w`` [n, k] (float32, float16, bfloat16) into ``out``, a scale for every 128 x 128; ``theta`` (float32, may be ``w`` itself, or None)
         receives the values that the codes stand for."""
-        n, k = w.shape
-        code = _dtype_code(w, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "w")
-        p, ld = self._matrix(w, n, k, w.dtype, "w")
+        n, k = shape = w.shape
+        code = _dtype_code(w, _REAL, "w")
+        p, ld = self._matrix(w, shape, w.dtype, "w")
+        pt, ldt = None, 0
         if theta is not None:
             _dtype_code(theta, (DTYPE_FP32,), "theta")
-        pt, ldt = self._matrix(theta, n, k, theta.dtype if theta is not None else None, "theta")
+            pt, ldt = self._matrix(theta, shape, theta.dtype, "theta")
         out = self._coded(out, n, k, CODE_GROUP, "out")
         self._check(self._lib.condensa_encode_blocks(self._h, p, ld, n, k, code, C.byref(out.struct), pt, ldt, _stream_handle(stream)))
 
@@ -702,7 +710,7 @@ class Context:
         rows = x.rows
         x = self._coded(x, rows, depth, 1, names[0])
         code = _dtype_code(y, (DTYPE_FP16, DTYPE_BF16), names[1])
-        p, ld = self._matrix(y, rows, width, y.dtype, names[1])
+        p, ld = self._matrix(y, (rows, width), y.dtype, names[1])
         self._check(call(self._h, C.byref(w.projection), C.byref(x.struct), rows, p, ld, code, _stream_handle(stream)))
 
     def projection_forward(self, w: Coded, x: Coded, y, stream=None):
@@ -717,14 +725,15 @@ class Context:
         """Root-mean-square norm of the rows of ``x + residual``: ``h`` receives the sum (it may be ``x`` or ``residual``), ``y`` the
         normalised rows times ``gain`` (float32, or the type of ``x``; None: ones), ``code`` the same in 8 bits, ``rstd`` (float32) what
         :meth:`norm_backward` needs. Any of the results may be None."""
-        rows, cols = x.shape
-        dtype = _dtype_code(x, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "x")
+        rows, cols = shape = x.shape
+        kind = x.dtype
+        dtype = _dtype_code(x, _REAL, "x")
         pg, gain_dtype = self._gain(gain, cols, dtype)
-        px, ldx = self._matrix(x, rows, cols, x.dtype, "x")
-        pr, ldr = self._matrix(residual, rows, cols, x.dtype, "residual")
-        ph, ldh = self._matrix(h, rows, cols, x.dtype, "h")
-        py, ldy = self._matrix(y, rows, cols, x.dtype, "y")
-        coded = self._coded(code, rows, cols, 1, "code").struct if code is not None else CodedMatrix()
+        px, ldx = self._matrix(x, shape, kind, "x")
+        pr, ldr = (None, 0) if residual is None else self._matrix(residual, shape, kind, "residual")
+        ph, ldh = (None, 0) if h is None else self._matrix(h, shape, kind, "h")
+        py, ldy = (None, 0) if y is None else self._matrix(y, shape, kind, "y")
+        coded = self._coded(code, rows, cols, 1, "code").struct if code is not None else _NO_CODE
         n = Norm(px, pr, pg, ph, py, coded, self._vector(rstd, rows, "rstd"), ldx, ldr, ldh, ldy, rows, cols, eps, dtype, gain_dtype, 0)
         self._check(self._lib.condensa_norm_forward(self._h, C.byref(n), _stream_handle(stream)))
 
@@ -732,14 +741,15 @@ class Context:
         """Gradients of :meth:`norm_forward`: ``h`` is what it left there (``x`` without a residual), ``dh`` the gradient that reaches h
         otherwise (None: none). ``dx`` receives the gradient of ``x`` and of the residual (it may be ``dy`` or ``dh``), ``code`` the same
         in 8 bits, ``dgain`` (float32) that of the gain, added to with ``accumulate``."""
-        rows, cols = dy.shape
-        dtype = _dtype_code(dy, (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), "dy")
+        rows, cols = shape = dy.shape
+        kind = dy.dtype
+        dtype = _dtype_code(dy, _REAL, "dy")
         pg, gain_dtype = self._gain(gain, cols, dtype)
-        py, ldy = self._matrix(dy, rows, cols, dy.dtype, "dy")
-        pd, ldd = self._matrix(dh, rows, cols, dy.dtype, "dh")
-        ph, ldh = self._matrix(h, rows, cols, dy.dtype, "h")
-        px, ldx = self._matrix(dx, rows, cols, dy.dtype, "dx")
-        coded = self._coded(code, rows, cols, 1, "code").struct if code is not None else CodedMatrix()
+        py, ldy = self._matrix(dy, shape, kind, "dy")
+        pd, ldd = (None, 0) if dh is None else self._matrix(dh, shape, kind, "dh")
+        ph, ldh = self._matrix(h, shape, kind, "h")
+        px, ldx = (None, 0) if dx is None else self._matrix(dx, shape, kind, "dx")
+        coded = self._coded(code, rows, cols, 1, "code").struct if code is not None else _NO_CODE
         n = NormGradient(py, pd, ph, pg, self._vector(rstd, rows, "rstd"), px, coded, self._vector(dgain, cols, "dgain"), ldy, ldd, ldh, ldx, rows, cols,
                          dtype, gain_dtype, 1 if accumulate else 0, 0)
         self._check(self._lib.condensa_norm_backward(self._h, C.byref(n), _stream_handle(stream)))
