@@ -483,8 +483,10 @@ CONDENSA_API int condensa_encode_blocks(condensa_ctx *ctx, const void *w, int64_
  * exact; sums are formed in fp32 by the matrix instruction, 32 terms at a time, which cuts instead of rounding (measured: the terms and
  * the sum so far at 2^-25 of the largest of them, the new sum at 2^-23 of itself), and are rounded once to the result. fp32 results are not offered for that reason. Rows do not mix: a NaN in a row
  * stays in that row of the result. The order of a sum depends on the shapes and the device only.
- * n and k at most 2^22, rows at most 2^31 - 256. No workspace is used. Any alignment of the result is taken; rows that are 16- or
- * 8-byte aligned are faster. */
+ * n and k at most 2^22, rows at most 2^31 - 256. No workspace is used, so calls on different streams do not wait for one another, and
+ * calls may be captured into a CUDA graph after one plain call of the same shape. Any alignment of the result is taken; rows that are
+ * 16- or 8-byte aligned are faster, and so are rows of codes a multiple of 128 bytes apart. Should a wait inside a kernel run out (about a
+ * second), what it concerns of the result becomes NaN. */
 typedef struct {
     condensa_coded code;    /* block form, read only                                               */
     int64_t n, k;

@@ -70,7 +70,7 @@ int backward_of(condensa_ctx *ctx, const NormBackParams &P, NormBackPlan &plan, 
     if (eights > (sizeof(T) == 4 ? 1024 : 2048)) {
         const unsigned strips = (unsigned)((eights + THREADS - 1) / THREADS);
         if (!run) {
-            plan.grid = stream_grid(ctx, P.rows, std::max(1, 4 / (int)strips));
+            plan.grid = (int)std::min(P.rows, std::max(1ll, 4ll * ctx->num_sms / strips));
             plan.slots = plan.grid;
             return CONDENSA_OK;
         }

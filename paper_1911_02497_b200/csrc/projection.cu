@@ -13,26 +13,23 @@ namespace {
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-int encode_tiled(condensa_ctx *ctx, EncodeTiled &f)
+// (an entry point of the driver: the same for the process)
+EncodeTiled find_encode_tiled()
 {
-    static EncodeTiled known = nullptr;         // (an entry point of the driver: the same for the process)
-    if (!known) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult got = cudaDriverEntryPointSymbolNotFound;
-        CU_TRY(ctx, cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &got));
-        if (got != cudaDriverEntryPointSuccess || !p) return fail(ctx, CONDENSA_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
-        known = (EncodeTiled)p;
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult got = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &got) != cudaSuccess) {
+        cudaGetLastError();
+        return nullptr;
     }
-    f = known;
-    return CONDENSA_OK;
+    return got == cudaDriverEntryPointSuccess ? (EncodeTiled)p : nullptr;
 }
 
 // Boxes of 128 columns x `high` rows of a code matrix, zero outside, swizzled in shared memory by 128 bytes.
 int code_map(condensa_ctx *ctx, CUtensorMap &map, const condensa_coded &c, long long rows, long long cols, int high)
 {
-    EncodeTiled f;
-    const int rc = encode_tiled(ctx, f);
-    if (rc) return rc;
+    static const EncodeTiled f = find_encode_tiled();
+    if (!f) return fail(ctx, CONDENSA_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
     const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)c.ld};
     const cuuint32_t box[2] = {GROUP, (cuuint32_t)high}, step[2] = {1, 1};
     const CUresult e = f(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, c.codes, dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -105,7 +102,6 @@ int resident_clusters(condensa_ctx *ctx, const Variant &v, int n, int &count)
     cfg.numAttrs = 1;
     count = 0;
     CU_TRY(ctx, cudaOccupancyMaxActiveClusters(&count, (const void *)v.f, &cfg));
-    if (count < 1) return fail(ctx, CONDENSA_ERR_INTERNAL, "no cluster of %d CTAs fits the device", n);
     ctx->cluster_fit.push_back({(const void *)v.f, n, count});
     return CONDENSA_OK;
 }
@@ -130,17 +126,20 @@ int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups,
             best = s;
         }
     };
-    const auto cut = [&](long long n, int step) { return (int)(((rows + n - 1) / n + step - 1) / step * step); };      // rows of n equal tiles
+    const auto cut = [&](int most, int step) {          // rows of equal tiles of at most so many
+        const long long n = (rows + most - 1) / most;
+        return (int)(((rows + n - 1) / n + step - 1) / step * step);
+    };
     int before = 0;
-    for (long long n = (rows + PJ_MAX_TILE - 1) / PJ_MAX_TILE; n <= (rows + 15) / 16 && n <= 64; ++n) {
-        const int tile = cut(n, 16);
+    for (int most = PJ_MAX_TILE; most >= 16; most -= 16) {
+        const int tile = cut(most, 16);
         if (tile == before) continue;
         before = tile;
         const long long tiles = (rows + tile - 1) / tile * ((width + PJ_WIDE - 1) / PJ_WIDE);
         for (int parts = 1; parts <= std::min(PJ_MAX_PARTS, quads); ++parts) {
             const Shape s = {false, tile, parts, tiles * parts};
             const long long ctas = tiles * parts;
-            double rounds = (double)((ctas + ctx->num_sms - 1) / ctx->num_sms);
+            const double rounds = (double)((ctas + ctx->num_sms - 1) / ctx->num_sms);
             if (parts > 1) {
                 int fit = 0;
                 const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), parts, fit);
@@ -151,8 +150,8 @@ int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups,
         }
     }
     before = 0;
-    for (long long n = (rows + PP_TILE - 1) / PP_TILE; rows > 64 && n <= (rows + 63) / 64 && (before == 0 || before > 64); ++n) {
-        const int tile = cut(n, 32);
+    for (int most = PP_TILE; rows > 64 && most >= 64; most -= 32) {
+        const int tile = cut(most, 32);
         if (tile == before) continue;
         before = tile;
         const long long tiles = (rows + tile - 1) / tile * ((width + 2 * PJ_WIDE - 1) / (2 * PJ_WIDE));
@@ -161,7 +160,7 @@ int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups,
             int fit = 0;
             const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), 2 * parts, fit);
             if (rc) return rc;
-            if (parts > 1 && tiles > fit) break;
+            if (fit < 1 || (parts > 1 && tiles > fit)) break;
             if (parts == 1) s.clusters = std::min(tiles, (long long)fit);
             const double rounds = (double)((tiles + fit - 1) / fit);
             offer(s, 2 * s.clusters, rounds, 0.1 + 0.0011 * tile, PJ_A + 0.5 * GROUP * tile, 1.5 + 0.004 * tile * rounds + (parts > 1 ? 2.0 + 0.01 * tile + 0.5 * parts : 0.0));
@@ -214,11 +213,13 @@ int run(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x
     P.stages = std::min(std::min(v.stages, deepest), room / stage);
     P.ring = std::max(P.stages * stage, v.sums ? P.tile * PJ_WIDE * 4 : 0);
     P.columns = 32;
-    while (P.columns < (u32)P.tile + 16) P.columns *= 2;
+    while (P.columns < (u32)P.tile + PJ_SLOTS * 8) P.columns *= 2;
     if ((rc = code_map(ctx, P.w, w->code, w->n, w->k, PJ_WIDE)) != 0) return rc;
     if ((rc = code_map(ctx, P.x, *x, rows, depth, high)) != 0) return rc;
     if ((rc = allow_smem(ctx, v.f)) != 0) return rc;
-    PdlLaunch l(ctx, 1, v.threads, (size_t)(v.fixed + P.ring), stream);
+    // A CTA of a pair has the SM to itself: it waits for its partner while it holds tensor memory, and two pairs that held it on one
+    // SM each would wait for one another. (A CTA by itself gives it back ahead of any such wait.)
+    PdlLaunch l(ctx, 1, v.threads, shape.pair ? (size_t)(PJ_SMEM_MOST - 1024) : (size_t)(v.fixed + P.ring), stream);
     l.cfg.gridDim = dim3((unsigned)ctas);
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;

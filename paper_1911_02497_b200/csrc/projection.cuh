@@ -20,6 +20,7 @@ constexpr int PJ_QUAD = 4;              // groups of the depth whose scales shar
 constexpr int PJ_STAGES = 12;           // most stages of the ring
 // Two warps bring the scales, two quads at a time and in turn: a warp's loads for its next two are on their way while it waits for
 // room. (One warp, a quad at a time, kept the products waiting: 2.2 PFLOP/s.)
+// A slot is a place in shared memory and one in tensor memory: it is filled again when the products of its batch are complete.
 constexpr int PJ_BATCH = 2, PJ_SLOTS = 2 * PJ_BATCH;    // quads
 constexpr int PJ_A = GROUP * PJ_WIDE;   // bytes of a stage's weights
 constexpr int PJ_SCALES = 1024;         // bytes of a quad's scales: weights, rows
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
             bool fine = true;
             for (int q = q0; q < q1 && fine; ++q) {
                 const int i = q - q0, slot = i % PJ_SLOTS, batch = i / PJ_BATCH;
-                const u32 to = sa + (u32)(i & 1) * 8;
+                const u32 to = sa + (u32)slot * 8;
                 if (i % PJ_BATCH == 0) {
                     fine = mbar_wait(sc_full + 8 * (batch & 1), (u32)(batch / 2) & 1);
                     if (!fine) break;
@@ -562,7 +563,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
                 if (!fine) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (int q = q0; q < q1 && fine; ++q, ++quad) {
-                    const u32 to = sa + (u32)(quad & 1) * 12, src = scales_u + (u32)(quad % PJ_SLOTS) * PP_SCALES, batch = (u32)quad / PJ_BATCH;
+                    const u32 slot = (u32)quad % PJ_SLOTS, to = sa + slot * 12, src = scales_u + slot * PP_SCALES, batch = (u32)quad / PJ_BATCH;
                     if (quad % PJ_BATCH == 0) {
                         fine = mbar_wait(sc_full + 8 * (batch & 1), batch / 2 & 1);
                         if (!fine) break;
