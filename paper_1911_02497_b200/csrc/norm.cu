@@ -138,22 +138,17 @@ int backward(condensa_ctx *ctx, const condensa_norm_gradient *p, cudaStream_t st
 
 // ------------------------------------------------------------------ encoders
 typedef void (*Encoder)(EncodeParams);
-template <class T> Encoder row_encoder_of(int access) { return access == 8 ? k_encode_rows<T, 8> : access == 4 ? k_encode_rows<T, 4> : k_encode_rows<T, 1>; }
+template <class T, int NG> Encoder row_encoder_as(int access) { return access == 8 ? k_encode_rows<T, 8, NG> : access == 4 ? k_encode_rows<T, 4, NG> : k_encode_rows<T, 1, NG>; }
+template <class T> Encoder row_encoder_of(int access, int ng) { return ng == 4 ? row_encoder_as<T, 4>(access) : ng == 2 ? row_encoder_as<T, 2>(access) : row_encoder_as<T, 1>(access); }
 template <class T> Encoder block_encoder_of(int access) { return access == 8 ? k_encode_blocks<T, 8> : access == 4 ? k_encode_blocks<T, 4> : k_encode_blocks<T, 1>; }
-Encoder row_encoder(int dtype, int access)
+Encoder row_encoder(int dtype, int access, int ng)
 {
-    return dtype == CONDENSA_DTYPE_BF16 ? row_encoder_of<__nv_bfloat16>(access) : dtype == CONDENSA_DTYPE_FP16 ? row_encoder_of<__half>(access) : row_encoder_of<float>(access);
+    return dtype == CONDENSA_DTYPE_BF16 ? row_encoder_of<__nv_bfloat16>(access, ng) : dtype == CONDENSA_DTYPE_FP16 ? row_encoder_of<__half>(access, ng) : row_encoder_of<float>(access, ng);
 }
 Encoder block_encoder(int dtype, int access)
 {
     return dtype == CONDENSA_DTYPE_BF16 ? block_encoder_of<__nv_bfloat16>(access) : dtype == CONDENSA_DTYPE_FP16 ? block_encoder_of<__half>(access) : block_encoder_of<float>(access);
 }
-void set_groups(EncodeParams &P)
-{
-    P.groups = (u32)((P.cols + GROUP - 1) / GROUP);
-    P.reciprocal = P.groups == 1 ? 0xFFFFFFFFu : (u32)((1ull << 32) / P.groups);
-}
-
 int encode_rows(condensa_ctx *ctx, const void *x, long long ldx, long long rows, long long cols, int dtype, const condensa_coded *out, cudaStream_t stream)
 {
     if (!out) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "out is NULL");
@@ -171,11 +166,16 @@ int encode_rows(condensa_ctx *ctx, const void *x, long long ldx, long long rows,
     P.codes = out->codes; P.scales = out->scales; P.ldc = out->ld; P.lds = out->ld_scales;
     P.rows = rows;
     P.cols = (int)cols;
-    set_groups(P);
-    const long long per = THREADS / GROUP_LANES * ENC_UNITS, grid = (rows * P.groups + per - 1) / per;
+    P.groups = (u32)((P.cols + GROUP - 1) / GROUP);
+    // runs of four groups, of two or of one, the longest that leave no more than a quarter of their places empty
+    const auto empty = [&](u32 n) { return (P.groups + n - 1) / n * n - P.groups; };
+    const int ng = 4 * empty(4) <= P.groups ? 4 : 4 * empty(2) <= P.groups ? 2 : 1;
+    P.runs = (P.groups + ng - 1) / ng;
+    P.reciprocal = P.runs == 1 ? 0xFFFFFFFFu : (u32)((1ull << 32) / P.runs);
+    const long long per = THREADS / GROUP_LANES * (ENC_UNITS / ng), grid = (rows * P.runs + per - 1) / per;
     if (grid > 0x7FFFFFFFll) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "too many groups for one launch");
     CU_TRY(ctx, cudaSetDevice(ctx->device));
-    return op_launch(ctx, "k_encode_rows", row_encoder(dtype, op_access(x, ldx, e, cols)), dim3((unsigned)grid), THREADS, stream, P);
+    return op_launch(ctx, "k_encode_rows", row_encoder(dtype, op_access(x, ldx, e, cols), ng), dim3((unsigned)grid), THREADS, stream, P);
 }
 
 int encode_blocks(condensa_ctx *ctx, const void *w, long long ldw, long long n, long long k, int dtype, const condensa_coded *out, float *theta, long long ld_theta,
@@ -200,7 +200,7 @@ int encode_blocks(condensa_ctx *ctx, const void *w, long long ldw, long long n, 
     P.theta = theta; P.ld_theta = ld_theta;
     P.rows = n;
     P.cols = (int)k;
-    set_groups(P);
+    P.groups = (u32)((P.cols + GROUP - 1) / GROUP);
     CU_TRY(ctx, cudaSetDevice(ctx->device));
     return op_launch(ctx, "k_encode_blocks", block_encoder(dtype, std::min(op_access(w, ldw, e, k), op_access(theta, ld_theta, 4, k))),
                      dim3((unsigned)((n + GROUP - 1) / GROUP * P.groups)), ENC_BLOCK, stream, P);

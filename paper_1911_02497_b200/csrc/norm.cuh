@@ -436,7 +436,8 @@ struct EncodeParams {
     long long ldx, ldc, lds, ld_theta;
     long long rows;
     int cols;
-    u32 groups, reciprocal;             // of a row; floor(2^32 / groups), at most 2^32 - 1
+    u32 groups;                         // of a row
+    u32 runs, reciprocal;               // rows: runs of groups of a row; floor(2^32 / runs), at most 2^32 - 1
 };
 
 constexpr int ENC_UNITS = 4;            // groups of a half-warp, all of whose loads leave together
@@ -460,50 +461,58 @@ __device__ __forceinline__ float most_raw(const Eight<T> &e)
     return to_f32(*reinterpret_cast<const T *>(&top));
 }
 
-// Rows: nothing is shared between groups, so half-warps take them one after the other, whatever rows they lie in.
-template <class T, int A>
+// Rows: nothing is shared between groups, so half-warps take them one after the other, whatever rows they lie in: runs of NG
+// neighbouring groups of a row, for which a place is found once (a place for each group: 28.5 us for 8192 x 6000 in bf16).
+template <class T, int A, int NG>
 __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__ EncodeParams P)
 {
     pdl_wait();
     pdl_launch_dependents();
-    constexpr int HALVES = THREADS / GROUP_LANES;
+    constexpr int HALVES = THREADS / GROUP_LANES, UNITS = ENC_UNITS / NG;
     const int half = threadIdx.x / GROUP_LANES, lane = threadIdx.x % GROUP_LANES;
-    const u64 units = (u64)P.rows * P.groups, first = (u64)blockIdx.x * (HALVES * ENC_UNITS) + half;
-    u64 row[ENC_UNITS];
-    int c[ENC_UNITS];
-    Eight<T> e[ENC_UNITS];
+    const u64 units = (u64)P.rows * P.runs, first = (u64)blockIdx.x * (HALVES * UNITS) + half;
+    u64 row[UNITS];
+    int c[UNITS];
+    Eight<T> e[UNITS][NG];
 #pragma unroll
-    for (int i = 0; i < ENC_UNITS; ++i) {
+    for (int i = 0; i < UNITS; ++i) {
         const u64 u = first + i * HALVES;
         u32 g;
         if (units >> 32) {
-            row[i] = u / P.groups;
-            g = (u32)(u - row[i] * P.groups);
+            row[i] = u / P.runs;
+            g = (u32)(u - row[i] * P.runs);
         } else {                        // (the estimate by the reciprocal is the quotient or one less)
             u32 r = __umulhi((u32)u, P.reciprocal);
-            g = (u32)u - r * P.groups;
-            if (g >= P.groups) {
-                g -= P.groups;
+            g = (u32)u - r * P.runs;
+            if (g >= P.runs) {
+                g -= P.runs;
                 r += 1;
             }
             row[i] = r;
         }
-        c[i] = u < units ? (int)g * GROUP + lane * 8 : P.cols;           // (P.cols: nothing to read or write)
-        e[i] = load8<A>((const T *)P.x + row[i] * P.ldx, c[i], P.cols);
+        c[i] = u < units ? (int)g * (NG * GROUP) + lane * 8 : P.cols;    // (P.cols: nothing to read or write)
+        const T *x = (const T *)P.x + row[i] * P.ldx;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) e[i][k] = load8<A>(x, c[i] + k * GROUP, P.cols);
     }
 #pragma unroll
-    for (int i = 0; i < ENC_UNITS; ++i) {
-        float v[8];
-        widen(e[i], v);
-        float most = group_most(most_raw(e[i]), 0xFFFFFFFFu);
-        if (is_odd(most)) {
-            most = group_most(most_finite(v), 0xFFFFu << (threadIdx.x & 16));
-            odd_to_nan(v);
-        }
-        const u32 s = scale_of(most);
-        if (c[i] < P.cols) {
-            store_codes<A>(P.codes + row[i] * P.ldc, c[i], P.cols, codes_of(v, scale_inverse(s)));
-            if (lane == 0) P.scales[row[i] * P.lds + c[i] / GROUP] = (u8)s;
+    for (int i = 0; i < UNITS; ++i) {
+        u8 *codes = P.codes + row[i] * P.ldc, *scales = P.scales + row[i] * P.lds;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            const int at = c[i] + k * GROUP;
+            float v[8];
+            widen(e[i][k], v);
+            float most = group_most(most_raw(e[i][k]), 0xFFFFFFFFu);
+            if (is_odd(most)) {
+                most = group_most(most_finite(v), 0xFFFFu << (threadIdx.x & 16));
+                odd_to_nan(v);
+            }
+            const u32 s = scale_of(most);
+            if (at < P.cols) {
+                store_codes<A>(codes, at, P.cols, codes_of(v, scale_inverse(s)));
+                if (lane == 0) scales[(u32)at / GROUP] = (u8)s;
+            }
         }
     }
 }
