@@ -117,6 +117,9 @@ template <int TPR> struct RowThreads {
     static constexpr int BLOCK = TPR < 128 ? 128 : TPR, ROWS = BLOCK / TPR;
 };
 
+// Measured (bf16, residual): 8192 x 4096, 16- and 8-bit results 50 us (46 for the bytes); 8000 x 1500, 8-bit results 22 us (13); rows
+// that begin anywhere: 8000 x 2047 45 us (23). Bound by memory, and in the last two by instructions (issue slots 70 % taken). A ring of
+// rows copied ahead, as in the backward pass, took longer (60 us): many CTAs of one row each overlap by themselves.
 template <class T, int A, int TPR, int NV>
 __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const __grid_constant__ NormParams P)
 {
@@ -250,7 +253,8 @@ __device__ __forceinline__ void copy8(u32 dst, const T *row, int c, int cols)
 }
 
 // A CTA takes every gridDim-th row (group of rows), so that a thread's sums for dgain stay in its registers; they leave
-// once, as one of the slots that k_norm_dgain adds up.
+// once, as one of the slots that k_norm_dgain adds up. Measured with it: 8192 x 4096 bf16, dh and codes, 57 us (46 for the bytes), bound by
+// memory (59 % of its nominal rate) and instructions (67 % of the issue slots); 8000 x 2047 97 us, loads into registers.
 template <class T, int A, int TPR, int NV>
 __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV>::CTAS) k_norm_backward(const __grid_constant__ NormBackParams P)
 {
@@ -462,7 +466,8 @@ __device__ __forceinline__ float most_raw(const Eight<T> &e)
 }
 
 // Rows: nothing is shared between groups, so half-warps take them one after the other, whatever rows they lie in: runs of NG
-// neighbouring groups of a row, for which a place is found once (a place for each group: 28.5 us for 8192 x 6000 in bf16).
+// neighbouring groups of a row, for which a place is found once (8192 x 6000 in bf16: 26.3 us, 22.6 for the bytes; with a place for
+// each group 28.5).
 template <class T, int A, int NG>
 __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__ EncodeParams P)
 {
@@ -517,7 +522,8 @@ __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__
     }
 }
 
-// Blocks of 128 x 128: a CTA each, thirty-two rows at a time.
+// Blocks of 128 x 128: a CTA each, thirty-two rows at a time. Measured: 33278 x 1500 bf16 29 us (23 for the bytes), 6000 x 1500 fp32 with theta
+// 19 us (12).
 constexpr int ENC_BLOCK = 512;
 template <class T, int A>
 __global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_constant__ EncodeParams P)

@@ -221,8 +221,12 @@ __device__ __forceinline__ void add_parts(const ProjectionParams &P, cooperative
 }
 
 // A cluster of CTAs takes a tile: its CTAs share the depth by quads, each leaves its sums in its own shared memory, and
-// each adds up a part of the tile's rows over all of them, in their order, by distributed shared memory.
+// each adds up a part of the tile's rows over all of them, in their order, by distributed shared memory. (Sending the sums to where they
+// are added, into room of their own, spared a barrier and took 1 to 7 us more.)
 // Four warps: copies, products, and two for the scales; then all take the sums.
+// Bound by launch, first copies and the end (3.7 us for the least product), then by the codes on their way: 1 row 1500 -> 6000: 5.1 us
+// (1.4 for 9 MB); 64 rows 9216 -> 4096: 12.5 us (5.9); 128 rows 4096^2: 11.0 us. All shared memory for the ring where the
+// CTAs are no more than SMs, since what is under way hides the latency (64 rows 9216 -> 4096 with half of it: 15.4 us).
 template <class T, bool TRANS>
 __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ ProjectionParams P)
 {
@@ -389,6 +393,10 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
 // of a CTA by itself. The first CTA of the pair issues the products. Persistent: two accumulators in tensor memory take
 // turns, so that a tile is written out while the next one is multiplied. SPLIT: the pairs of a cluster share one
 // tile's depth instead, as in the kernel above.
+// Bound by the tensor core (86 % of its cycles at 6011 rows 9216 -> 4096) and by what the tiles take from L2, 30 KB for a group:
+// 154 us, 2.95 PFLOP/s, back to back; 8192 rows 4096^2 backward 96 us, 2.87 PFLOP/s. (The products alone, with no copies, take 3.7 PFLOP/s;
+// 5 to 7 stages and any L2 promotion are alike.) 700 rows 1500 <- 33278: 48.5 us with rows of codes 1504 bytes apart, 39 with 1536:
+// a 128-byte piece of a row that starts anywhere is two lines.
 constexpr int PP_OUT_WARPS = 8;         // warps that write results: two for each 32 lanes of tensor memory, in turn
 constexpr int PP_THREADS = 128 + 32 * PP_OUT_WARPS;
 constexpr int PP_TILE = 224;            // most rows of a tile: two accumulators and the scales fill tensor memory
