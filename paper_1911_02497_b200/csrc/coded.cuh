@@ -149,6 +149,75 @@ __device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
     return e;
 }
 
+// The same in two steps, so that several loads can be under way: ask8() loads, take8() makes the eight values of it. Of rows that begin
+// anywhere the aligned pieces are loaded that hold the values; they may reach into the neighbouring rows, or between them, but not out of
+// the matrix (`off`: where the row begins in it, `total`: where it ends). NOW: the eight at once, where registers are too few for the
+// pieces; 32-bit values, whose pieces are three, always so.
+template <class T>
+struct Pieces {
+    static constexpr int V = 8, N = 2;                  // values of a piece, pieces
+    uint4 p[N];
+};
+template <int A, class T, bool NOW> using Asked = typename std::conditional<A == 1 && sizeof(T) == 2 && !NOW, Pieces<T>, Eight<T>>::type;
+
+template <int A, bool NOW = false, class T>
+__device__ __forceinline__ Asked<A, T, NOW> ask8(const T *base, long long off, long long total, int c, int cols)
+{
+    if constexpr (A != 1 || sizeof(T) == 4 || NOW) {
+        return load8<A>(base + off, c, cols);
+    } else {
+        typedef Pieces<T> P;
+        P a;
+        const long long at = off + c;
+        const int by = (int)(reinterpret_cast<uintptr_t>(base + at) % 16 / sizeof(T)), n = by ? P::N : P::N - 1;
+        const long long start = at - by;
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) a.p[i] = make_uint4(0, 0, 0, 0);
+        if (c < cols) {
+            if (start >= 0 && start + n * P::V <= total) {
+                const uint4 *s = reinterpret_cast<const uint4 *>(base + start);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i)
+                    if (i < n) a.p[i] = s[i];
+            } else {                    // the first and the last pieces of the matrix
+                T *v = reinterpret_cast<T *>(a.p);
+#pragma unroll
+                for (int i = 0; i < P::N * P::V; ++i)
+                    if (start + i >= 0 && start + i < total) v[i] = base[start + i];
+            }
+        }
+        return a;
+    }
+}
+template <int A, bool NOW = false, class T>
+__device__ __forceinline__ Eight<T> take8(const Asked<A, T, NOW> &a, const T *base, long long off, int c, int cols)
+{
+    if constexpr (A != 1 || sizeof(T) == 4 || NOW) {
+        return a;
+    } else {
+        typedef Pieces<T> P;
+        u32 w[4 * P::N];
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) {
+            w[4 * i] = a.p[i].x;
+            w[4 * i + 1] = a.p[i].y;
+            w[4 * i + 2] = a.p[i].z;
+            w[4 * i + 3] = a.p[i].w;
+        }
+        shift_words(w, (int)(reinterpret_cast<uintptr_t>(base + off + c) % 16 / sizeof(T)));
+        Eight<T> e;
+        u32 *d = reinterpret_cast<u32 *>(&e);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(e) / 4; ++i) d[i] = w[i];
+        if (c + 8 > cols) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i >= cols) e.v[i] = from_f32<T>(0.0f);
+        }
+        return e;
+    }
+}
+
 template <int A, class T>
 __device__ __forceinline__ void store8(T *row, int c, int cols, const Eight<T> &e)
 {

@@ -77,20 +77,22 @@ __device__ __forceinline__ void load_gain(const void *gain, int f32, int c, int 
     }
 }
 
+template <class T>
+__device__ __forceinline__ void add_rounded(Eight<T> &h, const Eight<T> &r)
+{
+    float a[8], b[8];
+    widen(h, a);
+    widen(r, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] += b[i];
+    h = rounded<T>(a);
+}
 // h of columns c .. c+7: x, or the rounded sum of x and the residual.
 template <class T, int A>
 __device__ __forceinline__ Eight<T> load_h(const NormParams &P, long long row, int c)
 {
     Eight<T> h = load8<A>((const T *)P.x + row * P.ldx, c, P.cols);
-    if (P.residual) {
-        const Eight<T> r = load8<A>((const T *)P.residual + row * P.ldr, c, P.cols);
-        float a[8], b[8];
-        widen(h, a);
-        widen(r, b);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] += b[i];
-        h = rounded<T>(a);
-    }
+    if (P.residual) add_rounded(h, load8<A>((const T *)P.residual + row * P.ldr, c, P.cols));
     return h;
 }
 
@@ -133,10 +135,20 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
     const long long row = ROWS == 1 ? blockIdx.x : (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
     if (row >= P.rows) return;                          // (whole rows of threads: no barrier misses them)
     const int t = ROWS == 1 ? threadIdx.x : threadIdx.x % TPR;
+    const long long ox = row * P.ldx, orr = row * P.ldr, last = P.rows - 1;
+    Asked<A, T, false> ax[NV], ar[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        ax[v] = ask8<A>((const T *)P.x, ox, last * P.ldx + P.cols, (v * TPR + t) * 8, P.cols);
+        if (P.residual) ar[v] = ask8<A>((const T *)P.residual, orr, last * P.ldr + P.cols, (v * TPR + t) * 8, P.cols);
+    }
     Eight<T> h[NV];
     float sum = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) h[v] = load_h<T, A>(P, row, (v * TPR + t) * 8);
+    for (int v = 0; v < NV; ++v) {
+        h[v] = take8<A>(ax[v], (const T *)P.x, ox, (v * TPR + t) * 8, P.cols);
+        if (P.residual) add_rounded(h[v], take8<A>(ar[v], (const T *)P.residual, orr, (v * TPR + t) * 8, P.cols));
+    }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         if (P.h) store8_warp<A>((T *)P.h + row * P.ldh, (v * TPR + t) * 8, P.cols, h[v], turn);
@@ -267,7 +279,8 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
     pdl_wait();
     pdl_launch_dependents();
     const int t = ROWS == 1 ? threadIdx.x : threadIdx.x % TPR, sub = ROWS == 1 ? 0 : threadIdx.x / TPR;
-    constexpr bool KEEP = TPR < 1024;                   // (a thread of 1024 has 64 registers: the gain is read again, from L1)
+    // where registers are short (a thread of 1024 has 64, and without a ring the next row's operands take them) the gain is read again, from L1
+    constexpr bool KEEP = TPR < 1024 && S > 0, AHEAD = S == 0 && TPR < 1024 && sizeof(T) == 2;
     float g[NV][8], acc[NV][8] = {};
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -296,8 +309,26 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
         if (S == 3) rstd_last = rstd_at(first + step);
     }
     int phase = 0, stage = 0;
+    // without a ring: the operands of a row, asked for ahead of the row before where registers allow it
+    constexpr bool NOW = TPR >= 1024;
+    Asked<A, T, NOW> asked[S == 0 ? NV : 1][3];
+    const long long last = P.rows - 1;
+    auto ask_row = [&](long long row) {
+        if constexpr (S == 0) {
+            if (row >= P.rows) return;
+            rstd_next = P.rstd[row];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * TPR + t) * 8;
+                asked[v][0] = ask8<A, NOW>((const T *)P.dy, row * P.ldy, last * P.ldy + P.cols, c, P.cols);
+                asked[v][1] = ask8<A, NOW>((const T *)P.h, row * P.ldh, last * P.ldh + P.cols, c, P.cols);
+                if (P.dh) asked[v][2] = ask8<A, NOW>((const T *)P.dh, row * P.ldd, last * P.ldd + P.cols, c, P.cols);
+            }
+        }
+    };
+    if (AHEAD) ask_row(first);
     for (long long row = first; row < P.rows; row += step, phase ^= 1) {
-        Eight<T> e[A == 1 ? NV : 1][3];
+        Eight<T> e[S == 0 ? NV : 1][3];
         auto take = [&](int o, int v) {
             if constexpr (S > 0) return *reinterpret_cast<const Eight<T> *>(place(stage, o, v));
             else return e[v][o];
@@ -309,14 +340,16 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
             ask(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
             asm volatile("cp.async.wait_group %0;" :: "n"(S > 0 ? S - 1 : 0) : "memory");
         } else {
-            rstd = P.rstd[row];
+            if (!AHEAD) ask_row(row);
+            rstd = rstd_next;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * TPR + t) * 8;
-                e[v][0] = load8<A>((const T *)P.dy + row * P.ldy, c, P.cols);
-                e[v][1] = load8<A>((const T *)P.h + row * P.ldh, c, P.cols);
-                if (P.dh) e[v][2] = load8<A>((const T *)P.dh + row * P.ldd, c, P.cols);
+                e[v][0] = take8<A, NOW>(asked[v][0], (const T *)P.dy, row * P.ldy, c, P.cols);
+                e[v][1] = take8<A, NOW>(asked[v][1], (const T *)P.h, row * P.ldh, c, P.cols);
+                if (P.dh) e[v][2] = take8<A, NOW>(asked[v][2], (const T *)P.dh, row * P.ldd, c, P.cols);
             }
+            if (AHEAD) ask_row(row + step);
         }
         float sum = 0.0f;
 #pragma unroll
@@ -478,7 +511,8 @@ __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__
     const u64 units = (u64)P.rows * P.runs, first = (u64)blockIdx.x * (HALVES * UNITS) + half;
     u64 row[UNITS];
     int c[UNITS];
-    Eight<T> e[UNITS][NG];
+    Asked<A, T, false> asked[UNITS][NG];
+    const long long total = (P.rows - 1) * P.ldx + P.cols;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
         const u64 u = first + i * HALVES;
@@ -496,9 +530,8 @@ __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__
             row[i] = r;
         }
         c[i] = u < units ? (int)g * (NG * GROUP) + lane * 8 : P.cols;    // (P.cols: nothing to read or write)
-        const T *x = (const T *)P.x + row[i] * P.ldx;
 #pragma unroll
-        for (int k = 0; k < NG; ++k) e[i][k] = load8<A>(x, c[i] + k * GROUP, P.cols);
+        for (int k = 0; k < NG; ++k) asked[i][k] = ask8<A>((const T *)P.x, row[i] * P.ldx, total, c[i] + k * GROUP, P.cols);
     }
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
@@ -506,9 +539,10 @@ __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
             const int at = c[i] + k * GROUP;
+            const Eight<T> e = take8<A>(asked[i][k], (const T *)P.x, row[i] * P.ldx, at, P.cols);
             float v[8];
-            widen(e[i][k], v);
-            float most = group_most(most_raw(e[i][k]), 0xFFFFFFFFu);
+            widen(e, v);
+            float most = group_most(most_raw(e), 0xFFFFFFFFu);
             if (is_odd(most)) {
                 most = group_most(most_finite(v), 0xFFFFu << (threadIdx.x & 16));
                 odd_to_nan(v);
@@ -536,12 +570,16 @@ __global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_consta
     const u32 bi = blockIdx.x / P.groups, bj = blockIdx.x - bi * P.groups;
     const int c = (int)bj * GROUP + threadIdx.x % GROUP_LANES * 8;
     const long long r0 = (long long)bi * GROUP + threadIdx.x / GROUP_LANES;
-    Eight<T> e[N];
+    Asked<A, T, false> asked[N];
+    const long long total = (P.rows - 1) * P.ldx + P.cols;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const long long r = r0 + i * STEP;
-        e[i] = load8<A>((const T *)P.x + r * P.ldx, r < P.rows ? c : P.cols, P.cols);
+        asked[i] = ask8<A>((const T *)P.x, r * P.ldx, total, r < P.rows ? c : P.cols, P.cols);
     }
+    Eight<T> e[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = take8<A>(asked[i], (const T *)P.x, (r0 + i * STEP) * P.ldx, c, P.cols);
     float most = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) most = most2(most, most_raw(e[i]));
