@@ -113,7 +113,7 @@ __device__ __forceinline__ void shift_words(u32 (&w)[12], int by)          // 32
 // number of columns that is a multiple of it), or one. It is fixed when compiling: a choice at every access made three to
 // four times as many instructions, and kept the loads of a thread from leaving together (128 x 128 blocks of bf16: 87 us).
 // Rows that begin anywhere (A = 1) are read by the aligned 16 bytes that hold the values, where those lie within the row, and
-// shifted; value by value the norm of 8000 x 2047 in bf16 took 79 us, not 22 as of 8000 x 2048.
+// shifted (value by value the norm of 8000 x 2047 in bf16 took 79 us, now 39; 25 for 8000 x 2048).
 template <int A, class T>
 __device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
 {
@@ -151,19 +151,18 @@ __device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
 
 // The same in two steps, so that several loads can be under way: ask8() loads, take8() makes the eight values of it. Of rows that begin
 // anywhere the aligned pieces are loaded that hold the values; they may reach into the neighbouring rows, or between them, but not out of
-// the matrix (`off`: where the row begins in it, `total`: where it ends). NOW: the eight at once, where registers are too few for the
-// pieces; 32-bit values, whose pieces are three, always so.
+// the matrix (`off`: where the row begins in it, `total`: where it ends). 32-bit values, which would take three pieces, come as eights at once.
 template <class T>
 struct Pieces {
     static constexpr int V = 8, N = 2;                  // values of a piece, pieces
     uint4 p[N];
 };
-template <int A, class T, bool NOW> using Asked = typename std::conditional<A == 1 && sizeof(T) == 2 && !NOW, Pieces<T>, Eight<T>>::type;
+template <int A, class T> using Asked = typename std::conditional<A == 1 && sizeof(T) == 2, Pieces<T>, Eight<T>>::type;
 
-template <int A, bool NOW = false, class T>
-__device__ __forceinline__ Asked<A, T, NOW> ask8(const T *base, long long off, long long total, int c, int cols)
+template <int A, class T>
+__device__ __forceinline__ Asked<A, T> ask8(const T *base, long long off, long long total, int c, int cols)
 {
-    if constexpr (A != 1 || sizeof(T) == 4 || NOW) {
+    if constexpr (A != 1 || sizeof(T) == 4) {
         return load8<A>(base + off, c, cols);
     } else {
         typedef Pieces<T> P;
@@ -189,10 +188,10 @@ __device__ __forceinline__ Asked<A, T, NOW> ask8(const T *base, long long off, l
         return a;
     }
 }
-template <int A, bool NOW = false, class T>
-__device__ __forceinline__ Eight<T> take8(const Asked<A, T, NOW> &a, const T *base, long long off, int c, int cols)
+template <int A, class T>
+__device__ __forceinline__ Eight<T> take8(const Asked<A, T> &a, const T *base, long long off, int c, int cols)
 {
-    if constexpr (A != 1 || sizeof(T) == 4 || NOW) {
+    if constexpr (A != 1 || sizeof(T) == 4) {
         return a;
     } else {
         typedef Pieces<T> P;

@@ -119,9 +119,9 @@ template <int TPR> struct RowThreads {
     static constexpr int BLOCK = TPR < 128 ? 128 : TPR, ROWS = BLOCK / TPR;
 };
 
-// Measured (bf16, residual): 8192 x 4096, 16- and 8-bit results 50 us (46 for the bytes); 8000 x 1500, 8-bit results 22 us (13); rows
-// that begin anywhere: 8000 x 2047 45 us (23). Bound by memory, and in the last two by instructions (issue slots 70 % taken). A ring of
-// rows copied ahead, as in the backward pass, took longer (60 us): many CTAs of one row each overlap by themselves.
+// Measured (bf16, residual): 8192 x 4096, 16- and 8-bit results 48 us (46 for the bytes); 8000 x 1500, 8-bit results 21 us (13); rows
+// that begin anywhere: 8000 x 2047 39 us (23). Bound by memory, and in the last two by instructions (issue slots 70 % taken). A ring of
+// rows copied ahead, as in the backward pass, took longer (60 us against 55 then): many CTAs of one row each overlap by themselves.
 template <class T, int A, int TPR, int NV>
 __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const __grid_constant__ NormParams P)
 {
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
     if (row >= P.rows) return;                          // (whole rows of threads: no barrier misses them)
     const int t = ROWS == 1 ? threadIdx.x : threadIdx.x % TPR;
     const long long ox = row * P.ldx, orr = row * P.ldr, last = P.rows - 1;
-    Asked<A, T, false> ax[NV], ar[NV];
+    Asked<A, T> ax[NV], ar[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         ax[v] = ask8<A>((const T *)P.x, ox, last * P.ldx + P.cols, (v * TPR + t) * 8, P.cols);
@@ -232,26 +232,28 @@ __device__ __forceinline__ void norm_back_out(const NormBackParams &P, long long
     }
 }
 
-// Operands on their way: every thread copies the eights that it will use itself into a ring of rows in shared memory
-// (cp.async), so what is in flight does not go by registers, nothing waits for other threads' copies, and the operands are read from
-// there twice instead of being kept across the row's sum. With loads into registers, a row at a time: 91 us for 8192 x 4096 in
-// bf16, against 46 for the bytes.
+// Operands on their way: the threads of a row copy it into a ring of rows in shared memory (cp.async), so what is in flight does not go by
+// registers, and the operands are read from there twice instead of being kept across the row's sum. With loads into registers,
+// a row at a time: 91 us for 8192 x 4096 in bf16, against 46 for the bytes. A thread copies the eights that it will use itself, and nobody
+// waits for anybody's copies. Where rows begin anywhere (A = 1) it copies the aligned 16 bytes in which its eight begins, one piece more
+// ends the row, the row's threads meet, and an eight is shifted together from its pieces (8000 x 2047: 54 us, value by value 155).
 template <class T, int A, int TPR, int NV> struct BackRing {
-    static constexpr int BLOCK = RowThreads<TPR>::BLOCK, EIGHT = 8 * sizeof(T);
-    static constexpr int ROW = 3 * NV * BLOCK * EIGHT;                 // bytes of a stage: dy, h, dh
-    static constexpr int STAGES = A == 1 ? 0 : 3 * ROW <= 75 * 1024 ? 3 : 2;
-    static constexpr int SMEM = STAGES * ROW;
-    static constexpr int FIT = SMEM ? 226 * 1024 / (SMEM + 1024) : 8, THREADS_SM = A == 1 ? 512 : 768, WANT = THREADS_SM / BLOCK > 0 ? THREADS_SM / BLOCK : 1;
+    static constexpr int BLOCK = RowThreads<TPR>::BLOCK, ROWS = RowThreads<TPR>::ROWS, EIGHT = 8 * sizeof(T);
+    static constexpr int ROOM = NV * TPR * EIGHT + (A == 1 ? 16 : 0);  // bytes of a row's operand
+    static constexpr int STAGE = 3 * ROWS * ROOM;                      // dy, h, dh
+    static constexpr int STAGES = 3 * STAGE <= 75 * 1024 ? 3 : 2;
+    static constexpr int SMEM = STAGES * STAGE;
+    static constexpr int FIT = 226 * 1024 / (SMEM + (A == 1 ? BLOCK * EIGHT : 0) + 2048), WANT = 768 / BLOCK > 0 ? 768 / BLOCK : 1;
     static constexpr int CTAS = FIT < WANT ? FIT : WANT;               // of an SM
     static_assert(SMEM <= 226 * 1024 && CTAS >= 1, "shared memory");
 };
 
-// `n` of 16 (or 8) bytes: past the end of a row, zeros
+// The first `bytes` of 16 (or 8); zeros behind them.
 template <int BYTES>
-__device__ __forceinline__ void copy_async(u32 dst, const void *src, bool there)
+__device__ __forceinline__ void copy_async(u32 dst, const void *src, int bytes)
 {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" :: "r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 template <int A, class T>
 __device__ __forceinline__ void copy8(u32 dst, const T *row, int c, int cols)
@@ -260,18 +262,63 @@ __device__ __forceinline__ void copy8(u32 dst, const T *row, int c, int cols)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const bool there = c + i * EACH < cols;
-        copy_async<BYTES>(dst + i * BYTES, there ? row + c + i * EACH : row, there);
+        copy_async<BYTES>(dst + i * BYTES, there ? row + c + i * EACH : row, there ? BYTES : 0);
     }
+}
+// Values that `row` begins behind an aligned 16 bytes.
+template <class T> __device__ __forceinline__ int begins_by(const T *row) { return (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)); }
+// Piece i of a row that begins anywhere: the aligned 16 bytes that hold its values from i * V - by on. A piece may reach into the
+// neighbouring rows, but not out of the matrix (`off`: where the row begins in it, `total`: where it ends).
+template <class T>
+__device__ __forceinline__ void copy_piece(char *dst, const T *base, long long off, long long total, int i, int cols)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    const int by = begins_by(base + off), first = i * V - by;
+    if (first >= cols) return;
+    const long long start = off + first;
+    if (start >= 0) {
+        copy_async<16>((u32)__cvta_generic_to_shared(dst), base + start, (int)min((long long)V, total - start) * (int)sizeof(T));
+    } else {                            // the matrix begins within this piece
+        for (int j = 0; j < V; ++j)
+            if (start + j >= 0 && start + j < total) reinterpret_cast<T *>(dst)[j] = base[start + j];
+    }
+}
+// The eight at columns c .. c+7 of such a row, whose pieces lie at `room`; zero past its end.
+template <class T>
+__device__ __forceinline__ Eight<T> from_pieces(const char *room, int by, int c, int cols)
+{
+    constexpr int W = (int)sizeof(T) * 2;               // words of an eight
+    u32 w[W + 4];
+    const uint4 *p = reinterpret_cast<const uint4 *>(room + c * (int)sizeof(T));
+#pragma unroll
+    for (int i = 0; i < W / 4 + 1; ++i) {
+        const uint4 x = p[i];
+        w[4 * i] = x.x;
+        w[4 * i + 1] = x.y;
+        w[4 * i + 2] = x.z;
+        w[4 * i + 3] = x.w;
+    }
+    shift_words(w, by);
+    Eight<T> e;
+    u32 *d = reinterpret_cast<u32 *>(&e);
+#pragma unroll
+    for (int i = 0; i < W; ++i) d[i] = w[i];
+    if (c + 8 > cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i >= cols) e.v[i] = from_f32<T>(0.0f);
+    }
+    return e;
 }
 
 // A CTA takes every gridDim-th row (group of rows), so that a thread's sums for dgain stay in its registers; they leave
-// once, as one of the slots that k_norm_dgain adds up. Measured with it: 8192 x 4096 bf16, dh and codes, 57 us (46 for the bytes), bound by
-// memory (59 % of its nominal rate) and instructions (67 % of the issue slots); 8000 x 2047 97 us, loads into registers.
+// once, as one of the slots that k_norm_dgain adds up. Measured with it: 8192 x 4096 bf16, dh and codes, 55 us (46 for the bytes), bound by
+// memory (59 % of its nominal rate) and instructions (67 % of the issue slots); 8192 x 1500 28 us (15).
 template <class T, int A, int TPR, int NV>
 __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV>::CTAS) k_norm_backward(const __grid_constant__ NormBackParams P)
 {
     using R = BackRing<T, A, TPR, NV>;
-    constexpr int ROWS = RowThreads<TPR>::ROWS, BLOCK = R::BLOCK, S = R::STAGES;
+    constexpr int ROWS = R::ROWS, BLOCK = R::BLOCK, S = R::STAGES;
     extern __shared__ __align__(16) char nb_ring[];
     __shared__ float slots[2][32];
     __shared__ Eight<T> s_turns[Turns<A, T, BLOCK>::N];
@@ -279,85 +326,69 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
     pdl_wait();
     pdl_launch_dependents();
     const int t = ROWS == 1 ? threadIdx.x : threadIdx.x % TPR, sub = ROWS == 1 ? 0 : threadIdx.x / TPR;
-    // where registers are short (a thread of 1024 has 64, and without a ring the next row's operands take them) the gain is read again, from L1
-    constexpr bool KEEP = TPR < 1024 && S > 0, AHEAD = S == 0 && TPR < 1024 && sizeof(T) == 2;
+    constexpr bool KEEP = TPR < 1024;                   // (a thread of 1024 has 64 registers: the gain is read again, from L1)
     float g[NV][8], acc[NV][8] = {};
 #pragma unroll
     for (int v = 0; v < NV; ++v)
         if (KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
-    const long long first = (long long)blockIdx.x * ROWS + sub, step = (long long)gridDim.x * ROWS;
-    // this thread's place of operand o (0: dy, 1: h, 2: dh), eight v, in a stage
-    auto place = [&](int stage, int o, int v) { return nb_ring + (((stage * 3 + o) * NV + v) * BLOCK + (int)threadIdx.x) * R::EIGHT; };
-    auto ask = [&](long long row, int stage) {
-        if (row < P.rows) {
+    const long long first = (long long)blockIdx.x * ROWS + sub, step = (long long)gridDim.x * ROWS, last = P.rows - 1;
+    // operand o (0: dy, 1: h, 2: dh) of this thread's row in a stage
+    auto room = [&](int stage, int o) { return nb_ring + ((stage * 3 + o) * ROWS + sub) * R::ROOM; };
+    auto copy = [&](int stage, int o, const T *base, long long ld, long long row) {
+        if constexpr (A == 1) {
+            constexpr int V = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < NV * 8 / V; ++i) {
+                const int piece = i * TPR + t;
+                copy_piece(room(stage, o) + piece * 16, base, row * ld, last * ld + P.cols, piece, P.cols);
+            }
+            if (t == 0) copy_piece(room(stage, o) + NV * 8 / V * TPR * 16, base, row * ld, last * ld + P.cols, NV * 8 / V * TPR, P.cols);
+        } else {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * TPR + t) * 8;
-                copy8<A>((u32)__cvta_generic_to_shared(place(stage, 0, v)), (const T *)P.dy + row * P.ldy, c, P.cols);
-                copy8<A>((u32)__cvta_generic_to_shared(place(stage, 1, v)), (const T *)P.h + row * P.ldh, c, P.cols);
-                if (P.dh) copy8<A>((u32)__cvta_generic_to_shared(place(stage, 2, v)), (const T *)P.dh + row * P.ldd, c, P.cols);
+                copy8<A>((u32)__cvta_generic_to_shared(room(stage, o) + c * (int)sizeof(T)), base + row * ld, c, P.cols);
             }
+        }
+    };
+    auto ask = [&](long long row, int stage) {
+        if (row < P.rows) {
+            copy(stage, 0, (const T *)P.dy, P.ldy, row);
+            copy(stage, 1, (const T *)P.h, P.ldh, row);
+            if (P.dh) copy(stage, 2, (const T *)P.dh, P.ldd, row);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    float rstd = 0.0f, rstd_next = 0.0f, rstd_last = 0.0f;
+    float rstd_next = 0.0f, rstd_last = 0.0f;
     auto rstd_at = [&](long long row) { return row < P.rows ? P.rstd[row] : 0.0f; };
-    if constexpr (S > 0) {
 #pragma unroll
-        for (int i = 0; i < S - 1; ++i) ask(first + i * step, i);
-        rstd_next = rstd_at(first);
-        if (S == 3) rstd_last = rstd_at(first + step);
-    }
+    for (int i = 0; i < S - 1; ++i) ask(first + i * step, i);
+    rstd_next = rstd_at(first);
+    if (S == 3) rstd_last = rstd_at(first + step);
     int phase = 0, stage = 0;
-    // without a ring: the operands of a row, asked for ahead of the row before where registers allow it
-    constexpr bool NOW = TPR >= 1024;
-    Asked<A, T, NOW> asked[S == 0 ? NV : 1][3];
-    const long long last = P.rows - 1;
-    auto ask_row = [&](long long row) {
-        if constexpr (S == 0) {
-            if (row >= P.rows) return;
-            rstd_next = P.rstd[row];
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * TPR + t) * 8;
-                asked[v][0] = ask8<A, NOW>((const T *)P.dy, row * P.ldy, last * P.ldy + P.cols, c, P.cols);
-                asked[v][1] = ask8<A, NOW>((const T *)P.h, row * P.ldh, last * P.ldh + P.cols, c, P.cols);
-                if (P.dh) asked[v][2] = ask8<A, NOW>((const T *)P.dh, row * P.ldd, last * P.ldd + P.cols, c, P.cols);
-            }
-        }
-    };
-    if (AHEAD) ask_row(first);
     for (long long row = first; row < P.rows; row += step, phase ^= 1) {
-        Eight<T> e[S == 0 ? NV : 1][3];
-        auto take = [&](int o, int v) {
-            if constexpr (S > 0) return *reinterpret_cast<const Eight<T> *>(place(stage, o, v));
-            else return e[v][o];
-        };
-        if constexpr (S > 0) {
-            rstd = rstd_next;
-            rstd_next = S == 3 ? rstd_last : rstd_at(row + step);
-            if (S == 3) rstd_last = rstd_at(row + 2 * step);
-            ask(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
-            asm volatile("cp.async.wait_group %0;" :: "n"(S > 0 ? S - 1 : 0) : "memory");
-        } else {
-            if (!AHEAD) ask_row(row);
-            rstd = rstd_next;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * TPR + t) * 8;
-                e[v][0] = take8<A, NOW>(asked[v][0], (const T *)P.dy, row * P.ldy, c, P.cols);
-                e[v][1] = take8<A, NOW>(asked[v][1], (const T *)P.h, row * P.ldh, c, P.cols);
-                if (P.dh) e[v][2] = take8<A, NOW>(asked[v][2], (const T *)P.dh, row * P.ldd, c, P.cols);
-            }
-            if (AHEAD) ask_row(row + step);
+        const float rstd = rstd_next;
+        rstd_next = S == 3 ? rstd_last : rstd_at(row + step);
+        if (S == 3) rstd_last = rstd_at(row + 2 * step);
+        // the row is here; where its threads share their copies they meet, which also says that the stage before has been read
+        asm volatile("cp.async.wait_group %0;" :: "n"(S - 2) : "memory");
+        if constexpr (A == 1) {
+            if (TPR == 32) __syncwarp();
+            else __syncthreads();
         }
+        ask(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
+        auto take = [&](int o, int v, const void *base, long long ld) {
+            const int c = (v * TPR + t) * 8;
+            if constexpr (A == 1) return from_pieces<T>(room(stage, o), begins_by((const T *)base + row * ld), c, P.cols);
+            else return *reinterpret_cast<const Eight<T> *>(room(stage, o) + c * (int)sizeof(T));
+        };
         float sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             if (!KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
             float dy[8], h[8];
-            widen(take(0, v), dy);
-            widen(take(1, v), h);
+            widen(take(0, v, P.dy, P.ldy), dy);
+            widen(take(1, v, P.h, P.ldh), h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float p = dy[i] * (h[i] * rstd);
@@ -370,14 +401,14 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK, BackRing<T, A, TPR, NV
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 if (!KEEP) load_gain<T, A>(P.gain, P.gain_f32, (v * TPR + t) * 8, P.cols, g[v]);
-                Eight<T> dy = take(0, v), h = take(1, v), dh;
-                if (P.dh) dh = take(2, v);
+                Eight<T> dy = take(0, v, P.dy, P.ldy), h = take(1, v, P.h, P.ldh), dh;
+                if (P.dh) dh = take(2, v, P.dh, P.ldd);
                 hold(dy);
                 hold(h);
                 norm_back_out<T, A>(P, row, (v * TPR + t) * 8, dy, h, dh, g[v], rstd, q, turn);
             }
         }
-        if (S > 0) stage = stage + 1 == S ? 0 : stage + 1;
+        stage = stage + 1 == S ? 0 : stage + 1;
     }
     if (!P.part) return;
     float *part = P.part + ((long long)blockIdx.x * ROWS + sub) * P.ld_part;
@@ -511,7 +542,7 @@ __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__
     const u64 units = (u64)P.rows * P.runs, first = (u64)blockIdx.x * (HALVES * UNITS) + half;
     u64 row[UNITS];
     int c[UNITS];
-    Asked<A, T, false> asked[UNITS][NG];
+    Asked<A, T> asked[UNITS][NG];
     const long long total = (P.rows - 1) * P.ldx + P.cols;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
@@ -570,7 +601,7 @@ __global__ void __launch_bounds__(ENC_BLOCK) k_encode_blocks(const __grid_consta
     const u32 bi = blockIdx.x / P.groups, bj = blockIdx.x - bi * P.groups;
     const int c = (int)bj * GROUP + threadIdx.x % GROUP_LANES * 8;
     const long long r0 = (long long)bi * GROUP + threadIdx.x / GROUP_LANES;
-    Asked<A, T, false> asked[N];
+    Asked<A, T> asked[N];
     const long long total = (P.rows - 1) * P.ldx + P.cols;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
