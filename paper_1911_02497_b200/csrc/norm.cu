@@ -19,7 +19,7 @@ int forward(condensa_ctx *ctx, const condensa_norm *p, cudaStream_t stream)
         return fail(ctx, CONDENSA_ERR_UNSUPPORTED, "gain_dtype must be CONDENSA_DTYPE_FP32 or dtype");
     if (p->reserved) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "reserved must be 0");
     if (!(p->eps > 0.0f) || !std::isfinite(p->eps)) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "eps must be positive and finite");
-    OpArgs a{ctx};
+    OpArgs a(ctx);
     int rc = a.sizes(p->rows, p->cols);
     if (rc || p->rows == 0) return rc;
     const int e = op_type_bytes(p->dtype), ge = op_type_bytes(p->gain_dtype);
@@ -77,7 +77,7 @@ int backward(condensa_ctx *ctx, const condensa_norm_gradient *p, cudaStream_t st
     if (p->gain && p->gain_dtype != CONDENSA_DTYPE_FP32 && p->gain_dtype != p->dtype)
         return fail(ctx, CONDENSA_ERR_UNSUPPORTED, "gain_dtype must be CONDENSA_DTYPE_FP32 or dtype");
     if (p->reserved) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "reserved must be 0");
-    OpArgs a{ctx};
+    OpArgs a(ctx);
     int rc = a.sizes(p->rows, p->cols);
     if (rc) return rc;
     const int e = op_type_bytes(p->dtype), ge = op_type_bytes(p->gain_dtype);
@@ -153,7 +153,7 @@ int encode_rows(condensa_ctx *ctx, const void *x, long long ldx, long long rows,
 {
     if (!out) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "out is NULL");
     if (!op_known_type(dtype)) return fail(ctx, CONDENSA_ERR_UNSUPPORTED, "dtype must be CONDENSA_DTYPE_FP32, _FP16 or _BF16");
-    OpArgs a{ctx};
+    OpArgs a(ctx);
     int rc = a.sizes(rows, cols);
     if (rc || rows == 0) return rc;
     const int e = op_type_bytes(dtype);
@@ -185,7 +185,7 @@ int encode_blocks(condensa_ctx *ctx, const void *w, long long ldw, long long n, 
     if (!op_known_type(dtype)) return fail(ctx, CONDENSA_ERR_UNSUPPORTED, "dtype must be CONDENSA_DTYPE_FP32, _FP16 or _BF16");
     if (n < 1 || k < 1) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "n and k must be positive");
     if (n > OP_MAX_WIDTH || k > OP_MAX_WIDTH) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "n and k must not exceed 2^22");
-    OpArgs a{ctx};
+    OpArgs a(ctx);
     const int e = op_type_bytes(dtype);
     int rc = a.matrix("w", w, ldw, n, k, e, false);
     if (rc) return rc;

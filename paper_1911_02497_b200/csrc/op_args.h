@@ -13,6 +13,11 @@ struct OpArgs {
     std::vector<Interval> iv;
     std::vector<RowRange> rows;
 
+    explicit OpArgs(condensa_ctx *c) : ctx(c)
+    {
+        iv.reserve(4);
+        rows.reserve(8);
+    }
     int matrix(const char *name, const void *p, long long ld, long long n, long long width, int e, bool out)
     {
         if (!p) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "%s is NULL", name);

@@ -150,8 +150,8 @@ int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups,
         }
     }
     before = 0;
-    for (int most = PP_TILE; rows > 64 && most >= 64; most -= 32) {
-        const int tile = cut(most, 32);
+    for (int most = PP_TILE; rows > 64 && most >= 64; most -= 16) {
+        const int tile = cut(most, 16);
         if (tile == before) continue;
         before = tile;
         const long long tiles = (rows + tile - 1) / tile * ((width + 2 * PJ_WIDE - 1) / (2 * PJ_WIDE));
@@ -177,7 +177,7 @@ int run(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x
     if (w->n < 1 || w->k < 1) return fail(ctx, CONDENSA_ERR_INVALID_ARG, "n and k must be positive");
     if (w->n > OP_MAX_WIDTH || w->k > OP_MAX_WIDTH) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "n and k must not exceed 2^22");
     const long long depth = trans ? w->n : w->k, width = trans ? w->k : w->n;
-    OpArgs a{ctx};
+    OpArgs a(ctx);
     int rc = a.sizes(rows, depth);
     if (rc || rows == 0) return rc;
     if ((rc = a.coded("w", w->code, w->n, w->k, GROUP, false)) != 0) return rc;

@@ -659,7 +659,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
             const int col0 = (int)(t % (u32)P.blocks * 2 + side) * PJ_WIDE + w * 32;
             const int rows = (int)min(P.rows - row0, (long long)P.tile);
 #pragma unroll 1
-            for (int c = turns * 32; c < P.tile; c += PP_OUT_WARPS / 4 * 32) {
+            for (int c = turns * 32; c < P.tile; c += PP_OUT_WARPS / 4 * 32) {          // (the last may be a half: what is behind it is read, not used)
                 float v[32];
                 tmem_ld(at + (u32)c, v);
                 tmem_ld_wait(v);
@@ -670,7 +670,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
                 if constexpr (SPLIT) {
                     float *sums = reinterpret_cast<float *>(ring);          // [row][128 output columns]
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) sums[(c + i) * PJ_WIDE + w * 32 + lane] = v[i];
+                    for (int i = 0; i < 32; ++i)
+                        if (i < 16 || c + 16 < P.tile) sums[(c + i) * PJ_WIDE + w * 32 + lane] = v[i];
                 } else if (c < rows) {
                     T *out = (T *)P.out + (row0 + c) * P.ldo;
                     if (P.access == 8) write_block<8>(v, turn, out, P.ldo, rows - c, col0, P.width, lane);

@@ -447,9 +447,10 @@ class Coded:
         self.codes, self.scales, self.high, self.device = codes, scales, high, codes.get_device()
         self.struct = CodedMatrix(codes.data_ptr(), scales.data_ptr(), ld, ld_scales)
         self.projection = Projection(self.struct, self.rows, self.cols) if high > 1 else None
+        self.ref = C.byref(self.struct if high == 1 else self.projection)       # what the library's calls take
 
 
-_REAL = (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16)
+_REAL, _HALF = (DTYPE_FP32, DTYPE_FP16, DTYPE_BF16), (DTYPE_FP16, DTYPE_BF16)
 _NO_CODE = CodedMatrix()
 
 
@@ -657,11 +658,12 @@ class Context:
         return x.data_ptr(), (ld if rows > 1 else max(cols, ld))
 
     def _coded(self, code, rows: int, cols: int, high: int, name: str) -> Coded:
-        if not isinstance(code, Coded) or code.high != high:
+        if code.__class__ is not Coded or code.high != high:
             raise TypeError("%s must be made by %s" % (name, "coded_rows" if high == 1 else "coded_blocks"))
-        if (code.rows, code.cols) != (rows, cols):
+        if code.rows != rows or code.cols != cols:
             raise ValueError("%s has shape %s, not %s" % (name, (code.rows, code.cols), (rows, cols)))
-        self._here(code.device, name)
+        if code.device != self.device:
+            self._here(code.device, name)
         return code
 
     def _vector(self, x, n: int, name: str):
@@ -669,9 +671,10 @@ class Context:
         if x is None:
             return None
         _dtype_code(x, (DTYPE_FP32,), name)
-        if tuple(x.shape) != (n,) or not _contiguous(x):
+        if x.shape != (n,) or not x.is_contiguous():
             raise ValueError("%s must be contiguous and hold %d elements" % (name, n))
-        self._here(x.get_device(), name)
+        if x.get_device() != self.device:
+            self._here(x.get_device(), name)
         return x.data_ptr()
 
     def _gain(self, gain, cols: int, dtype: int):
@@ -679,9 +682,10 @@ class Context:
         if gain is None:
             return None, DTYPE_FP32
         code = _dtype_code(gain, (DTYPE_FP32, dtype), "gain")
-        if tuple(gain.shape) != (cols,) or not _contiguous(gain):
+        if gain.shape != (cols,) or not gain.is_contiguous():
             raise ValueError("gain must be contiguous and hold %d elements" % cols)
-        self._here(gain.get_device(), "gain")
+        if gain.get_device() != self.device:
+            self._here(gain.get_device(), "gain")
         return gain.data_ptr(), code
 
     def encode_rows(self, x, out: Coded, stream=None):
@@ -690,7 +694,7 @@ class Context:
         code = _dtype_code(x, _REAL, "x")
         p, ld = self._matrix(x, shape, x.dtype, "x")
         out = self._coded(out, rows, cols, 1, "out")
-        self._check(self._lib.condensa_encode_rows(self._h, p, ld, rows, cols, code, C.byref(out.struct), _stream_handle(stream)))
+        self._check(self._lib.condensa_encode_rows(self._h, p, ld, rows, cols, code, out.ref, _stream_handle(stream)))
 
     def encode_blocks(self, w, out: Coded, theta=None, stream=None):
         """``w`` [n, k] (float32, float16, bfloat16) into ``out``, a scale for every 128 x 128; ``theta`` (float32, may be ``w`` itself, or None)
@@ -706,19 +710,21 @@ class Context:
         self._check(self._lib.condensa_encode_blocks(self._h, p, ld, n, k, code, C.byref(out.struct), pt, ldt, _stream_handle(stream)))
 
     def _product(self, call, w: Coded, x: Coded, y, depth: int, width: int, names, stream):
-        w = self._coded(w, w.rows, w.cols, CODE_GROUP, "w")
-        rows = x.rows
-        x = self._coded(x, rows, depth, 1, names[0])
-        code = _dtype_code(y, (DTYPE_FP16, DTYPE_BF16), names[1])
-        p, ld = self._matrix(y, (rows, width), y.dtype, names[1])
-        self._check(call(self._h, C.byref(w.projection), C.byref(x.struct), rows, p, ld, code, _stream_handle(stream)))
+        x = self._coded(x, x.rows, depth, 1, names[0])
+        code = _dtype_code(y, _HALF, names[1])
+        p, ld = self._matrix(y, (x.rows, width), y.dtype, names[1])
+        rc = call(self._h, w.ref, x.ref, x.rows, p, ld, code, _stream_handle(stream))
+        if rc:
+            self._check(rc)
 
     def projection_forward(self, w: Coded, x: Coded, y, stream=None):
         """``y = x w^T``: ``w`` [n, k] by :func:`coded_blocks`, ``x`` [rows, k] by :func:`coded_rows`, ``y`` [rows, n] float16 or bfloat16."""
+        w = self._coded(w, w.rows, w.cols, CODE_GROUP, "w")
         self._product(self._lib.condensa_projection_forward, w, x, y, w.cols, w.rows, ("x", "y"), stream)
 
     def projection_backward(self, w: Coded, dy: Coded, dx, stream=None):
         """``dx = dy w``, the gradient that reaches the rows: ``dy`` [rows, n] by :func:`coded_rows`, ``dx`` [rows, k] float16 or bfloat16."""
+        w = self._coded(w, w.rows, w.cols, CODE_GROUP, "w")
         self._product(self._lib.condensa_projection_backward, w, dy, dx, w.rows, w.cols, ("dy", "dx"), stream)
 
     def norm_forward(self, x, gain, eps=1e-5, residual=None, h=None, y=None, code: Optional[Coded] = None, rstd=None, stream=None):
