@@ -539,7 +539,8 @@ typedef struct {
 } condensa_norm_gradient;
 
 /* Outputs may overlap nothing else of the call but as said above ("itself": the same address and stride). forward uses no
- * workspace; backward does where dgain is formed: a captured call must not run while another call of the context runs. */
+ * workspace; backward does where dgain is formed: a captured call must not run while another call of the context runs. Calls may be
+ * captured into a CUDA graph after one plain call of the same shape. */
 CONDENSA_API int condensa_norm_forward(condensa_ctx *ctx, const condensa_norm *norm, void *stream);
 CONDENSA_API int condensa_norm_backward(condensa_ctx *ctx, const condensa_norm_gradient *norm, void *stream);
 

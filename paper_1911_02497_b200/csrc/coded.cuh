@@ -217,9 +217,11 @@ __device__ __forceinline__ Eight<T> take8(const Asked<A, T> &a, const T *base, l
     }
 }
 
+// The other way; of rows that begin anywhere whole warps write (store8_warp).
 template <int A, class T>
 __device__ __forceinline__ void store8(T *row, int c, int cols, const Eight<T> &e)
 {
+    static_assert(A == 8 || A == 4, "access width");
     if constexpr (A == 8) {
         const uint4 *s = reinterpret_cast<const uint4 *>(&e);
         uint4 *d = reinterpret_cast<uint4 *>(row + c);
@@ -227,17 +229,13 @@ __device__ __forceinline__ void store8(T *row, int c, int cols, const Eight<T> &
 #pragma unroll
             for (int i = 0; i < (int)sizeof(e) / 16; ++i) d[i] = s[i];
         }
-    } else if constexpr (A == 4) {
+    } else {
         typedef typename Access<T>::Four Four;
         const Four *s = reinterpret_cast<const Four *>(&e);
         Four *d = reinterpret_cast<Four *>(row + c);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (c + 4 * i < cols) d[i] = s[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < cols) row[c + i] = e.v[i];
     }
 }
 

@@ -455,27 +455,27 @@ __device__ __forceinline__ void write_block(const float (&v)[32], u32 *turn, T *
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (i < rows) out[i * ldo + col0 + lane] = from_f32<T>(v[i]);
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) turn[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
-    __syncwarp();
-    const int i0 = lane / 4, n8 = lane % 4 * 8, first = (i0 & 1) * 4;      // (odd pairs read their halves the other way round: no bank conflicts)
-    T *row = out + (long long)(2 * i0) * ldo;
+        for (int i = 0; i < 16; ++i) turn[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
+        __syncwarp();
+        const int i0 = lane / 4, n8 = lane % 4 * 8, first = (i0 & 1) * 4;      // (odd pairs read their halves the other way round: no bank conflicts)
+        T *row = out + (long long)(2 * i0) * ldo;
 #pragma unroll
-    for (int r = 0; r < 2; ++r, row += 16 * ldo) {
-        const u32 *at = turn + (r * 8 + i0) * 32 + n8;
-        const uint4 x = *reinterpret_cast<const uint4 *>(at + first), y = *reinterpret_cast<const uint4 *>(at + (4 - first));
-        const uint4 a = first ? y : x, b = first ? x : y;
+        for (int r = 0; r < 2; ++r, row += 16 * ldo) {
+            const u32 *at = turn + (r * 8 + i0) * 32 + n8;
+            const uint4 x = *reinterpret_cast<const uint4 *>(at + first), y = *reinterpret_cast<const uint4 *>(at + (4 - first));
+            const uint4 a = first ? y : x, b = first ? x : y;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const u32 sel = h ? 0x7632u : 0x5410u;
-            Eight<T> e;
-            *reinterpret_cast<uint4 *>(&e) = make_uint4(__byte_perm(a.x, a.y, sel), __byte_perm(a.z, a.w, sel), __byte_perm(b.x, b.y, sel), __byte_perm(b.z, b.w, sel));
-            if (16 * r + 2 * i0 + h < rows) store8<A>(row + h * ldo, col0 + n8, width, e);
+            for (int h = 0; h < 2; ++h) {
+                const u32 sel = h ? 0x7632u : 0x5410u;
+                Eight<T> e;
+                *reinterpret_cast<uint4 *>(&e) = make_uint4(__byte_perm(a.x, a.y, sel), __byte_perm(a.z, a.w, sel), __byte_perm(b.x, b.y, sel), __byte_perm(b.z, b.w, sel));
+                if (16 * r + 2 * i0 + h < rows) store8<A>(row + h * ldo, col0 + n8, width, e);
+            }
         }
+        __syncwarp();
     }
-    __syncwarp();
 }
 
 template <class T, bool TRANS, bool SPLIT>

@@ -328,3 +328,45 @@ def test_refusals(ctx):
     assert ctx._lib.condensa_norm_forward(ctx._h, None, None) == bad and ctx._lib.condensa_norm_backward(ctx._h, None, None) == bad
     assert ctx._lib.condensa_norm_forward(None, None, None) == bad
     assert f.room.intact() and b.room.intact()
+
+
+@pytest.mark.parametrize("cols", [100, 1500, 20000])
+def test_one_buffer_in_several_places(ctx, cols):
+    """x as its own residual, with the sum and the result over it; one gradient as dy, dh and dx."""
+    f = Forward(5, cols, "bfloat16")
+    f.r = f.x
+    f.want_kept = f.want()
+    f.h = f.x
+    ctx.norm_forward(f.x, f.g, EPS, residual=f.x, h=f.x, y=f.y, code=f.code, rstd=f.rstd)
+    f.check()
+    b = Backward(5, cols, "bfloat16")
+    b.dh = b.dy
+    b.kept = b.want()
+    b.dx = b.dy
+    ctx.norm_backward(b.dy, b.h, b.g, b.rstd, dh=b.dy, dx=b.dy, code=b.code, dgain=b.dgain)
+    b.check()
+
+
+@pytest.mark.parametrize("cols,pad", [(99, 0), (99, 2), (1001, 0), (1001, 4), (5003, 1), (12345, 0)])
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+def test_rows_that_begin_anywhere(ctx, cols, pad, dtype):
+    """Every operand at another place within its 16 bytes; neighbouring rows full of NaN, which no row may take over."""
+    import torch
+    for off in range(0, 8, 3):
+        f = Forward(6, cols, dtype, dtype, pad=pad, off=off)
+        f.y = f.room.put(np.full((6, cols), 7.0), dtype, pad + 3, off + 1)
+        f.r = f.room.put(f64(f.r), dtype, pad + 1, off + 2)
+        f.x[2], f.r[2] = float("nan"), float("nan")
+        ctx.norm_forward(f.x, f.g, EPS, residual=f.r, h=f.h, y=f.y, code=f.code, rstd=f.rstd)
+        f.check()
+        b = Backward(6, cols, dtype, dtype, pad=pad, off=off)
+        b.dy = b.room.put(f64(b.dy), dtype, pad + 5, off + 3)
+        b.dh = b.room.put(f64(b.dh), dtype, pad, off + 1)
+        b.dy[3] = float("nan")
+        b.kept = b.want()
+        ctx.norm_backward(b.dy, b.h, b.g, b.rstd, dh=b.dh, dx=b.dx, code=b.code)
+        b.check(dgain_too=False)
+        b.dy[3] = 0.0
+        b.kept = b.want()
+        ctx.norm_backward(b.dy, b.h, b.g, b.rstd, dh=b.dh, dx=b.dx, code=b.code, dgain=b.dgain)
+        b.check()

@@ -234,3 +234,44 @@ def test_refusals(ctx):
         assert call(case, ld=20) == bad and call(case, y=case.y.data_ptr() + 1) == bad and call(case, ld=1 << 60) == large
     assert ctx.launch_count() == before and c.room.intact() and d.room.intact()
     assert ctx._lib.condensa_projection_forward(None, None, None, 0, None, 0, 0, None) == bad
+
+
+@pytest.mark.parametrize("rows", [9, 300])
+def test_one_matrix_as_both_operands(ctx, rows):
+    """Inputs may share memory: the codes of w's first rows as x, under scales of their own."""
+    from paper_1911_02497_b200 import cstep
+    c = Case(rows, 700, 400)
+    scales = fill(c.room.coded(rows, 700), np.random.RandomState(9)).scales
+    c.x = cstep.coded_rows(c.w.codes[:rows], scales)
+    c.run(ctx)
+    c.check()
+
+
+def test_contexts_of_two_threads(ctx):
+    """A context for each thread: calls at the same time, on streams of their own."""
+    import threading
+
+    import torch
+    from paper_1911_02497_b200 import cstep
+    cases = [Case(rows, 1500, 2000, seed=rows) for rows in (3, 700)]
+    for c in cases:
+        c.run(ctx)
+    torch.cuda.synchronize()
+    want, failed = [c.y.clone() for c in cases], []
+
+    def work(c, expected):
+        try:
+            own, stream = cstep.Context(0), torch.cuda.Stream()
+            for _ in range(50):
+                c.run(own, stream)
+            stream.synchronize()
+            if not torch.equal(c.y, expected):
+                failed.append("bits")
+            own.close()
+        except Exception as e:      # noqa: BLE001 - told by the test's own thread
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=a) for a in zip(cases, want)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not failed
