@@ -224,7 +224,7 @@ __device__ __forceinline__ void add_parts(const ProjectionParams &P, cooperative
 // each adds up a part of the tile's rows over all of them, in their order, by distributed shared memory. (Sending the sums to where they
 // are added, into room of their own, spared a barrier and took 1 to 7 us more.)
 // Four warps: copies, products, and two for the scales; then all take the sums.
-// Bound by launch, first copies and the end (3.7 us for the least product), then by the codes on their way: 1 row 1500 -> 6000: 5.1 us
+// Bound by launch, first copies and the end (3.9 us for 1 row 512 -> 512), then by the codes on their way: 1 row 1500 -> 6000: 5.1 us
 // (1.4 for 9 MB); 64 rows 9216 -> 4096: 12.5 us (5.9); 128 rows 4096^2: 11.0 us. All shared memory for the ring where the
 // CTAs are no more than SMs, since what is under way hides the latency (64 rows 9216 -> 4096 with half of it: 15.4 us).
 template <class T, bool TRANS>
