@@ -116,10 +116,10 @@ __device__ __forceinline__ void norm_out(const NormParams &P, long long row, int
 }
 
 template <int TPR> struct RowThreads {
-    static constexpr int BLOCK = TPR < 128 ? 128 : TPR, ROWS = BLOCK / TPR;
+    static constexpr int BLOCK = TPR == 32 ? 128 : TPR, ROWS = BLOCK / TPR;
 };
 
-// Measured (bf16, residual): 8192 x 4096, 16- and 8-bit results 48 us (46 for the bytes); 8000 x 1500, 8-bit results 21 us (13); rows
+// Measured (bf16, residual): 8192 x 4096, 16- and 8-bit results 48 us (46 for the bytes); 8000 x 1500, 8-bit results 19 us (13); rows
 // that begin anywhere: 8000 x 2047 39 us (23). Bound by memory, and in the last two by instructions (issue slots 70 % taken). A ring of
 // rows copied ahead, as in the backward pass, took longer (60 us against 55 then): many CTAs of one row each overlap by themselves.
 template <class T, int A, int TPR, int NV>

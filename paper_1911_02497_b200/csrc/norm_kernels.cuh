@@ -31,7 +31,9 @@ int forward_as(condensa_ctx *ctx, const NormParams &P, cudaStream_t stream)
     return op_launch(ctx, "k_norm_forward", k_norm_forward<T, A, TPR, NV>, dim3((unsigned)((P.rows + ROWS - 1) / ROWS)), RowThreads<TPR>::BLOCK, stream, P);
 }
 
-// The threads of a row: as many as hold it with one or two eights each.
+// The threads of a row: as many as hold it with one or two eights each. With steps of powers of two alone, where up to half of the threads
+// have nothing to do: 8000 x 1500 bf16 21 us instead of 19, 4000 x 6000 42 instead of 36; backward 4000 x 6000 56 instead of 43, 2000 x 9999
+// 127 instead of 85.
 template <class T, int A>
 int forward_of(condensa_ctx *ctx, const NormParams &P, cudaStream_t stream)
 {
@@ -41,9 +43,13 @@ int forward_of(condensa_ctx *ctx, const NormParams &P, cudaStream_t stream)
     return eights <= 32   ? forward_as<T, A, 32, 1>(ctx, P, stream)
          : eights <= 64   ? forward_as<T, A, 32, 2>(ctx, P, stream)
          : eights <= 128  ? forward_as<T, A, 128, 1>(ctx, P, stream)
+         : eights <= 192  ? forward_as<T, A, 96, 2>(ctx, P, stream)
          : eights <= 256  ? forward_as<T, A, 128, 2>(ctx, P, stream)
+         : eights <= 384  ? forward_as<T, A, 192, 2>(ctx, P, stream)
          : eights <= 512  ? forward_as<T, A, 256, 2>(ctx, P, stream)
+         : eights <= 768  ? forward_as<T, A, 384, 2>(ctx, P, stream)
          : eights <= 1024 ? forward_as<T, A, 512, 2>(ctx, P, stream)
+         : eights <= 1536 ? forward_as<T, A, 768, 2>(ctx, P, stream)
                           : forward_as<T, A, 1024, 2>(ctx, P, stream);
 }
 
@@ -79,13 +85,17 @@ int backward_of(condensa_ctx *ctx, const NormBackParams &P, NormBackPlan &plan, 
         if (rc || (!P.dx && !P.codes)) return rc;
         return op_launch(ctx, "k_norm_backward_long", k_norm_backward_long<T, A, LONG_TPR>, dim3((unsigned)P.rows), LONG_TPR, stream, P);
     }
-    if constexpr (sizeof(T) == 2)
-        if (eights > 1024) return backward_as<T, A, 1024, 2>(ctx, P, plan, run, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (eights > 1536) return backward_as<T, A, 1024, 2>(ctx, P, plan, run, stream);
+        if (eights > 1024) return backward_as<T, A, 768, 2>(ctx, P, plan, run, stream);
+    }
     return eights <= 32  ? backward_as<T, A, 32, 1>(ctx, P, plan, run, stream)
          : eights <= 64  ? backward_as<T, A, 32, 2>(ctx, P, plan, run, stream)
          : eights <= 128 ? backward_as<T, A, 128, 1>(ctx, P, plan, run, stream)
-         : eights <= 256 ? backward_as<T, A, 128, 2>(ctx, P, plan, run, stream)
+         : eights <= 256 ? backward_as<T, A, 128, 2>(ctx, P, plan, run, stream)      // (96 threads: 32 instead of 28 us for 8192 x 1500 in bf16)
+         : eights <= 384 ? backward_as<T, A, 192, 2>(ctx, P, plan, run, stream)
          : eights <= 512 ? backward_as<T, A, 256, 2>(ctx, P, plan, run, stream)
+         : eights <= 768 ? backward_as<T, A, 384, 2>(ctx, P, plan, run, stream)
                          : backward_as<T, A, 512, 2>(ctx, P, plan, run, stream);
 }
 
