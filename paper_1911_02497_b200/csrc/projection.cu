@@ -110,9 +110,9 @@ int resident_clusters(condensa_ctx *ctx, const Variant &v, int n, int &count)
 // what differs). A group of the depth costs a CTA by itself 150 ns and 0.6 for each row of the tile, one of a pair 100 and 1.1, and all
 // their codes pass L2 at 13 MB/us. Codes come from memory at 70 KB/us for an SM and at no more than 4.5 MB/us in so short a time.
 // A row of sums takes a single CTA 26 ns to write, a pair 4 ns; sums over a cluster cost 0.7 us and its barriers, more for wider tiles.
-// Examples (us): 1 row 1500 -> 6000: (single, tile 16, 1 part) 5.4, 3 parts 6.0. 128 rows 4096^2: (single, 32, 1) 10.4, (64, 1) 10.9,
-// (128, 1) 13.2, (128, 4) 13.0, pairs (64, 1) 11.8. 512 rows: pairs (128, 1) 12.0, single (128, 1) 14.1, pairs (192, 1) 14.8.
-// 2048 rows: pairs (160, 1) 30.7, (224, 1) 33.0, single (128, 1) 39.3.
+// Examples (us): 1 row 1500 -> 6000: (single, tile 16, 1 part) 5.4, 3 parts 6.0. 128 rows 4096^2: pairs (64, 1) 10.0, single (32, 1) 10.3,
+// (64, 1) 10.8, (128, 1) 13.2, (128, 4) 12.8. 512 rows: pairs (128, 1) 12.0, single (128, 1) 14.0, pairs (192, 1) 14.7.
+// 2048 rows: pairs (160, 1) 28.4, (224, 1) 32.1, single (128, 1) 39.7. 64 rows 9216 -> 4096: single (64, 3) 13.5, (32, 2) 13.8, (64, 1) 17.6.
 int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups, int dtype, bool trans, Shape &best)
 {
     const int quads = (groups + PJ_QUAD - 1) / PJ_QUAD;
@@ -163,7 +163,7 @@ int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups,
             if (fit < 1 || (parts > 1 && tiles > fit)) break;
             if (parts == 1) s.clusters = std::min(tiles, (long long)fit);
             const double rounds = (double)((tiles + fit - 1) / fit);
-            offer(s, 2 * s.clusters, rounds, 0.1 + 0.0011 * tile, PJ_A + 0.5 * GROUP * tile, 1.5 + 0.004 * tile * rounds + (parts > 1 ? 2.0 + 0.01 * tile + 0.5 * parts : 0.0));
+            offer(s, 2 * s.clusters, rounds, 0.1 + 0.0011 * tile, PJ_A + 0.5 * GROUP * tile, 0.5 + 0.004 * tile * rounds + (parts > 1 ? 2.0 + 0.01 * tile + 0.5 * parts : 0.0));
         }
     }
     return CONDENSA_OK;
