@@ -225,7 +225,7 @@ __device__ __forceinline__ void add_parts(const ProjectionParams &P, cooperative
 // are added, into room of their own, spared a barrier and took 1 to 7 us more.)
 // Four warps: copies, products, and two for the scales; then all take the sums.
 // Bound by launch, first copies and the end (3.9 us for 1 row 512 -> 512), then by the codes on their way: 1 row 1500 -> 6000: 5.1 us
-// (1.4 for 9 MB); 64 rows 9216 -> 4096: 12.5 us (5.9); 128 rows 4096^2: 11.0 us. All shared memory for the ring where the
+// (1.4 for 9 MB); 1 row 9216^2: 17.3 us (13.0), 4096 -> 33278: 23.5 us (20.9); 64 rows 9216 -> 4096: 13.5 us (5.9). All shared memory for the ring where the
 // CTAs are no more than SMs, since what is under way hides the latency (64 rows 9216 -> 4096 with half of it: 15.4 us).
 template <class T, bool TRANS>
 __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ ProjectionParams P)
