@@ -504,7 +504,7 @@ CONDENSA_API int condensa_projection_backward(condensa_ctx *ctx, const condensa_
  *             dx_ij = dh_ij + r_i * (t_ij - h_ij * r_i * q_i)        (the gradient of x and of the residual alike)
  *             dgain_j = sum over i of dy_ij * h_ij * r_i
  * x, residual, h, y, dy, dh and dx share `dtype` (CONDENSA_DTYPE_FP32, _FP16, _BF16), gain has `gain_dtype` (CONDENSA_DTYPE_FP32 or
- * dtype). Everything is formed in fp32 (a sum of squares beyond its range in fp64) and rounded once for each result, codes included. The gradient of a result in 8 bits is that of
+ * dtype). Everything is formed in fp32 (squares whose mean with eps is near or beyond either end of its range in fp64) and rounded once for each result, codes included. The gradient of a result in 8 bits is that of
  * the value ahead of the rounding. Sums over a row and over rows run in an order that depends on the shape and the device
  * only. An infinity in a row makes its place NaN and the row's other results 0, a NaN the whole row NaN. */
 typedef struct {

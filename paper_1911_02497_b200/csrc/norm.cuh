@@ -56,12 +56,16 @@ __device__ __forceinline__ F row_sum(F v, F *slots)
     return lanes_sum(lane < TPR / 32 ? slots[lane] : (F)0, 32);
 }
 
-// (the root's approximation, and one Newton step: every thread of a row does this, and quotients and roots in full were a tenth of the kernel)
-__device__ __forceinline__ float rstd_of(float sum, float inv_cols, float eps)
+// 1 / sqrt(x), x the mean of squares and eps (the root's approximation, and one Newton step: every thread of a row does this, and quotients and
+// roots in full were a tenth of the kernel)
+__device__ __forceinline__ float rstd_of(float x)
 {
-    const float x = fmaf(sum, inv_cols, eps), r = rsqrtf(x);
+    const float r = rsqrtf(x);
     return fmaf(r * 0.5f, fmaf(-x * r, r, 1.0f), r);
 }
+// Whether fp32 can be trusted with x: not where it or the squares' sum overflowed or is no number, nor where squares may have been
+// subnormal. Each of those lost at most 2^-150, so from 2^-100 on all of them lost less than 2^-50 of x.
+__device__ __forceinline__ bool in_fp32_range(float x) { return x >= 0x1p-100f && x <= 3.4e38f; }
 __device__ __forceinline__ float rstd_of(double sum, int cols, float eps) { return (float)(1.0 / sqrt(sum / cols + (double)eps)); }
 
 template <class T, int A>
@@ -158,8 +162,9 @@ __global__ void __launch_bounds__(RowThreads<TPR>::BLOCK) k_norm_forward(const _
         for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
     }
     sum = row_sum<TPR>(sum, slots);
-    float rstd = rstd_of(sum, P.inv_cols, P.eps);
-    if (!(sum <= 3.4e38f)) {                            // beyond fp32, or not a number (the same for the row)
+    const float mean = fmaf(sum, P.inv_cols, P.eps);
+    float rstd = rstd_of(mean);
+    if (!in_fp32_range(mean)) {                         // (the same for the row)
         double d = 0.0;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
