@@ -40,14 +40,7 @@ int code_map(condensa_ctx *ctx, CUtensorMap &map, const condensa_coded &c, long 
 
 typedef void (*Kernel)(ProjectionParams);
 
-constexpr int PJ_SMEM_MOST = 227 * 1024, PJ_SMEM_HALF = 113 * 1024, PJ_MAX_PARTS = 8, PP_MAX_PARTS = 4;
-
-// How a product is cut.
-struct Shape {
-    bool pair;              // pairs of CTAs, or single ones
-    int tile, parts;        // rows of a tile; CTAs (pairs) that share its depth
-    long long clusters;     // CTAs (pairs) launched: one per tile and part, or as many as the device holds at once
-};
+constexpr int PJ_SMEM_MOST = 227 * 1024, PJ_SMEM_HALF = 113 * 1024;
 
 struct Variant {
     Kernel f;
@@ -56,7 +49,7 @@ struct Variant {
 };
 
 template <class T, bool TRANS>
-Variant variant_of(const Shape &s)
+Variant variant_of(const ProjectionCut &s)
 {
     if (!s.pair) return {k_projection<T, TRANS>, PJ_WIDE, 128, PJ_PAD + PJ_SLOTS * PJ_SCALES, PJ_STAGES, true};
     const int fixed = PJ_PAD + PJ_SLOTS * PP_SCALES + PP_OUT;
@@ -64,7 +57,7 @@ Variant variant_of(const Shape &s)
     return {k_projection_pair<T, TRANS, false>, 2 * PJ_WIDE, PP_THREADS, fixed, PP_STAGES, false};
 }
 
-Variant variant_of(int dtype, bool trans, const Shape &s)
+Variant variant_of(int dtype, bool trans, const ProjectionCut &s)
 {
     return dtype == CONDENSA_DTYPE_BF16 ? (trans ? variant_of<__nv_bfloat16, true>(s) : variant_of<__nv_bfloat16, false>(s))
                                         : (trans ? variant_of<__half, true>(s) : variant_of<__half, false>(s));
@@ -106,69 +99,6 @@ int resident_clusters(condensa_ctx *ctx, const Variant &v, int n, int &count)
     return CONDENSA_OK;
 }
 
-// The cut that a simple account in microseconds makes cheapest; its figures are measured (the start and end of a launch are left out but for
-// what differs). A group of the depth costs a CTA by itself 150 ns and 0.6 for each row of the tile, one of a pair 100 and 1.1, and all
-// their codes pass L2 at 13 MB/us. Codes come from memory at 70 KB/us for an SM and at no more than 4.5 MB/us in so short a time.
-// A row of sums takes a single CTA 26 ns to write, a pair 4 ns; sums over a cluster cost 0.7 us and its barriers, more for wider tiles.
-// Examples (us): 1 row 1500 -> 6000: (single, tile 16, 1 part) 5.4, 3 parts 6.0. 128 rows 4096^2: pairs (64, 1) 10.0, single (32, 1) 10.3,
-// (64, 1) 10.8, (128, 1) 13.2, (128, 4) 12.8. 512 rows: pairs (128, 1) 12.0, single (128, 1) 14.0, pairs (192, 1) 14.7.
-// 2048 rows: pairs (160, 1) 28.4, (224, 1) 32.1, single (128, 1) 39.7. 64 rows 9216 -> 4096: single (64, 3) 13.5, (32, 2) 13.8, (64, 1) 17.6.
-int choose_shape(condensa_ctx *ctx, long long rows, long long width, int groups, int dtype, bool trans, Shape &best)
-{
-    const int quads = (groups + PJ_QUAD - 1) / PJ_QUAD;
-    const double sms = ctx->num_sms, codes = (double)groups * GROUP * (double)(width + rows);
-    double least = 0.0;
-    auto offer = [&](const Shape &s, long long ctas, double rounds, double group, double bytes, double more) {
-        const double depth = (double)((quads + s.parts - 1) / s.parts * PJ_QUAD), busy = std::min((double)ctas, sms);
-        const double t = std::max(rounds * depth * std::max(group, bytes * busy / 13e6), codes / std::min(4.5e6, 70e3 * busy)) + more;
-        if (least == 0.0 || t < 0.99 * least) {
-            least = t;
-            best = s;
-        }
-    };
-    const auto cut = [&](int most, int step) {          // rows of equal tiles of at most so many
-        const long long n = (rows + most - 1) / most;
-        return (int)(((rows + n - 1) / n + step - 1) / step * step);
-    };
-    int before = 0;
-    for (int most = PJ_MAX_TILE; most >= 16; most -= 16) {
-        const int tile = cut(most, 16);
-        if (tile == before) continue;
-        before = tile;
-        const long long tiles = (rows + tile - 1) / tile * ((width + PJ_WIDE - 1) / PJ_WIDE);
-        for (int parts = 1; parts <= std::min(PJ_MAX_PARTS, quads); ++parts) {
-            const Shape s = {false, tile, parts, tiles * parts};
-            const long long ctas = tiles * parts;
-            const double rounds = (double)((ctas + ctx->num_sms - 1) / ctx->num_sms);
-            if (parts > 1) {
-                int fit = 0;
-                const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), parts, fit);
-                if (rc) return rc;
-                if (tiles > fit) break;
-            }
-            offer(s, ctas, rounds, 0.15 + 0.0006 * tile, PJ_A + (double)GROUP * tile, 0.026 * tile * rounds + (parts > 1 ? 0.7 + 0.3 * parts + 0.006 * tile : 0.0));
-        }
-    }
-    before = 0;
-    for (int most = PP_TILE; rows > 64 && most >= 64; most -= 16) {
-        const int tile = cut(most, 16);
-        if (tile == before) continue;
-        before = tile;
-        const long long tiles = (rows + tile - 1) / tile * ((width + 2 * PJ_WIDE - 1) / (2 * PJ_WIDE));
-        for (int parts = 1; parts <= std::min(PP_MAX_PARTS, quads); ++parts) {
-            Shape s = {true, tile, parts, tiles * parts};
-            int fit = 0;
-            const int rc = resident_clusters(ctx, variant_of(dtype, trans, s), 2 * parts, fit);
-            if (rc) return rc;
-            if (fit < 1 || (parts > 1 && tiles > fit)) break;
-            if (parts == 1) s.clusters = std::min(tiles, (long long)fit);
-            const double rounds = (double)((tiles + fit - 1) / fit);
-            offer(s, 2 * s.clusters, rounds, 0.1 + 0.0011 * tile, PJ_A + 0.5 * GROUP * tile, 0.5 + 0.004 * tile * rounds + (parts > 1 ? 2.0 + 0.01 * tile + 0.5 * parts : 0.0));
-        }
-    }
-    return CONDENSA_OK;
-}
-
 int run(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x, long long rows, void *y, long long ldy, int dtype, bool trans,
         cudaStream_t stream)
 {
@@ -199,8 +129,11 @@ int run(condensa_ctx *ctx, const condensa_projection *w, const condensa_coded *x
     P.groups = (int)((depth + GROUP - 1) / GROUP);
     P.access = op_access(y, ldy, 2, width);
     const int quads = (P.groups + PJ_QUAD - 1) / PJ_QUAD;
-    Shape shape;
-    if ((rc = choose_shape(ctx, rows, width, P.groups, dtype, trans, shape)) != 0) return rc;
+    ProjectionCut shape;
+    rc = choose_cut(rows, width, P.groups, ctx->num_sms, [&](const ProjectionCut &s, int n, int &count) {
+        return resident_clusters(ctx, variant_of(dtype, trans, s), n, count);
+    }, shape);
+    if (rc) return rc;
     const Variant v = variant_of(dtype, trans, shape);
     const int high = shape.pair ? shape.tile / 2 : shape.tile, stage = PJ_A + high * GROUP, deepest = (quads + shape.parts - 1) / shape.parts * PJ_QUAD;
     P.tile = shape.tile;

@@ -12,20 +12,18 @@
 #include <cuda.h>
 
 #include "coded.cuh"
+#include "projection_cut.h"
 
 namespace cs {
 
-constexpr int PJ_WIDE = 128;            // output columns of a tile
-constexpr int PJ_QUAD = 4;              // groups of the depth whose scales share a word
+static_assert(PJ_GROUP == GROUP, "columns that share a scale");
 constexpr int PJ_STAGES = 12;           // most stages of the ring
 // Two warps bring the scales, two quads at a time and in turn: a warp's loads for its next two are on their way while it waits for
 // room. (One warp, a quad at a time, kept the products waiting: 2.2 PFLOP/s.)
 // A slot is a place in shared memory and one in tensor memory: it is filled again when the products of its batch are complete.
 constexpr int PJ_BATCH = 2, PJ_SLOTS = 2 * PJ_BATCH;    // quads
-constexpr int PJ_A = GROUP * PJ_WIDE;   // bytes of a stage's weights
 constexpr int PJ_SCALES = 1024;         // bytes of a quad's scales: weights, rows
 constexpr int PJ_PAD = 1024;            // swizzle patterns start at multiples of 1024 bytes
-constexpr int PJ_MAX_TILE = 128;        // rows of a tile
 
 struct ProjectionParams {
     CUtensorMap w, x;                   // codes, boxes of 128 bytes x 128 resp. `tile` rows
@@ -399,7 +397,6 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
 // a 128-byte piece of a row that starts anywhere is two lines.
 constexpr int PP_OUT_WARPS = 8;         // warps that write results: two for each 32 lanes of tensor memory, in turn
 constexpr int PP_THREADS = 128 + 32 * PP_OUT_WARPS;
-constexpr int PP_TILE = 224;            // most rows of a tile: two accumulators and the scales fill tensor memory
 constexpr int PP_STAGES = 8;
 constexpr int PP_SCALES = 1536;         // bytes of a quad's scales: weights, rows
 constexpr int PP_COLUMNS = 512;
