@@ -106,31 +106,40 @@ __device__ __forceinline__ void tmem_ld_wait(float (&v)[N])
 }
 
 // The scale bytes of a quad on their way to shared memory: those of 128 output columns' weights, the same for all of them, and
-// those of the rows `lane`, `lane` + 32, ... of a tile. Nothing here is looked at before it is stored, so that all loads leave together.
+// those of the rows `lane`, `lane` + 32, ... of a tile. Nothing here is looked at before it is stored, so that all loads leave together. Bytes
+// that fill up a row's last word are not scales and are not read. Of three that are left there the third is another load: by pairs, which take
+// tile after tile, it is kept apart (8000 rows 300 -> 8000: 42.6 us, joined at once 46.8), by a CTA with one tile it is joined at once (32 rows
+// 6000 -> 1500: 7.9 us, kept apart 8.2).
 template <int N>
 struct QuadScales {
-    u32 w[PJ_QUAD], x[N];
+    static constexpr bool APART = N > 4;
+    u32 w[PJ_QUAD], x[N], third[N];
 
     __device__ __forceinline__ void fetch(const ProjectionParams &P, int quad, long long block, long long row)
     {
         const u8 *s = P.w_scales + min(block, (long long)(P.width - 1) / GROUP) * P.w_wide;
-        const int g = quad * PJ_QUAD;
+        const int g = quad * PJ_QUAD, left = P.groups - g;
 #pragma unroll
         for (int b = 0; b < PJ_QUAD; ++b) w[b] = s[min(g + b, P.groups - 1) * P.w_depth];       // (past the last group: anything, it is not used)
 #pragma unroll
-        for (int c = 0; c < N; ++c)
+        for (int c = 0; c < N; ++c) {
+            third[c] = 0;
             if (c * 32 < P.tile) {
                 const long long r = min(row + c * 32, P.rows - 1);      // (past the last row: the same)
                 const u8 *at = P.x_scales + r * P.ld_xs + g;
-                if (g + PJ_QUAD <= P.groups || r + 1 < P.rows) {
-                    x[c] = *reinterpret_cast<const u32 *>(at);          // a row's last word lies within its stride ...
-                } else {                                                // ... but for the last row, which may end with its groups
-                    x[c] = 0;
-                    for (int b = 0; g + b < P.groups; ++b) x[c] |= (u32)at[b] << (8 * b);
+                if (left >= PJ_QUAD) {
+                    x[c] = *reinterpret_cast<const u32 *>(at);
+                } else {
+                    x[c] = left >= 2 ? *reinterpret_cast<const u16 *>(at) : at[0];
+                    if (left == 3) {
+                        if (APART) third[c] = at[2];
+                        else x[c] |= (u32)at[2] << 16;
+                    }
                 }
             } else {
                 x[c] = 0;
             }
+        }
     }
     // 512 bytes for the weights, 512 for each 128 rows: 32 lanes of four words
     __device__ __forceinline__ void store(char *to, int lane) const
@@ -138,8 +147,9 @@ struct QuadScales {
         const u32 a = w[0] | w[1] << 8 | w[2] << 16 | w[3] << 24;
         uint4 *d = reinterpret_cast<uint4 *>(to) + lane;
         d[0] = make_uint4(a, a, a, a);
+        const auto row = [&](int c) { return c < N ? x[c < N ? c : 0] | third[c < N ? c : 0] << 16 : 0u; };
 #pragma unroll
-        for (int i = 0; i < (N + 3) / 4; ++i) d[32 * (i + 1)] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], 4 * i + 3 < N ? x[4 * i + 3 < N ? 4 * i + 3 : 0] : 0u);
+        for (int i = 0; i < (N + 3) / 4; ++i) d[32 * (i + 1)] = make_uint4(row(4 * i), row(4 * i + 1), row(4 * i + 2), row(4 * i + 3));
     }
 };
 

@@ -49,3 +49,28 @@ def test_large_products(ctx, rows, width, depth, back):
         assert not bool(got.isnan().any()) and bool((y[rows] == 7).all())
         bound = HALF[dtype] * want.abs() + LEAST[dtype] + (33 * depth / 32 + 40) * E * size * (1 + HALF[dtype])
         assert bool(((got.clamp(-top, top) - want.clamp(-top, top)).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("rows", [1, 40, 700])
+@pytest.mark.parametrize("depth", [100, 200, 300, 500, 600, 800])
+def test_what_fills_rows_up_has_no_part(ctx, rows, depth, back):
+    """One to four groups in the last word of a row's scales; the bytes behind codes and scales are those of no number, then zeros."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(depth)
+    width = 520
+    results = []
+    w, W = _coded(depth if back else width, width if back else depth, GROUP, g)
+    x, X = _coded(rows, depth, 1, g)
+    for fill in (255, 0):
+        for c in (w, x):
+            for part in (c.codes.view(torch.uint8), c.scales):
+                n, apart = part.shape[0], part.stride(0)
+                torch.as_strided(part, (n, apart), (apart, 1))[:, part.shape[1]:] = fill
+        y = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
+        (ctx.projection_backward if back else ctx.projection_forward)(w, x, y)
+        results.append(y)
+    want, size = X @ (W if back else W.t()), X.abs() @ (W if back else W.t()).abs()
+    bound = HALF["bfloat16"] * want.abs() + (33 * depth / 32 + 40) * E * size * (1 + HALF["bfloat16"])
+    assert torch.equal(*results) and bool(((results[0].double() - want).abs() <= bound).all())
