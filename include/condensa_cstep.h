@@ -457,7 +457,9 @@ CONDENSA_API int condensa_adapter_backward(condensa_ctx *ctx, const condensa_ada
  * finite becomes the code of NaN and has no part in its group's scale. Scales being powers of two, only the code rounds.
  *
  * codes: 16-byte aligned, rows `ld` bytes apart, a multiple of 16 (a single row may have any multiple that holds it); bytes past
- * the columns are neither read nor written. scales: 4-byte aligned, rows `ld_scales` bytes apart, a multiple of 4; the same. */
+ * the columns are neither read nor written. scales: 4-byte aligned, rows `ld_scales` bytes apart, a multiple of 4; the same.
+ * Of the other matrices of these calls nothing past a row's columns is written; where rows begin at any alignment, the aligned 16 bytes that hold
+ * values of a row are read whole (not ahead of the matrix's first value, nor behind its last), and what else lies there has no part in the result. */
 #define CONDENSA_CODE_GROUP 128
 
 typedef struct {

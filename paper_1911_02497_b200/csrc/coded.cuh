@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "common.cuh"
+#include "pieces.h"
 
 namespace cs {
 
@@ -150,11 +151,12 @@ __device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
 }
 
 // The same in two steps, so that several loads can be under way: ask8() loads, take8() makes the eight values of it. Of rows that begin
-// anywhere the aligned pieces are loaded that hold the values; they may reach into the neighbouring rows, or between them, but not out of
-// the matrix (`off`: where the row begins in it, `total`: where it ends). 32-bit values, which would take three pieces, come as eights at once.
+// anywhere the aligned pieces are loaded that hold the values. What else lies in such 16 bytes is read with them, of the neighbouring rows or
+// between them, but no piece without a value of the row, and nothing out of the matrix (`off`: where the row begins in it, `total`: where it
+// ends). 32-bit values, which would take three pieces, come as eights at once.
 template <class T>
 struct Pieces {
-    static constexpr int V = 8, N = 2;                  // values of a piece, pieces
+    static constexpr int V = PIECE, N = 2;              // values of a piece, pieces
     uint4 p[N];
 };
 template <int A, class T> using Asked = typename std::conditional<A == 1 && sizeof(T) == 2, Pieces<T>, Eight<T>>::type;
@@ -168,7 +170,7 @@ __device__ __forceinline__ Asked<A, T> ask8(const T *base, long long off, long l
         typedef Pieces<T> P;
         P a;
         const long long at = off + c;
-        const int by = (int)(reinterpret_cast<uintptr_t>(base + at) % 16 / sizeof(T)), n = by ? P::N : P::N - 1;
+        const int by = (int)(reinterpret_cast<uintptr_t>(base + at) % 16 / sizeof(T)), n = second_piece(by, c, cols) ? P::N : P::N - 1;
         const long long start = at - by;
 #pragma unroll
         for (int i = 0; i < P::N; ++i) a.p[i] = make_uint4(0, 0, 0, 0);
@@ -182,7 +184,7 @@ __device__ __forceinline__ Asked<A, T> ask8(const T *base, long long off, long l
                 T *v = reinterpret_cast<T *>(a.p);
 #pragma unroll
                 for (int i = 0; i < P::N * P::V; ++i)
-                    if (start + i >= 0 && start + i < total) v[i] = base[start + i];
+                    if (start + i >= 0 && start + i < total && i < n * P::V) v[i] = base[start + i];
             }
         }
         return a;
