@@ -23,7 +23,7 @@ SOURCES = {
     "norm_bf16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "norm_launch.cuh", "norm_kernels.cuh", API_H],
     "norm_f16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "norm_launch.cuh", "norm_kernels.cuh", API_H],
     "norm_f32.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "norm_launch.cuh", "norm_kernels.cuh", API_H],
-    "projection.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "projection.cuh", "projection_cut.h", API_H],
+    "projection.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "projection.cuh", "projection_cut.h", "ring.h", API_H],
     "adamw.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adamw.cuh", API_H],
 }
 

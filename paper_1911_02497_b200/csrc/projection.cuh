@@ -13,6 +13,7 @@
 
 #include "coded.cuh"
 #include "projection_cut.h"
+#include "ring.h"
 
 namespace cs {
 
@@ -241,7 +242,7 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
     extern __shared__ char pj_raw[];
     __shared__ u64 bars[2 * PJ_STAGES + 4 + 1];
     __shared__ u32 s_tmem;
-    __shared__ int s_fail;
+    __shared__ int s_fail, s_issued;
     char *ring = pj_raw + ((PJ_PAD - (smem_u32(pj_raw) & (PJ_PAD - 1))) & (PJ_PAD - 1));
     char *scales = ring + P.ring;
     const u32 ring_u = smem_u32(ring), scales_u = smem_u32(scales);
@@ -286,9 +287,9 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
 
     if (warp == 0) {                    // ---- copies
         if (elect_one()) {
-            int stage = 0;
+            int stage = 0, g = g0;
             u32 turn = 0;
-            for (int g = g0; g < g1; ++g) {
+            for (; g < g1; ++g) {
                 if (g - g0 >= P.stages && !mbar_wait(empty + 8 * stage, turn ^ 1)) {
                     s_fail = 1;
                     break;
@@ -303,6 +304,7 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
                     turn ^= 1;
                 }
             }
+            s_issued = g - g0;
         }
     } else if (warp == 1) {             // ---- products
         if (elect_one()) {
@@ -370,10 +372,8 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
     bool fine = mbar_wait(done, 0);
     __syncthreads();
     fine = fine && !s_fail;
-    if (!fine && tid == 0) {            // a wait ran out: the results are no numbers, but no copy lands in what comes next
-        const int n = g1 - g0;
-        for (int i = max(0, n - P.stages); i < n; ++i) mbar_wait(full + 8 * (i % P.stages), (u32)(i / P.stages) & 1);
-    }
+    if (!fine && tid == 0)              // a wait ran out: the results are no numbers, but no copy lands in what comes next
+        copies_under_way(s_issued, P.stages, [&](int s, int parity) { mbar_wait(full + 8 * s, (u32)parity); });
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     float *sums = reinterpret_cast<float *>(ring);                      // [row][128 output columns]
@@ -560,11 +560,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
                     }
                 }
             }
-            if (!fine) {                // a wait ran out: the results are no numbers, but no copy lands in what comes next
-                s_fail = 1;
-                for (int i = max(0, issued - P.stages); i < issued; ++i)
-                    mbar_wait(side == 0 ? full + 8 * (i % P.stages) : empty + 8 * (i % P.stages), (u32)(i / P.stages) & 1);
-            }
+            if (!fine) s_fail = 1;      // a wait ran out: the results are no numbers
+            // Whichever warp gave up, no copy lands in what comes next: the leader, at whose barriers both CTAs' copies are counted,
+            // waits for all of them ahead of the cluster's last barrier. (Nobody waits for this: the products are behind it.)
+            if (side == 0) copies_under_way(issued, P.stages, [&](int s, int parity) { mbar_wait(full + 8 * s, (u32)parity); });
         }
     } else if (warp == 1) {             // ---- products, issued by the leader
         if (side == 0 && elect_one()) {
