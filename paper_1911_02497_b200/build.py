@@ -19,10 +19,10 @@ SOURCES = {
     "adapter_bf16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
     "adapter_f16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
     "adapter_f32.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adapter.cuh", "adapter_launch.cuh", "adapter_kernels.cuh", API_H],
-    "norm.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "norm_launch.cuh", API_H],
-    "norm_bf16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "norm_launch.cuh", "norm_kernels.cuh", API_H],
-    "norm_f16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "norm_launch.cuh", "norm_kernels.cuh", API_H],
-    "norm_f32.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "norm_launch.cuh", "norm_kernels.cuh", API_H],
+    "norm.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "row_runs.h", "norm_launch.cuh", API_H],
+    "norm_bf16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "row_runs.h", "norm_launch.cuh", "norm_kernels.cuh", API_H],
+    "norm_f16.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "row_runs.h", "norm_launch.cuh", "norm_kernels.cuh", API_H],
+    "norm_f32.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "norm.cuh", "row_runs.h", "norm_launch.cuh", "norm_kernels.cuh", API_H],
     "projection.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "op_args.h", "coded.cuh", "pieces.h", "projection.cuh", "projection_cut.h", "ring.h", API_H],
     "adamw.cu": ["common.cuh", "ctx.cuh", "op_workspace.h", "ranges.h", "adamw.cuh", API_H],
 }

@@ -167,15 +167,12 @@ int encode_rows(condensa_ctx *ctx, const void *x, long long ldx, long long rows,
     P.rows = rows;
     P.cols = (int)cols;
     P.groups = (u32)((P.cols + GROUP - 1) / GROUP);
-    // runs of four groups, of two or of one, the longest that leave no more than a quarter of their places empty
-    const auto empty = [&](u32 n) { return (P.groups + n - 1) / n * n - P.groups; };
-    const int ng = 4 * empty(4) <= P.groups ? 4 : 4 * empty(2) <= P.groups ? 2 : 1;
-    P.runs = (P.groups + ng - 1) / ng;
-    P.reciprocal = P.runs == 1 ? 0xFFFFFFFFu : (u32)((1ull << 32) / P.runs);
-    const long long per = THREADS / GROUP_LANES * (ENC_UNITS / ng), grid = (rows * P.runs + per - 1) / per;
-    if (grid > 0x7FFFFFFFll) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "too many groups for one launch");
+    RowRuns plan;
+    if (!plan_row_runs(rows, P.groups, THREADS / GROUP_LANES, plan)) return fail(ctx, CONDENSA_ERR_TOO_LARGE, "too many groups for one launch");
+    P.runs = plan.runs;
+    P.reciprocal = plan.reciprocal;
     CU_TRY(ctx, cudaSetDevice(ctx->device));
-    return op_launch(ctx, "k_encode_rows", row_encoder(dtype, op_access(x, ldx, e, cols), ng), dim3((unsigned)grid), THREADS, stream, P);
+    return op_launch(ctx, "k_encode_rows", row_encoder(dtype, op_access(x, ldx, e, cols), plan.groups_of_run), dim3((unsigned)plan.grid), THREADS, stream, P);
 }
 
 int encode_blocks(condensa_ctx *ctx, const void *w, long long ldw, long long n, long long k, int dtype, const condensa_coded *out, float *theta, long long ld_theta,

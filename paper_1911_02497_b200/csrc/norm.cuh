@@ -6,6 +6,7 @@
 // is 16 neighbouring lanes, its largest magnitude four shuffles.
 #pragma once
 #include "coded.cuh"
+#include "row_runs.h"
 
 namespace cs {
 
@@ -513,8 +514,6 @@ struct EncodeParams {
     u32 runs, reciprocal;               // rows: runs of groups of a row; floor(2^32 / runs), at most 2^32 - 1
 };
 
-constexpr int ENC_UNITS = 4;            // groups of a half-warp, all of whose loads leave together
-
 // Largest magnitude of eight values as they lie in memory; no number if one of them is none. Patterns of 16-bit values
 // are compared two at a time.
 __device__ __forceinline__ float most_raw(const Eight<float> &e)
@@ -544,27 +543,16 @@ __global__ void __launch_bounds__(THREADS) k_encode_rows(const __grid_constant__
     pdl_launch_dependents();
     constexpr int HALVES = THREADS / GROUP_LANES, UNITS = ENC_UNITS / NG;
     const int half = threadIdx.x / GROUP_LANES, lane = threadIdx.x % GROUP_LANES;
-    const u64 units = (u64)P.rows * P.runs, first = (u64)blockIdx.x * (HALVES * UNITS) + half;
-    u64 row[UNITS];
+    const u32 units = (u32)P.rows * P.runs, first = blockIdx.x * (HALVES * UNITS) + half;
+    u32 row[UNITS];
     int c[UNITS];
     Asked<A, T> asked[UNITS][NG];
     const long long total = (P.rows - 1) * P.ldx + P.cols;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
-        const u64 u = first + i * HALVES;
+        const u32 u = first + i * HALVES;
         u32 g;
-        if (units >> 32) {
-            row[i] = u / P.runs;
-            g = (u32)(u - row[i] * P.runs);
-        } else {                        // (the estimate by the reciprocal is the quotient or one less)
-            u32 r = __umulhi((u32)u, P.reciprocal);
-            g = (u32)u - r * P.runs;
-            if (g >= P.runs) {
-                g -= P.runs;
-                r += 1;
-            }
-            row[i] = r;
-        }
+        place_of_run(u, P.runs, P.reciprocal, [](u32 a, u32 b) { return __umulhi(a, b); }, row[i], g);
         c[i] = u < units ? (int)g * (NG * GROUP) + lane * 8 : P.cols;    // (P.cols: nothing to read or write)
 #pragma unroll
         for (int k = 0; k < NG; ++k) asked[i][k] = ask8<A>((const T *)P.x, row[i] * P.ldx, total, c[i] + k * GROUP, P.cols);
