@@ -473,7 +473,8 @@ CONDENSA_API int condensa_encode_rows(condensa_ctx *ctx, const void *x, int64_t 
                                       int dtype, const condensa_coded *out, void *stream);
 
 /* w [n][k] (theta of a C-step, say) into the block form. theta (NULL: not written): the values that the codes stand for, fp32, so that
- * condensa_cstep_lagrange_update() can go by what the codes hold; it may be w itself (dtype fp32, same stride). */
+ * condensa_cstep_lagrange_update() can go by what the codes hold; it may be w itself (dtype fp32, same stride). Weights of 1.9375 * 2^127 or more, which are
+ * next to the largest of fp32, become codes for 2^128: infinite in theta. */
 CONDENSA_API int condensa_encode_blocks(condensa_ctx *ctx, const void *w, int64_t ldw, int64_t n, int64_t k, int dtype,
                                         const condensa_coded *out, float *theta, int64_t ld_theta, void *stream);
 
