@@ -1,5 +1,5 @@
 // What every source file of the host side shares: the context, error texts, per-kernel timing,
-// launch helpers, the workspace of the list operators and the adapters.
+// launch helpers, the workspace of the operators.
 #pragma once
 #include "../../include/condensa_cstep.h"
 
@@ -63,9 +63,9 @@ struct condensa_ctx {
     std::vector<double> prof_ms;            // accumulated per name
     std::vector<int64_t> prof_cnt;
     struct ClusterFit { const void *f; int size, count; };
-    std::vector<ClusterFit> cluster_fit;    // clusters of a kernel that the device holds at once
-    std::vector<const void *> op_smem_set;  // adapter kernels whose shared memory limit has been raised on this device
-    OpWorkspace op;                         // of the list operators and the adapters; apart from the C-step's
+    std::vector<ClusterFit> cluster_fit;    // clusters of a kernel that the device holds at once; size 0: CTAs of it that an SM holds
+    std::vector<const void *> op_smem_set;  // kernels of the adapters and of the 8-bit products whose shared memory limit has been raised on this device
+    OpWorkspace op;                         // of the list operators, the adapters and the norm's gradient; apart from the C-step's
 };
 
 inline int fail(condensa_ctx *c, int code, const char *fmt, ...)

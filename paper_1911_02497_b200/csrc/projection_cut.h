@@ -22,9 +22,9 @@ struct ProjectionCut {
 // what differs). A group of the depth costs a CTA by itself 150 ns and 0.6 for each row of the tile, one of a pair 100 and 1.1, and all
 // their codes pass L2 at 13 MB/us. Codes come from memory at 70 KB/us for an SM and at no more than 4.5 MB/us in so short a time.
 // A row of sums takes a single CTA 26 ns to write, a pair 4 ns; sums over a cluster cost 0.7 us and its barriers, more for wider tiles.
-// Examples (us): 1 row 1500 -> 6000: (single, tile 16, 1 part) 5.4, 3 parts 6.0. 128 rows 4096^2: pairs (64, 1) 10.0, single (32, 1) 10.3,
-// (64, 1) 10.8, (128, 1) 13.2, (128, 4) 12.8. 512 rows: pairs (128, 1) 12.0, single (128, 1) 14.0, pairs (192, 1) 14.7.
-// 2048 rows: pairs (160, 1) 28.4, (224, 1) 32.1, single (128, 1) 39.7. 64 rows 9216 -> 4096: single (64, 3) 13.5, (32, 2) 13.8, (64, 1) 17.6.
+// Examples (us; chosen first): 1 row 1500 -> 6000: (single, tile 16, 1 part) 5.3, 3 parts 5.8. 128 rows 4096^2: pairs (64, 1) 9.7, single (32, 1)
+// 10.2, (64, 2) 10.6. 512 rows: pairs (128, 1) 11.5, (176, 1) 13.4, single (128, 1) 14.1. 2048 rows: pairs (160, 1) 27.9, (176, 1) 29.0. 64 rows
+// 9216 -> 4096: single (32, 2) 13.6, (64, 3) 13.4. Over 16 shapes the choice took at most 4 % more than the best of all cuts.
 //
 // fit(cut, n, count): clusters of n CTAs of the cut's kernel that the device holds at once; what it returns other than 0 is returned.
 template <class Fit>
