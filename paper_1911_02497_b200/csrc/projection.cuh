@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(128, 2) k_projection(const __grid_constant__ P
         }
     }
     __syncwarp();
-    bool fine = mbar_wait(done, 0);
+    bool fine = mbar_wait(done, 0);     // (the last commit of the thread whose commits arrive here: those ahead of it are through)
     __syncthreads();
     fine = fine && !s_fail;
     if (!fine && tid == 0)              // a wait ran out: the results are no numbers, but no copy lands in what comes next
@@ -562,10 +562,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
                     }
                 }
             }
-            if (!fine) s_fail = 1;      // a wait ran out: the results are no numbers
-            // Whichever warp gave up, no copy lands in what comes next: the leader, at whose barriers both CTAs' copies are counted,
-            // waits for all of them ahead of the cluster's last barrier. (Nobody waits for this: the products are behind it.)
-            if (side == 0) copies_under_way(issued, P.stages, [&](int s, int parity) { mbar_wait(full + 8 * s, (u32)parity); });
+            // The leader's commits arrive in both CTAs: each is waited for before a CTA ends. (Nobody waits for this: the products are behind it.)
+            copies_under_way(issued, P.stages, [&](int s, int parity) { fine = fine && mbar_wait(empty + 8 * s, (u32)parity); });
+            if (!fine) {                // a wait ran out, here or in a warp that this one heard no more of: the results are no numbers
+                s_fail = 1;
+                // No copy lands in what comes next: the leader, at whose barriers both CTAs' copies are counted, waits for all of them
+                // ahead of the cluster's last barrier.
+                if (side == 0) copies_under_way(issued, P.stages, [&](int s, int parity) { mbar_wait(full + 8 * s, (u32)parity); });
+            }
         }
     } else if (warp == 1) {             // ---- products, issued by the leader
         if (side == 0 && elect_one()) {
@@ -637,11 +641,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
         if (turns) pass();
         fetch();
         u32 phase = 0;
+        bool fine = true;
         for (long long i = turns * PJ_BATCH; i < all; i += PJ_SLOTS, phase ^= 1) {
-            if (i >= PJ_SLOTS && !mbar_wait(sc_empty + 8 * turns, phase ^ 1)) {
-                s_fail = 1;
-                break;
-            }
+            fine = i < PJ_SLOTS || mbar_wait(sc_empty + 8 * turns, phase ^ 1);
+            if (!fine) break;
 #pragma unroll
             for (int j = 0; j < PJ_BATCH; ++j)
                 if (i + j < all) next[j].store(scales + (turns * PJ_BATCH + j) * PP_SCALES, lane);
@@ -651,6 +654,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) k_projection_pair(const __grid_
             pass();
             fetch();
         }
+        if (fine && last_batch_commits(all, PJ_BATCH, turns)) fine = mbar_wait(sc_empty + 8 * turns, phase ^ 1);
+        if (!fine) s_fail = 1;
     } else if (warp >= 4) {             // ---- results
         const u32 empty_at = peer_address(acc_empty, leader);
         const int w = warp & 3, turns = (warp - 4) / 4;
